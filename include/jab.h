@@ -341,6 +341,98 @@ jab_status jab_selftest_bounds_check(int32_t* buf_dev, int32_t n, jab_stream_t s
  * (JAB_OK if no kernel reported a problem since the last call). */
 jab_status jab_get_device_status(jab_stream_t stream);
 
+/* ---- Serving a fitted block ---------------------------------------------------------------------
+ * What runs a block whose weights have been quantised on new tokens: its joint projection in 8-bit
+ * integers, a paged key / value cache that is quantised as it is written, and attention over it.
+ * Codes are symmetric (Eq. 2 with one scale per row): s = fl32(max|x| / qmax), q = clip(rint(fl32(x /
+ * s)), -qmax, qmax), qmax = 2^(bits-1) - 1; a row of zeros has s = 0 and codes 0. A row with an
+ * infinity or a NaN gets a NaN scale, so that what is computed from it is NaN, and raises
+ * JAB_ERR_NONFINITE on the device. Row pitches (ld*) are in elements; rows start on 16 bytes. Index
+ * arrays on the device are checked there: a value out of range raises JAB_ERR_INVALID_ARG in the
+ * device status, and nothing outside the caller's buffers is read or written for it. */
+typedef enum { JAB_FP16 = 0, JAB_BF16 = 1, JAB_FP32 = 2 } jab_dtype;
+
+/* A paged cache of one block, device buffers owned by the caller:
+ *   k_codes, v_codes    bytes [n_pages, n_kv_heads, page_tokens, head_dim * bits / 8], 16-byte aligned:
+ *                       8 bits: q + 128; 4 bits: q + 8, element 2i in the low half of byte i
+ *   k_scales, v_scales  fp32 [n_pages, n_kv_heads, page_tokens]
+ * head_dim 64 or 128, bits 8 or 4, page_tokens a multiple of 16 up to 4096. */
+typedef struct {
+  int32_t n_kv_heads, head_dim, bits, page_tokens;
+  int64_t n_pages;
+  void* k_codes;
+  void* v_codes;
+  float* k_scales;
+  float* v_scales;
+} jab_kv_cache;
+
+/* Y[m, n] = s_m w_n sum_k qx[m, k] codes[n, k]: the rows of X are quantised to 8 bits (one scale s_m per
+ * token), the sum is exact (whole numbers), and the two products by the scales are rounded to fp32 before
+ * the result is rounded to y_type.
+ *   X_dev         x_type (JAB_FP16 or JAB_BF16) [M, K], pitch ldx
+ *   codes_dev     int8 [N, K] (jab_quantize with group_size = d_model, any bit width), 16-byte aligned
+ *   w_scales_dev  fp32 [N]
+ *   Y_dev         out y_type [M, N], pitch ldy
+ * K a multiple of 16 up to 131072; M >= 0 (0: nothing to do), N >= 1. ws 256-byte aligned. */
+size_t jab_quantized_linear_workspace_size(int64_t M, int32_t N, int32_t K);
+jab_status jab_quantized_linear(int64_t M, int32_t N, int32_t K, const void* X_dev, jab_dtype x_type,
+                                int64_t ldx, const int8_t* codes_dev, const float* w_scales_dev,
+                                void* Y_dev, jab_dtype y_type, int64_t ldy, void* ws, size_t ws_bytes,
+                                jab_stream_t stream);
+
+/* cos and sin of position * theta^(-2j / head_dim), fp32 [length, head_dim / 2] each: the rotation
+ * table that jab_kv_write reads. */
+jab_status jab_rope_table(int32_t length, int32_t head_dim, float theta, float* cos_dev, float* sin_dev,
+                          jab_stream_t stream);
+
+/* New tokens into the cache: rows [Q | K | V] of the joint projection. Q and K are rotated at the token's
+ * position (rotate-half; each product and sum rounded to fp32), K and V quantised per (token, head) and
+ * written to the token's slot.
+ *   X_dev          type [n_tokens, (n_q_heads + 2 n_kv_heads) * head_dim], pitch ldx
+ *   slots_dev      int64 [n_tokens]: page * page_tokens + place in the page; < 0: padding, of which
+ *                  nothing is read or written. Two tokens must not share a slot.
+ *   positions_dev, cos_dev, sin_dev   int32 [n_tokens] and fp32 [rope_len, head_dim / 2]; all NULL: no
+ *                  rotation
+ *   Q_dev          out type [n_tokens, n_q_heads * head_dim] (no pitch), or NULL
+ * type is JAB_FP16, JAB_BF16 or JAB_FP32. */
+jab_status jab_kv_write(const jab_kv_cache* cache, int64_t n_tokens, int32_t n_q_heads, const void* X_dev,
+                        jab_dtype type, int64_t ldx, const int64_t* slots_dev,
+                        const int32_t* positions_dev, const float* cos_dev, const float* sin_dev,
+                        int32_t rope_len, void* Q_dev, jab_stream_t stream);
+
+/* Cached tokens as numbers: tokens starts[b] .. starts[b] + counts[b] - 1 of every sequence.
+ *   pages_dev   int32 [n_seqs, max_pages]: token j of sequence b is in page pages[b, j / page_tokens]
+ *   starts_dev  int32 [n_seqs] or NULL (0); counts_dev int32 [n_seqs]
+ *   K_dev, V_dev  out type [n_seqs, T, n_kv_heads, head_dim]; tokens from counts[b] on are 0 */
+jab_status jab_kv_read(const jab_kv_cache* cache, int32_t n_seqs, const int32_t* pages_dev,
+                       int32_t max_pages, const int32_t* starts_dev, const int32_t* counts_dev, int32_t T,
+                       void* K_dev, void* V_dev, jab_dtype type, jab_stream_t stream);
+
+/* Attention of new tokens over the cache. Sequence b has the query rows q_start[b] .. q_start[b + 1] - 1
+ * of Q, the last ones of its seq_lens[b] cached tokens (they are in the cache already): query i of n sees
+ * key j when j <= p and, with window > 0, j > p - window, where p = seq_lens[b] - n + i. A row
+ * that sees nothing has output 0 and log-sum-exp -inf.
+ *   Q_dev        type (JAB_FP16 or JAB_BF16) [n_tokens, n_q_heads * head_dim], pitch ldq
+ *   q_start_dev  int32 [n_seqs + 1], increasing from 0 to n_tokens
+ *   pages_dev    int32 [n_seqs, max_pages], seq_lens_dev int32 [n_seqs]
+ *   max_q_len, max_seq_len   the longest of the sequences, or more: they set how the work is cut up, not
+ *                what is computed
+ *   shared_len   the first shared_len cached tokens (a multiple of page_tokens, 0: none) are in the same
+ *                pages for all sequences: they are read through the first sequence's row, once for all
+ *   softmax_scale  <= 0 selects 1/sqrt(head_dim)
+ *   O_dev        out type [n_tokens, n_q_heads * head_dim], pitch ldo
+ *   lse_dev      out fp32 [n_tokens, n_q_heads] or NULL: natural log-sum-exp of the scaled scores
+ * n_q_heads a multiple of n_kv_heads; n_seqs up to 4096; ws 256-byte aligned. */
+size_t jab_kv_attention_workspace_size(const jab_kv_cache* cache, int32_t n_seqs, int64_t n_tokens,
+                                       int32_t n_q_heads, int32_t max_q_len, int32_t max_seq_len,
+                                       int32_t shared_len);
+jab_status jab_kv_attention(const jab_kv_cache* cache, int32_t n_seqs, int64_t n_tokens,
+                            int32_t n_q_heads, const void* Q_dev, jab_dtype type, int64_t ldq,
+                            const int32_t* q_start_dev, const int32_t* pages_dev, int32_t max_pages,
+                            const int32_t* seq_lens_dev, int32_t max_q_len, int32_t max_seq_len,
+                            int32_t shared_len, int32_t window, float softmax_scale, void* O_dev,
+                            int64_t ldo, float* lse_dev, void* ws, size_t ws_bytes, jab_stream_t stream);
+
 /* ---- Instrumentation (not part of the method): per-launch-site device time with CUDA events. ----
  * jab_timing_enable(1) makes every later entry-point call record a CUDA event pair on its stream
  * around each of its kernel launch sites. jab_timing_collect synchronises those events and folds

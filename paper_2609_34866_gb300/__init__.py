@@ -15,4 +15,6 @@ from .binding import (  # noqa: F401
     jab_loss_backward_scales_prepared, jab_flip_rate, jab_reference_projection,
     jab_loss_forward_kl, jab_hutchinson_trace, jab_omega_scores, jab_rademacher_probes,
     jab_set_deterministic, jab_selftest_bounds_check, jab_loss_backward_scales_kl,
+    KvCache, jab_quantized_linear, jab_quantized_linear_workspace_size, jab_rope_table, jab_kv_write,
+    jab_kv_read, jab_kv_attention, jab_kv_attention_workspace_size,
 )

@@ -52,6 +52,15 @@ def desc_from_shape(shape, group_size: int) -> BlockDesc:
                      1 if shape.use_rope else 0, float(shape.rope_theta), 0.0)
 
 
+class _KvCacheDesc(ctypes.Structure):
+    """jab_kv_cache"""
+
+    _fields_ = [("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("bits", ctypes.c_int32),
+                ("page_tokens", ctypes.c_int32), ("n_pages", ctypes.c_int64),
+                ("k_codes", ctypes.c_void_p), ("v_codes", ctypes.c_void_p),
+                ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p)]
+
+
 _P = ctypes.c_void_p
 _LIB = None
 
@@ -107,7 +116,20 @@ def lib() -> ctypes.CDLL:
     L.jab_timing_get.argtypes = [i32, ctypes.POINTER(ctypes.c_char_p), ctypes.POINTER(ctypes.c_double),
                                  ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(ctypes.c_int64)]
     L.jab_timing_reset.argtypes = []
+    KV = ctypes.POINTER(_KvCacheDesc)
+    i64 = ctypes.c_int64
+    L.jab_quantized_linear_workspace_size.argtypes = [i64, i32, i32]
+    L.jab_quantized_linear_workspace_size.restype = sz
+    L.jab_quantized_linear.argtypes = [i64, i32, i32, _P, i32, i64, _P, _P, _P, i32, i64, _P, sz, _P]
+    L.jab_rope_table.argtypes = [i32, i32, f32, _P, _P, _P]
+    L.jab_kv_write.argtypes = [KV, i64, i32, _P, i32, i64, _P, _P, _P, _P, i32, _P, _P]
+    L.jab_kv_read.argtypes = [KV, i32, _P, i32, _P, _P, i32, _P, _P, i32, _P]
+    L.jab_kv_attention_workspace_size.argtypes = [KV, i32, i64, i32, i32, i32, i32]
+    L.jab_kv_attention_workspace_size.restype = sz
+    L.jab_kv_attention.argtypes = [KV, i32, i64, i32, _P, i32, i64, _P, _P, i32, _P, i32, i32, i32, i32, f32,
+                                   _P, i64, _P, _P, sz, _P]
     for fn in ("jab_reference_forward", "jab_loss_forward", "jab_loss_forward_noalloc",
+               "jab_quantized_linear", "jab_rope_table", "jab_kv_write", "jab_kv_read", "jab_kv_attention",
                "jab_loss_backward_scales", "jab_loss_backward_weights", "jab_allocate_bits",
                "jab_prepare_x", "jab_loss_backward_scales_prepared", "jab_flip_rate",
                "jab_loss_backward_scales_kl",
@@ -369,6 +391,154 @@ def jab_init_scales(desc, bits, mode, W, scales, stream=None):
                                _ptr(W, torch.bfloat16, "W"), _ptr(scales, torch.float32, "scales"),
                                _stream(stream))
     _check(st, "jab_init_scales")
+
+
+# ---------------------------------------------------------------- serving a fitted block
+_DTYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
+
+
+def _dtype(t: torch.Tensor, name: str) -> int:
+    if t.dtype not in _DTYPES:
+        raise ValueError(f"{name} must be float16, bfloat16 or float32, got {t.dtype}")
+    return _DTYPES[t.dtype]
+
+
+def _rows(t: torch.Tensor, width: int, name: str, rows: Optional[int] = None):
+    """(pointer, row pitch) of a CUDA tensor of rows of `width` contiguous elements: the first dimension
+    may have any stride, the others are flattened."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.dim() < 2 or t.shape[1:].numel() != width or (t.shape[0] > 0 and not t[0].is_contiguous()):
+        raise ValueError(f"{name} must have rows of {width} contiguous elements")
+    if rows is not None and t.shape[0] != rows:
+        raise ValueError(f"{name} must have {rows} rows")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else width
+
+
+def _shaped(t: torch.Tensor, shape, dtype, name: str) -> int:
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    return _ptr(t, dtype, name)
+
+
+class KvCache:
+    """A paged cache of quantised keys and values (jab_kv_cache): caller-owned tensors k_codes, v_codes
+    (uint8 [n_pages, n_kv_heads, page_tokens, head_dim * bits / 8]) and k_scales, v_scales (float32
+    [n_pages, n_kv_heads, page_tokens]), allocated here unless given."""
+
+    def __init__(self, n_kv_heads: int, head_dim: int, bits: int, page_tokens: int, n_pages: int, device=None,
+                 k_codes=None, v_codes=None, k_scales=None, v_scales=None):
+        if bits not in (4, 8):
+            raise ValueError("bits must be 4 or 8")
+        device = device or torch.device("cuda", torch.cuda.current_device())
+        lead = (n_pages, n_kv_heads, page_tokens)
+        codes = lead + (head_dim * bits // 8,)
+
+        def have(t, shape, dtype, name):
+            t = torch.zeros(shape, dtype=dtype, device=device) if t is None else t
+            _shaped(t, shape, dtype, name)
+            return t
+
+        self.n_kv_heads, self.head_dim, self.bits = int(n_kv_heads), int(head_dim), int(bits)
+        self.page_tokens, self.n_pages = int(page_tokens), int(n_pages)
+        self.k_codes = have(k_codes, codes, torch.uint8, "k_codes")
+        self.v_codes = have(v_codes, codes, torch.uint8, "v_codes")
+        self.k_scales = have(k_scales, lead, torch.float32, "k_scales")
+        self.v_scales = have(v_scales, lead, torch.float32, "v_scales")
+        self.desc = _KvCacheDesc(self.n_kv_heads, self.head_dim, self.bits, self.page_tokens, self.n_pages,
+                                 self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.k_scales.data_ptr(),
+                                 self.v_scales.data_ptr())
+
+
+def jab_quantized_linear_workspace_size(M: int, N: int, K: int) -> int:
+    return int(lib().jab_quantized_linear_workspace_size(M, N, K))
+
+
+def jab_quantized_linear(x, codes, w_scales, y, ws, stream=None):
+    """y[m, n] = s_m w_scales[n] sum_k q(x)[m, k] codes[n, k]: x fp16 / bf16 [M, K] quantised to 8 bits per row,
+    codes int8 [N, K], the sum exact. y fp16 / bf16 / fp32 [M, N]; ws uint8, jab_quantized_linear_workspace_size
+    bytes. Rows of x and y may have a pitch."""
+    (M, K), N = x.shape, codes.shape[0]
+    xp, ldx = _rows(x, K, "x")
+    yp, ldy = _rows(y, N, "y", M)
+    st = lib().jab_quantized_linear(M, N, K, xp, _dtype(x, "x"), ldx, _shaped(codes, (N, K), torch.int8, "codes"),
+                                    _shaped(w_scales, (N,), torch.float32, "w_scales"), yp, _dtype(y, "y"), ldy,
+                                    _ptr(ws, torch.uint8, "ws"), ws.numel(), _stream(stream))
+    _check(st, "jab_quantized_linear")
+
+
+def jab_rope_table(cos, sin, theta: float, stream=None):
+    """cos and sin of position * theta^(-2j / head_dim) into fp32 [length, head_dim / 2] each."""
+    st = lib().jab_rope_table(cos.shape[0], 2 * cos.shape[1], float(theta), _ptr(cos, torch.float32, "cos"),
+                              _shaped(sin, cos.shape, torch.float32, "sin"), _stream(stream))
+    _check(st, "jab_rope_table")
+
+
+def jab_kv_write(cache: KvCache, qkv, n_q_heads: int, slots, q_out=None, positions=None, rope=None, stream=None):
+    """Rows [Q | K | V] (fp16 / bf16 / fp32 [n_tokens, (n_q_heads + 2 n_kv_heads) * head_dim]): Q and K rotated at
+    `positions` (int32 [n_tokens]) by the table rope = (cos, sin), as they are without a table, K and V quantised into the slots (int64
+    [n_tokens]; < 0: padding), the rotated Q into q_out [n_tokens, n_q_heads * head_dim]."""
+    n, dh = qkv.shape[0], cache.head_dim
+    xp, ldx = _rows(qkv, (n_q_heads + 2 * cache.n_kv_heads) * dh, "qkv")
+    if rope is not None and positions is None:
+        raise ValueError("rope needs positions")
+    cos = sin = pos = None
+    length = 0
+    if rope is not None:
+        length = rope[0].shape[0]
+        cos, sin = (_shaped(t, (length, dh // 2), torch.float32, "rope") for t in rope)
+        pos = _shaped(positions, (n,), torch.int32, "positions")
+    if q_out is not None:
+        if q_out.dtype != qkv.dtype or q_out.numel() != n * n_q_heads * dh:
+            raise ValueError("q_out must be [n_tokens, n_q_heads * head_dim] in qkv's type")
+        q_out = _ptr(q_out, None, "q_out")
+    st = lib().jab_kv_write(ctypes.byref(cache.desc), n, int(n_q_heads), xp, _dtype(qkv, "qkv"), ldx,
+                            _shaped(slots, (n,), torch.int64, "slots"), pos, cos, sin, length, q_out,
+                            _stream(stream))
+    _check(st, "jab_kv_write")
+
+
+def jab_kv_read(cache: KvCache, pages, counts, k, v, starts=None, stream=None):
+    """Cached tokens starts[b] .. starts[b] + counts[b] - 1 of every sequence as numbers, into k and v (fp16 /
+    bf16 / fp32 [n_seqs, T, n_kv_heads, head_dim]; 0 from counts[b] on). pages int32 [n_seqs, max_pages]."""
+    B, T = k.shape[0], k.shape[1]
+    shape = (B, T, cache.n_kv_heads, cache.head_dim)
+    st = lib().jab_kv_read(ctypes.byref(cache.desc), B, _shaped(pages, (B, pages.shape[1]), torch.int32, "pages"),
+                           pages.shape[1], None if starts is None else _shaped(starts, (B,), torch.int32, "starts"),
+                           _shaped(counts, (B,), torch.int32, "counts"), T, _shaped(k, shape, k.dtype, "k"),
+                           _shaped(v, shape, k.dtype, "v"), _dtype(k, "k"), _stream(stream))
+    _check(st, "jab_kv_read")
+
+
+def jab_kv_attention_workspace_size(cache: KvCache, n_seqs: int, n_tokens: int, n_q_heads: int, max_q_len: int,
+                                    max_seq_len: int, shared_len: int = 0) -> int:
+    return int(lib().jab_kv_attention_workspace_size(ctypes.byref(cache.desc), n_seqs, n_tokens, n_q_heads,
+                                                     max_q_len, max_seq_len, shared_len))
+
+
+def jab_kv_attention(cache: KvCache, q, q_start, pages, seq_lens, out, ws, max_q_len: int, max_seq_len: int,
+                     shared_len: int = 0, window: int = 0, softmax_scale: float = 0.0, lse=None, stream=None):
+    """Attention of the query rows q_start[b] .. q_start[b + 1] - 1 of q (fp16 / bf16 [n_tokens, n_q_heads,
+    head_dim]) over the seq_lens[b] cached tokens of their sequence, the last of which are the queries' own:
+    causal, within `window` keys if window > 0, the first shared_len keys read once for all sequences. out like
+    q, lse fp32 [n_tokens, n_q_heads]; ws uint8, jab_kv_attention_workspace_size bytes."""
+    n, B = q.shape[0], seq_lens.shape[0]
+    dh = cache.head_dim
+    hq = q[0].numel() // dh if n else 0
+    if n == 0:
+        return
+    qp, ldq = _rows(q, hq * dh, "q")
+    op, ldo = _rows(out, hq * dh, "out", n)
+    if out.dtype != q.dtype:
+        raise ValueError("out must have q's type")
+    st = lib().jab_kv_attention(
+        ctypes.byref(cache.desc), B, n, hq, qp, _dtype(q, "q"), ldq, _shaped(q_start, (B + 1,), torch.int32, "q_start"),
+        _shaped(pages, (B, pages.shape[1]), torch.int32, "pages"), pages.shape[1],
+        _shaped(seq_lens, (B,), torch.int32, "seq_lens"), int(max_q_len), int(max_seq_len), int(shared_len),
+        int(window), float(softmax_scale), op, ldo,
+        None if lse is None else _shaped(lse, (n, hq), torch.float32, "lse"), _ptr(ws, torch.uint8, "ws"), ws.numel(),
+        _stream(stream))
+    _check(st, "jab_kv_attention")
 
 
 def jab_selftest_wait_timeout(stream=None):
