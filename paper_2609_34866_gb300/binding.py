@@ -163,8 +163,8 @@ def _ptr(t: Optional[torch.Tensor], dtype=None, name="tensor") -> Optional[int]:
 
 
 def _stream(stream) -> Optional[int]:
-    if stream is None:
-        stream = torch.cuda.current_stream()
+    if stream is None:  # (the stream's handle alone: building torch's stream object takes longer than a launch)
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -408,15 +408,21 @@ def _rows(t: torch.Tensor, width: int, name: str, rows: Optional[int] = None):
     may have any stride, the others are flattened."""
     if not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor")
-    if t.dim() < 2 or t.shape[1:].numel() != width or (t.shape[0] > 0 and not t[0].is_contiguous()):
+    shape, strides, have = t.shape, t.stride(), 1
+    for d in range(len(shape) - 1, 0, -1):
+        if shape[d] != 1 and strides[d] != have:
+            have = -1
+            break
+        have *= shape[d]
+    if len(shape) < 2 or have != width:
         raise ValueError(f"{name} must have rows of {width} contiguous elements")
-    if rows is not None and t.shape[0] != rows:
+    if rows is not None and shape[0] != rows:
         raise ValueError(f"{name} must have {rows} rows")
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else width
+    return t.data_ptr(), strides[0] if shape[0] > 1 else width
 
 
 def _shaped(t: torch.Tensor, shape, dtype, name: str) -> int:
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
     return _ptr(t, dtype, name)
 
@@ -448,6 +454,7 @@ class KvCache:
         self.desc = _KvCacheDesc(self.n_kv_heads, self.head_dim, self.bits, self.page_tokens, self.n_pages,
                                  self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.k_scales.data_ptr(),
                                  self.v_scales.data_ptr())
+        self.ref = ctypes.byref(self.desc)
 
 
 def jab_quantized_linear_workspace_size(M: int, N: int, K: int) -> int:
@@ -489,10 +496,10 @@ def jab_kv_write(cache: KvCache, qkv, n_q_heads: int, slots, q_out=None, positio
         cos, sin = (_shaped(t, (length, dh // 2), torch.float32, "rope") for t in rope)
         pos = _shaped(positions, (n,), torch.int32, "positions")
     if q_out is not None:
-        if q_out.dtype != qkv.dtype or q_out.numel() != n * n_q_heads * dh:
+        if q_out.numel() != n * n_q_heads * dh:
             raise ValueError("q_out must be [n_tokens, n_q_heads * head_dim] in qkv's type")
-        q_out = _ptr(q_out, None, "q_out")
-    st = lib().jab_kv_write(ctypes.byref(cache.desc), n, int(n_q_heads), xp, _dtype(qkv, "qkv"), ldx,
+        q_out = _ptr(q_out, qkv.dtype, "q_out")
+    st = lib().jab_kv_write(cache.ref, n, int(n_q_heads), xp, _dtype(qkv, "qkv"), ldx,
                             _shaped(slots, (n,), torch.int64, "slots"), pos, cos, sin, length, q_out,
                             _stream(stream))
     _check(st, "jab_kv_write")
@@ -503,7 +510,7 @@ def jab_kv_read(cache: KvCache, pages, counts, k, v, starts=None, stream=None):
     bf16 / fp32 [n_seqs, T, n_kv_heads, head_dim]; 0 from counts[b] on). pages int32 [n_seqs, max_pages]."""
     B, T = k.shape[0], k.shape[1]
     shape = (B, T, cache.n_kv_heads, cache.head_dim)
-    st = lib().jab_kv_read(ctypes.byref(cache.desc), B, _shaped(pages, (B, pages.shape[1]), torch.int32, "pages"),
+    st = lib().jab_kv_read(cache.ref, B, _shaped(pages, (B, pages.shape[1]), torch.int32, "pages"),
                            pages.shape[1], None if starts is None else _shaped(starts, (B,), torch.int32, "starts"),
                            _shaped(counts, (B,), torch.int32, "counts"), T, _shaped(k, shape, k.dtype, "k"),
                            _shaped(v, shape, k.dtype, "v"), _dtype(k, "k"), _stream(stream))
@@ -512,7 +519,7 @@ def jab_kv_read(cache: KvCache, pages, counts, k, v, starts=None, stream=None):
 
 def jab_kv_attention_workspace_size(cache: KvCache, n_seqs: int, n_tokens: int, n_q_heads: int, max_q_len: int,
                                     max_seq_len: int, shared_len: int = 0) -> int:
-    return int(lib().jab_kv_attention_workspace_size(ctypes.byref(cache.desc), n_seqs, n_tokens, n_q_heads,
+    return int(lib().jab_kv_attention_workspace_size(cache.ref, n_seqs, n_tokens, n_q_heads,
                                                      max_q_len, max_seq_len, shared_len))
 
 
@@ -524,15 +531,15 @@ def jab_kv_attention(cache: KvCache, q, q_start, pages, seq_lens, out, ws, max_q
     q, lse fp32 [n_tokens, n_q_heads]; ws uint8, jab_kv_attention_workspace_size bytes."""
     n, B = q.shape[0], seq_lens.shape[0]
     dh = cache.head_dim
-    hq = q[0].numel() // dh if n else 0
     if n == 0:
         return
+    hq = q.numel() // (n * dh)
     qp, ldq = _rows(q, hq * dh, "q")
     op, ldo = _rows(out, hq * dh, "out", n)
     if out.dtype != q.dtype:
         raise ValueError("out must have q's type")
     st = lib().jab_kv_attention(
-        ctypes.byref(cache.desc), B, n, hq, qp, _dtype(q, "q"), ldq, _shaped(q_start, (B + 1,), torch.int32, "q_start"),
+        cache.ref, B, n, hq, qp, _dtype(q, "q"), ldq, _shaped(q_start, (B + 1,), torch.int32, "q_start"),
         _shaped(pages, (B, pages.shape[1]), torch.int32, "pages"), pages.shape[1],
         _shaped(seq_lens, (B,), torch.int32, "seq_lens"), int(max_q_len), int(max_seq_len), int(shared_len),
         int(window), float(softmax_scale), op, ldo,

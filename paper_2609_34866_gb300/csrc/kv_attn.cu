@@ -24,181 +24,14 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "common.cuh"
-#include "serve.h"
+#include "kv_attn.cuh"
 #include "tc.cuh"
 
 namespace jab {
+namespace kv {
 namespace {
 
 constexpr int W = 4;  // warps of a block
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-
-struct AttnParams {
-  const uint8_t *k_codes, *v_codes;
-  const float *k_scales, *v_scales;
-  int n_kv, G, n_pages, max_pages, page;
-  FastDiv by_page, by_g;
-  const void* q;
-  int64_t ldq;
-  const int32_t *q_start, *pages, *lens;
-  int n_seqs, n_tokens, shared, window;
-  float scale_log2;
-  void* out;
-  int64_t ldo;
-  float* lse;
-  int n_slots;
-  int32_t* plan;     // [0..7] scalars, then cum_t [E + 1], cum_i [E + 1]
-  float2* part_ml;   // [n_slots, R]: maximum, sum
-  float* part_o;     // [n_slots, R, DH]
-  int* status;
-};
-
-enum { kTotal = 0, kItems = 1, kPer = 2, kLo = 3, kHi = 4, kPlanHead = 8 };
-
-// A stretch of the list: the queries of a sequence and the keys that are its own, or (shared) all queries
-// and the shared keys.
-struct Entry {
-  int tok0, nq, len, kbeg;
-  bool all;
-};
-
-__device__ __forceinline__ Entry entry_of(const AttnParams& p, int e) {
-  Entry en;
-  en.all = false;
-  if (p.shared > 0 && e-- == 0) {
-    en.all = true;
-    en.tok0 = 0, en.nq = p.n_tokens, en.len = p.shared, en.kbeg = 0;
-    return en;
-  }
-  const int a = __ldg(p.q_start + e), b = __ldg(p.q_start + e + 1);
-  en.tok0 = min(max(a, 0), p.n_tokens);
-  en.nq = min(max(b, en.tok0), p.n_tokens) - en.tok0;
-  const int64_t room = min((int64_t)p.max_pages * p.page, (int64_t)INT32_MAX);
-  const int len = __ldg(p.lens + e);
-  en.len = (int)min((int64_t)max(len, 0), room);
-  en.kbeg = p.shared;
-  if (a != en.tok0 || b != en.tok0 + en.nq || len != en.len) report(p.status, JAB_ERR_INVALID_ARG);
-  return en;
-}
-
-// First key tile and number of key tiles of row tile rt (at least one: an item that sees nothing still has
-// its zeros to write).
-__device__ __forceinline__ void key_tiles(const AttnParams& p, const Entry& en, int rt, int R, int plo, int phi, int& t0, int& n) {
-  int lo, hi;
-  if (en.all) {
-    lo = plo, hi = phi;
-  } else {
-    const int i0 = p.by_g.quot(rt * R), i1 = p.by_g.quot(min((rt + 1) * R, en.nq * p.G) - 1);
-    const int first = en.len - en.nq + 1;
-    hi = first + i1;
-    lo = max(p.window > 0 ? first + i0 - p.window : 0, en.kbeg);
-  }
-  t0 = max(lo, 0) / 16;
-  n = hi > lo ? max((hi + 15) / 16 - t0, 1) : 1;
-}
-
-// The plan, by every block for itself: cum_t[e], cum_i[e] = key tiles and items of a KV head before entry e.
-template <int R>
-__device__ void make_plan(const AttnParams& p, int E, int* cum_t, int* cum_i, int* head) {
-  __shared__ int w_t[W], w_i[W], w_lo[W], w_hi[W];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int first = p.shared > 0 ? 1 : 0;
-  if (first) {  // what any query sees of the shared keys
-    int lo = p.shared, hi = 0;
-    for (int b = tid; b < p.n_seqs; b += 32 * W) {
-      const Entry en = entry_of(p, b + 1);
-      if (en.nq > 0) {
-        lo = min(lo, p.window > 0 ? max(en.len - en.nq + 1 - p.window, 0) : 0);
-        hi = max(hi, min(en.len, p.shared));
-      }
-    }
-    lo = __reduce_min_sync(0xffffffffu, lo);
-    hi = __reduce_max_sync(0xffffffffu, hi);
-    if (lane == 0) w_lo[warp] = lo, w_hi[warp] = hi;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < W; ++w) lo = min(lo, w_lo[w]), hi = max(hi, w_hi[w]);
-    if (tid == 0) head[kLo] = lo, head[kHi] = hi;
-    __syncthreads();
-  } else if (tid == 0) {
-    head[kLo] = head[kHi] = 0;
-  }
-  const int run = (E + 32 * W - 1) / (32 * W);
-  const int e0 = min(tid * run, E), e1 = min(e0 + run, E);
-  int st = 0, si = 0;
-  for (int pass = 0; pass < 2; ++pass) {
-    int at = 0, ai = 0;
-    if (pass == 1) {  // exclusive prefix over the threads
-      int t = st, i = si;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int ut = __shfl_up_sync(0xffffffffu, t, o), ui = __shfl_up_sync(0xffffffffu, i, o);
-        if (lane >= o) t += ut, i += ui;
-      }
-      if (lane == 31) w_t[warp] = t, w_i[warp] = i;
-      __syncthreads();
-      at = t - st, ai = i - si;
-      for (int w = 0; w < warp; ++w) at += w_t[w], ai += w_i[w];
-    }
-    for (int e = e0; e < e1; ++e) {
-      const Entry en = entry_of(p, e);
-      const int nrt = (en.nq * p.G + R - 1) / R;
-      if (pass == 1) cum_t[e] = at, cum_i[e] = ai;
-      int sum = 0;
-      if (en.all) {
-        int t0, n;
-        key_tiles(p, en, 0, R, head[kLo], head[kHi], t0, n);
-        sum = n * nrt;
-      } else {
-        for (int rt = 0; rt < nrt; ++rt) {
-          int t0, n;
-          key_tiles(p, en, rt, R, 0, 0, t0, n);
-          sum += n;
-        }
-      }
-      at += sum, ai += nrt;
-    }
-    if (pass == 0) st = at, si = ai;
-  }
-  if (tid == 32 * W - 1) {
-    int t = 0, i = 0;
-    for (int w = 0; w < W; ++w) t += w_t[w], i += w_i[w];
-    cum_t[E] = t, cum_i[E] = i;
-    head[kTotal] = t, head[kItems] = i;
-    const int64_t all = (int64_t)t * p.n_kv;
-    const int64_t per = (all + gridDim.x - 1) / gridDim.x;
-    head[kPer] = (int)min(((per + W - 1) / W) * W, (int64_t)INT32_MAX);  // (E = 0: 0)
-  }
-  __syncthreads();
-  if (blockIdx.x == 0) {
-    for (int i = tid; i < kPlanHead; i += 32 * W) p.plan[i] = head[i];
-    for (int i = tid; i <= E; i += 32 * W) p.plan[kPlanHead + i] = cum_t[i], p.plan[kPlanHead + E + 1 + i] = cum_i[i];
-  }
-}
-
-// Last e with cum[e] <= y (cum[0] = 0 <= y < cum[E]).
-__device__ __forceinline__ int find(const int* cum, int E, int y) {
-  int lo = 0, hi = E;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (cum[mid] <= y) lo = mid;
-    else hi = mid;
-  }
-  return lo;
-}
-
-// Position of a token in its sequence.
-__device__ __forceinline__ int position_of(const AttnParams& p, int token) {
-  int lo = 0, hi = p.n_seqs;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (__ldg(p.q_start + mid) <= token) lo = mid;
-    else hi = mid;
-  }
-  const Entry en = entry_of(p, lo + (p.shared > 0 ? 1 : 0));
-  return en.len - en.nq + token - en.tok0;
-}
 
 // ------------------------------------------------------------------ codes to fp16
 // A byte b under the exponent of 1024 is 1024 + b; less 1152 it is b - 128.
@@ -302,10 +135,8 @@ __device__ __forceinline__ float load_q(const T* row, bool live, uint32_t (&b)[D
     for (int i = 0; i < DH / 4; ++i) big = max(big, __float_as_uint(f[i]) & 0x7fffffffu);
     big = max(big, __shfl_xor_sync(0xffffffffu, big, 1));
     big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
-    // its largest to [8, 16); both powers of two are normal numbers for e in 4 .. 253
-    const int e = min(max((int)(big >> 23), 4), 253);
-    const float by = __uint_as_float((uint32_t)(257 - e) << 23);  // 2^(130 - e)
-    back = __uint_as_float((uint32_t)(e - 3) << 23);              // 2^(e - 130)
+    float by;
+    row_power(big, by, back);
 #pragma unroll
     for (int i = 0; i < DH / 4; ++i) f[i] *= by;
   }
@@ -318,71 +149,39 @@ __device__ __forceinline__ float load_q(const T* row, bool live, uint32_t (&b)[D
   return back;
 }
 
-template <class T>
-__device__ __forceinline__ void store_out(T* p, float v);
-template <>
-__device__ __forceinline__ void store_out<half_t>(half_t* p, float v) { *p = __float2half_rn(v); }
-template <>
-__device__ __forceinline__ void store_out<bf16_t>(bf16_t* p, float v) { *p = __float2bfloat16_rn(v); }
-
-// 2^(a - b) with 2^(-inf - -inf) = 0.
-__device__ __forceinline__ float shift2(float a, float b) { return a == -INFINITY ? 0.f : exp2f(a - b); }
-
 template <class T, int DH, int BITS, int NT>
 __global__ void __launch_bounds__(32 * W) kv_attn_kernel(const __grid_constant__ AttnParams p) {
   constexpr int R = 8 * NT, MT = DH / 16, KS = DH / 16, PITCH = DH + 4;
   using TT = Tile<DH, BITS>;
   extern __shared__ __align__(16) uint8_t dyn[];
   __shared__ int head[kPlanHead];
-  __shared__ int row_lo[R], row_hi[R], bounds[2];
+  __shared__ int row_lo[R], row_hi[R];
   __shared__ float2 sm_ml[W][R];
   float* sm_o = reinterpret_cast<float*>(dyn);               // [W][R][PITCH]
-  const int E = p.n_seqs + (p.shared > 0 ? 1 : 0);
+  const int E = entries(p);
   int* cum_t = reinterpret_cast<int*>(dyn + W * R * PITCH * 4);
   int* cum_i = cum_t + E + 1;
   stream_order();
-  make_plan<R>(p, E, cum_t, cum_i, head);
+  make_plan<R, 16, W, W>(p, cum_t, cum_i, head);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, q4 = lane & 3;
-  const int total = head[kTotal], per = head[kPer], plo = head[kLo], phi = head[kHi];
-  const int64_t all = (int64_t)total * p.n_kv;
-  const int64_t x1 = min(all, ((int64_t)blockIdx.x + 1) * per);
-  for (int64_t x = (int64_t)blockIdx.x * per; x < x1;) {
-    // the item that tile x is in: KV head h, entry e, row tile rt, its tiles [base, base + n) of the head's
-    const int h = (int)(x / total), y = (int)(x - (int64_t)h * total);
-    const int e = find(cum_t, E, y);
-    const Entry en = entry_of(p, e);
-    int rt = 0, base = cum_t[e], t0, n;
-    key_tiles(p, en, 0, R, plo, phi, t0, n);
-    if (en.all) {
-      rt = (y - base) / n;
-      base += rt * n;
-    } else {
-      while (y >= base + n) {
-        base += n;
-        key_tiles(p, en, ++rt, R, 0, 0, t0, n);
-      }
-    }
-    const int s0 = y - base, s1 = (int)min((int64_t)n, s0 + (x1 - x));  // this block's part of the item
-    const int rows = min(R, en.nq * p.G - rt * R);
-    // what the rows see; rows past the end see all, of a Q of zeros
+  const int64_t all = (int64_t)head[kTotal] * p.n_kv;
+  const int64_t x0 = (int64_t)blockIdx.x * head[kPer], x1 = min(all, x0 + head[kPer]);
+  for (int64_t x = x0; x < x1;) {
+    const Item it = item_at<R, 16>(p, cum_t, head, x, x1);
+    const Entry& en = it.en;
+    const int h = it.h, rt = it.rt, t0 = it.t0, s0 = it.s0, s1 = it.s1, rows = it.rows;
     __syncthreads();
+    // what the rows see; rows past the end see all, of a Q of zeros
     if (tid < R) {
       int lo = 0, hi = INT32_MAX;
       if (tid < rows) {
         const int token = en.tok0 + p.by_g.quot(rt * R + tid);
-        const int pos = en.all ? position_of(p, token) : en.len - en.nq + token - en.tok0;
-        lo = max(en.kbeg, p.window > 0 ? pos + 1 - p.window : 0);
-        hi = min(pos + 1, en.len);
+        seen_by_row(p, en, en.all ? position_of(p, token) : en.len - en.nq + token - en.tok0, lo, hi);
       }
       row_lo[tid] = lo, row_hi[tid] = hi;
     }
-    __syncthreads();
-    if (warp == 0) {
-      int lo = 0, hi = INT32_MAX;
-      for (int r = lane; r < rows; r += 32) lo = max(lo, row_lo[r]), hi = min(hi, row_hi[r]);
-      lo = __reduce_max_sync(0xffffffffu, lo), hi = __reduce_min_sync(0xffffffffu, hi);
-      if (lane == 0) bounds[0] = lo, bounds[1] = hi;
-    }
+    int all_lo, all_hi;
+    seen_by_all(p, en, rt * R, rt * R + rows, head, all_lo, all_hi);
     // Q
     uint32_t qf[NT][DH / 8];
     float fac[NT][2];
@@ -395,18 +194,17 @@ __global__ void __launch_bounds__(32 * W) kv_attn_kernel(const __grid_constant__
       fac[j][1] = __shfl_sync(0xffffffffu, back, 8 * q4 + 4);
     }
     __syncthreads();
-    const int all_lo = bounds[0], all_hi = bounds[1];
 
-    const int32_t* table = p.pages + (en.all ? 0 : (int64_t)(e - (p.shared > 0 ? 1 : 0)) * p.max_pages);
+    const int32_t* table = p.pages + (en.all ? 0 : (int64_t)(it.e - (p.list.all ? 1 : 0)) * p.max_pages);
     auto first_row = [&](int t) -> int64_t {  // row of the cache of the first key of tile t
-      const int key = (t0 + t) * 16, pg = min(p.by_page.quot(key), p.max_pages - 1);
+      const int key = (t0 + t) * 16, pg = p.by_page.quot(key);
+      if (key >= en.len) return (int64_t)h * p.page;  // a tile with nothing to see: any page, not the table's entry
       int id = __ldg(table + pg);
       if (id < 0 || id >= p.n_pages) {
         report(p.status, JAB_ERR_INVALID_ARG);
         id = 0;
       }
-      const int in = key - pg * p.page;
-      return ((int64_t)id * p.n_kv + h) * p.page + (in < p.page ? in : 0);
+      return ((int64_t)id * p.n_kv + h) * p.page + (key - pg * p.page);
     };
 
     float o[NT][MT][4] = {}, m[NT][2], l[NT][2];
@@ -557,11 +355,9 @@ __global__ void __launch_bounds__(32 * W) kv_attn_kernel(const __grid_constant__
         for (int i = 0; i < MT; ++i) *reinterpret_cast<float2*>(at + 2 * i) = make_float2(o[j][i][c], o[j][i][c + 2]);
       }
     __syncthreads();
-    const bool whole = s0 == 0 && s1 == n && p.shared == 0;
-    const int item = h * head[kItems] + cum_i[e] + rt;
-    const bool first = x == (int64_t)blockIdx.x * per;
-    const int64_t slot = p.shared > 0 ? (int64_t)blockIdx.x + item : 2 * (int64_t)blockIdx.x + (first ? 0 : 1);
-    if (!whole && slot >= p.n_slots) report(p.status, JAB_ERR_INVALID_ARG);
+    const bool whole = s0 == 0 && s1 == it.n && p.shared == 0;
+    const int64_t slot = slot_of(p, blockIdx.x, h * head[kItems] + cum_i[it.e] + rt, x == x0);
+    if (!whole && slot >= p.list.n_slots) report(p.status, JAB_ERR_INVALID_ARG);
     for (int r = warp; r < rows; r += W) {
       float mx = -INFINITY;
 #pragma unroll
@@ -583,12 +379,12 @@ __global__ void __launch_bounds__(32 * W) kv_attn_kernel(const __grid_constant__
         for (int w = 0; w < W; ++w) v += f[w] * sm_o[(w * R + r) * PITCH + d];
         if (whole)
           store_out(static_cast<T*>(p.out) + token * p.ldo + (int64_t)qh * DH + d, v * inv);
-        else if (slot < p.n_slots)
-          p.part_o[(slot * R + r) * DH + d] = v;
+        else if (slot < p.list.n_slots)
+          p.list.part_o[(slot * R + r) * DH + d] = v;
       }
       if (lane == 0) {
         if (!whole) {
-          if (slot < p.n_slots) p.part_ml[slot * R + r] = make_float2(mx, lsum);
+          if (slot < p.list.n_slots) p.list.part_ml[slot * R + r] = make_float2(mx, lsum);
         } else if (p.lse != nullptr) {
           p.lse[token * ((int64_t)p.n_kv * p.G) + qh] = lsum == 0.f ? -INFINITY : (mx + log2f(lsum)) * kLn2;
         }
@@ -598,62 +394,65 @@ __global__ void __launch_bounds__(32 * W) kv_attn_kernel(const __grid_constant__
   }
 }
 
-// Joins the parts of every (token, query head) whose keys went to several blocks or entries, in the list's
-// order; one warp each.
+// Adds to (mx, l, o) the parts that a list's blocks left of one (token, query head) in entry e. False: none, or the
+// output is written already. A lane holds dimensions lane, lane + 32, ...
+template <int DH, int R, int KT>
+__device__ __forceinline__ bool join(AttnParams p, const List& list, int e, int token, int h, int gi, int lane, float& mx, float& l,
+                                     float (&o)[DH / 32]) {
+  p.list = list;
+  const int E = entries(p);
+  const int* head = list.plan;
+  const int* cum_t = list.plan + kPlanHead;
+  const int* cum_i = cum_t + E + 1;
+  const Entry en = entry_of(p, e);
+  if (token < en.tok0 || token >= en.tok0 + en.nq) return false;
+  const int rr = (token - en.tok0) * p.G + gi, want = rr / R, r = rr - want * R;
+  int base = cum_t[e], t0, n;
+  if (en.all) {
+    key_tiles<R, KT>(p, en, 0, head, t0, n);
+    base += want * n;
+  } else {
+    for (int rt = 0;; ++rt) {
+      key_tiles<R, KT>(p, en, rt, head, t0, n);
+      if (rt == want) break;
+      base += n;
+    }
+  }
+  const int per = head[kPer];
+  const int64_t y0 = (int64_t)h * head[kTotal] + base, y1 = y0 + n;
+  const int c0 = (int)(y0 / per), c1 = (int)((y1 - 1) / per);
+  if (c0 == c1 && p.shared == 0) return false;  // written by its block
+  const int item = h * head[kItems] + cum_i[e] + want;
+  for (int c = c0; c <= c1; ++c) {
+    const int64_t slot = slot_of(p, c, item, (int64_t)c * per >= y0);
+    if (slot >= list.n_slots) continue;
+    const float2 ml = list.part_ml[slot * R + r];
+    const float mn = fmaxf(mx, ml.x), fa = shift2(mx, mn), fb = shift2(ml.x, mn);
+    mx = mn;
+    l = l * fa + ml.y * fb;
+#pragma unroll
+    for (int i = 0; i < DH / 32; ++i) o[i] = o[i] * fa + fb * list.part_o[(slot * R + r) * DH + lane + 32 * i];
+  }
+  return true;
+}
+
+// Joins the parts of every (token, query head) whose keys went to several blocks or entries, in the lists' order; one
+// warp each. by_keys: the list of kv_attn_kernel; by_tiles: of the tile kernel.
 template <class T, int DH, int R>
-__global__ void __launch_bounds__(128) kv_merge_kernel(const __grid_constant__ AttnParams p) {
+__global__ void __launch_bounds__(128) kv_merge_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ List by_keys,
+                                                       const __grid_constant__ List by_tiles) {
   stream_order();
-  const int lane = threadIdx.x & 31;
-  const int Hq = p.n_kv * p.G;
+  const int lane = threadIdx.x & 31, Hq = p.n_kv * p.G;
   const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
   if (unit >= (int64_t)p.n_tokens * Hq) return;
-  const int token = (int)(unit / Hq), qh = (int)(unit - (int64_t)token * Hq);
-  const int h = qh / p.G, gi = qh - h * p.G;
-  const int first = p.shared > 0 ? 1 : 0, E = p.n_seqs + first;
-  const int* cum_t = p.plan + kPlanHead;
-  const int* cum_i = cum_t + E + 1;
-  const int total = p.plan[kTotal], items = p.plan[kItems], per = p.plan[kPer], plo = p.plan[kLo], phi = p.plan[kHi];
-  int lo = 0, hi = p.n_seqs;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (__ldg(p.q_start + mid) <= token) lo = mid;
-    else hi = mid;
-  }
-  const int e_seq = lo + first;
+  const int token = (int)(unit / Hq), qh = (int)(unit - (int64_t)token * Hq), h = qh / p.G, gi = qh - h * p.G;
+  const int b = sequence_of(p, token);
   float mx = -INFINITY, l = 0.f, o[DH / 32] = {};
   bool any = false;
-  for (int k = first ? 0 : 1; k < 2; ++k) {
-    const int e = k == 0 ? 0 : e_seq;
-    const Entry en = entry_of(p, e);
-    if (token < en.tok0 || token >= en.tok0 + en.nq) continue;
-    const int rr = (token - en.tok0) * p.G + gi, want = rr / R, r = rr - want * R;
-    int base = cum_t[e], t0, n;
-    if (en.all) {
-      key_tiles(p, en, 0, R, plo, phi, t0, n);
-      base += want * n;
-    } else {
-      for (int rt = 0;; ++rt) {
-        key_tiles(p, en, rt, R, 0, 0, t0, n);
-        if (rt == want) break;
-        base += n;
-      }
-    }
-    const int64_t y0 = (int64_t)h * total + base, y1 = y0 + n;
-    const int c0 = (int)(y0 / per), c1 = (int)((y1 - 1) / per);
-    if (c0 == c1 && !first) return;  // written by its block
-    const int item = h * items + cum_i[e] + want;
-    any = true;
-    for (int c = c0; c <= c1; ++c) {
-      const int64_t slot = first ? (int64_t)c + item : 2 * (int64_t)c + ((int64_t)c * per >= y0 ? 0 : 1);
-      if (slot >= p.n_slots) continue;
-      const float2 ml = p.part_ml[slot * R + r];
-      const float mn = fmaxf(mx, ml.x), fa = shift2(mx, mn), fb = shift2(ml.x, mn);
-      mx = mn;
-      l = l * fa + ml.y * fb;
-#pragma unroll
-      for (int i = 0; i < DH / 32; ++i) o[i] = o[i] * fa + fb * p.part_o[(slot * R + r) * DH + lane + 32 * i];
-    }
-  }
+  if (by_keys.used && by_keys.all) any |= join<DH, R, 16>(p, by_keys, 0, token, h, gi, lane, mx, l, o);
+  if (by_tiles.used && by_tiles.all) any |= join<DH, kTileRows, kTileKeys>(p, by_tiles, 0, token, h, gi, lane, mx, l, o);
+  if (by_keys.used) any |= join<DH, R, 16>(p, by_keys, b + (by_keys.all ? 1 : 0), token, h, gi, lane, mx, l, o);
+  if (by_tiles.used) any |= join<DH, kTileRows, kTileKeys>(p, by_tiles, b + (by_tiles.all ? 1 : 0), token, h, gi, lane, mx, l, o);
   if (!any) return;
   const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
@@ -663,29 +462,62 @@ __global__ void __launch_bounds__(128) kv_merge_kernel(const __grid_constant__ A
 }
 
 // ------------------------------------------------------------------ host side
-constexpr int kMaxBlocks = 1216;
+constexpr int kMaxBlocks = 1216, kMaxTileBlocks = 512;
+constexpr int kFewRows = 32;  // rows of a sequence up to which all of the work goes by 16 keys
 
-int row_tiles(int G, int max_q) { return max_q * G <= 8 ? 1 : max_q * G <= 16 ? 2 : 4; }
+int n_tiles_of_rows(int64_t rows) { return rows <= 8 ? 1 : rows <= 16 ? 2 : 4; }
 
-struct Scratch {
-  size_t plan, ml, o, total;
-  int64_t slots;
+// Which kernel takes what. Sequences of up to kFewRows (token, head) rows go by 16-key tiles: the cache's bytes bound
+// them, not the products. Longer ones fill 128-row tiles; where lengths are mixed, those of up to 8 rows still go
+// by keys, in a launch of their own.
+struct Route {
+  List keys, tiles;
+  int nt;  // 8-row blocks of the by-keys kernel
+  size_t keys_plan, keys_ml, keys_o, tiles_plan, tiles_ml, tiles_o, total;
 };
 
-Scratch plan_scratch(int n_kv, int dh, int n_seqs, int64_t n_tokens, int G, int max_q, bool shared) {
-  const int R = 8 * (shared ? 4 : row_tiles(G, max_q));
-  Scratch s;
-  s.slots = 2 * kMaxBlocks;
-  if (shared) s.slots = kMaxBlocks + (int64_t)n_kv * (2 * ((n_tokens * G + R - 1) / R) + n_seqs);
-  s.plan = 0;
-  s.ml = ((size_t)(kPlanHead + 2 * (n_seqs + 2)) * 4 + 255) / 256 * 256;
-  s.o = s.ml + ((size_t)s.slots * R * 8 + 255) / 256 * 256;
-  s.total = s.o + (size_t)s.slots * R * dh * 4;
-  return s;
+Route route(int dh, int n_kv, int n_seqs, int64_t n_tokens, int G, int max_q, bool shared) {
+  Route r{};
+  const int64_t rows = (int64_t)max_q * G, all_rows = n_tokens * G;
+  const bool tiles_own = rows > kFewRows, uniform = n_tokens == (int64_t)n_seqs * max_q;
+  const bool tiles_all = shared && all_rows > kFewRows;
+  const bool keys_own = !tiles_own || !uniform, keys_all = shared && !tiles_all;
+  r.keys.used = keys_own || keys_all;
+  r.tiles.used = tiles_own || tiles_all;
+  r.keys.all = keys_all;
+  r.tiles.all = tiles_all;
+  r.nt = !tiles_own ? n_tiles_of_rows(keys_all ? std::max(rows, all_rows) : rows) : keys_all ? 4 : 1;
+  const int split = !tiles_own ? INT32_MAX : uniform ? 0 : 8;  // rows up to which a sequence goes by keys
+  r.keys.min_rows = 1, r.keys.max_rows = keys_own ? split : 0;
+  r.tiles.min_rows = tiles_own ? split + 1 : INT32_MAX, r.tiles.max_rows = INT32_MAX;
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t o = at;
+    at = (at + bytes + 255) / 256 * 256;
+    return o;
+  };
+  auto slots = [&](int blocks, int R, bool all, bool own) {
+    if (!shared) return 2 * (int64_t)blocks;
+    return blocks + (int64_t)n_kv * ((all ? (all_rows + R - 1) / R : 0) + (own ? (all_rows + R - 1) / R + n_seqs : 0));
+  };
+  const size_t plan_bytes = (size_t)(kPlanHead + 2 * (n_seqs + 2)) * 4;
+  if (r.keys.used) {
+    const int R = 8 * r.nt;
+    const int64_t n = slots(kMaxBlocks, R, keys_all, keys_own);
+    r.keys.n_slots = (int)std::min<int64_t>(n, INT32_MAX);
+    r.keys_plan = take(plan_bytes), r.keys_ml = take((size_t)n * R * 8), r.keys_o = take((size_t)n * R * dh * 4);
+  }
+  if (r.tiles.used) {
+    const int64_t n = slots(kMaxTileBlocks, kTileRows, tiles_all, tiles_own);
+    r.tiles.n_slots = (int)std::min<int64_t>(n, INT32_MAX);
+    r.tiles_plan = take(plan_bytes), r.tiles_ml = take((size_t)n * kTileRows * 8), r.tiles_o = take((size_t)n * kTileRows * dh * 4);
+  }
+  r.total = std::max<size_t>(at, 256);
+  return r;
 }
 
 template <class T, int DH, int BITS, int NT>
-cudaError_t launch_as(const AttnParams& p, int64_t est_tiles, int sms, cudaStream_t st) {
+cudaError_t launch_keys(const AttnParams& p, int64_t est_tiles, int sms, cudaStream_t st) {
   auto kern = kv_attn_kernel<T, DH, BITS, NT>;
   constexpr int R = 8 * NT;
   const size_t most = (size_t)W * R * (DH + 4) * 4 + (size_t)2 * (4096 + 2) * 4;
@@ -695,7 +527,7 @@ cudaError_t launch_as(const AttnParams& p, int64_t est_tiles, int sms, cudaStrea
     if (e != cudaSuccess) return e;
     attr_set = true;
   }
-  const int E = p.n_seqs + (p.shared > 0 ? 1 : 0);
+  const int E = p.n_seqs + (p.list.all ? 1 : 0);
   const size_t smem = (size_t)W * R * (DH + 4) * 4 + (size_t)2 * (E + 1) * 4;
   static size_t asked = 0;
   static int occ = 0;
@@ -707,33 +539,43 @@ cudaError_t launch_as(const AttnParams& p, int64_t est_tiles, int sms, cudaStrea
     asked = smem;
   }
   const int64_t grid = std::max<int64_t>(1, std::min<int64_t>({(int64_t)sms * occ, kMaxBlocks, (est_tiles + W - 1) / W}));
-  cudaError_t e = launch_after(kern, (unsigned)grid, 32 * W, smem, st, p);
-  if (e != cudaSuccess) return e;
-  const int64_t units = (int64_t)p.n_tokens * p.n_kv * p.G;
-  return launch_after(kv_merge_kernel<T, DH, R>, (unsigned)((units + 3) / 4), 128, 0, st, p);
+  return launch_after(kern, (unsigned)grid, 32 * W, smem, st, p);
 }
 
-template <class T, int DH, int BITS>
-cudaError_t launch_nt(const AttnParams& p, int nt, int64_t est, int sms, cudaStream_t st) {
-  return nt == 1 ? launch_as<T, DH, BITS, 1>(p, est, sms, st) : nt == 2 ? launch_as<T, DH, BITS, 2>(p, est, sms, st)
-                                                                        : launch_as<T, DH, BITS, 4>(p, est, sms, st);
-}
-template <class T>
-cudaError_t launch_type(const AttnParams& p, int dh, int bits, int nt, int64_t est, int sms, cudaStream_t st) {
-  if (dh == 128)
-    return bits == 8 ? launch_nt<T, 128, 8>(p, nt, est, sms, st) : launch_nt<T, 128, 4>(p, nt, est, sms, st);
-  return bits == 8 ? launch_nt<T, 64, 8>(p, nt, est, sms, st) : launch_nt<T, 64, 4>(p, nt, est, sms, st);
+template <class T, int DH>
+cudaError_t launch_all(AttnParams p, const Route& r, int bits, jab_dtype type, int max_q, int max_len, int sms, cudaStream_t st) {
+  cudaError_t e;
+  if (r.keys.used) {
+    p.list = r.keys;
+    const int64_t est = (int64_t)p.n_kv * p.n_seqs * ((int64_t)max_len / 16 + 1) * std::max<int64_t>(1, (int64_t)max_q * p.G / (8 * r.nt));
+    if (bits == 8)
+      e = r.nt == 1 ? launch_keys<T, DH, 8, 1>(p, est, sms, st) : r.nt == 2 ? launch_keys<T, DH, 8, 2>(p, est, sms, st) : launch_keys<T, DH, 8, 4>(p, est, sms, st);
+    else
+      e = r.nt == 1 ? launch_keys<T, DH, 4, 1>(p, est, sms, st) : r.nt == 2 ? launch_keys<T, DH, 4, 2>(p, est, sms, st) : launch_keys<T, DH, 4, 4>(p, est, sms, st);
+    if (e != cudaSuccess) return e;
+  }
+  if (r.tiles.used) {
+    p.list = r.tiles;
+    const int64_t rts = ((int64_t)max_q * p.G + kTileRows - 1) / kTileRows, kts = max_len / kTileKeys + 1;
+    const int64_t est = p.n_kv * (p.n_seqs * rts * kts + (r.tiles.all ? ((int64_t)p.n_tokens * p.G / kTileRows + 1) * kts : 0));
+    if ((e = launch_tiles(p, type, DH, bits, est, std::min(sms, kMaxTileBlocks), st)) != cudaSuccess) return e;
+  }
+  const unsigned blocks = (unsigned)(((int64_t)p.n_tokens * p.n_kv * p.G + 3) / 4);
+  return r.nt == 1   ? launch_after(kv_merge_kernel<T, DH, 8>, blocks, 128, 0, st, p, r.keys, r.tiles)
+         : r.nt == 2 ? launch_after(kv_merge_kernel<T, DH, 16>, blocks, 128, 0, st, p, r.keys, r.tiles)
+                     : launch_after(kv_merge_kernel<T, DH, 32>, blocks, 128, 0, st, p, r.keys, r.tiles);
 }
 
 }  // namespace
+}  // namespace kv
 
 size_t kv_attention_scratch(int n_kv, int dh, int n_seqs, int64_t n_tokens, int n_q_heads, int max_q, int shared) {
-  return plan_scratch(n_kv, dh, n_seqs, n_tokens, n_q_heads / n_kv, max_q, shared > 0).total;
+  return kv::route(dh, n_kv, n_seqs, n_tokens, n_q_heads / n_kv, max_q, shared > 0).total;
 }
 
 cudaError_t launch_kv_attention(const KvAttnArgs& a, int sms, cudaStream_t st) {
   const jab_kv_cache& c = a.cache;
-  AttnParams p{};
+  kv::AttnParams p{};
   p.k_codes = static_cast<const uint8_t*>(c.k_codes);
   p.v_codes = static_cast<const uint8_t*>(c.v_codes);
   p.k_scales = c.k_scales;
@@ -754,22 +596,25 @@ cudaError_t launch_kv_attention(const KvAttnArgs& a, int sms, cudaStream_t st) {
   p.n_tokens = (int)a.n_tokens;
   p.shared = a.shared;
   p.window = a.window;
-  p.scale_log2 = a.scale * kLog2e;
+  p.scale_log2 = a.scale * kv::kLog2e;
   p.out = a.out;
   p.ldo = a.ldo;
   p.lse = a.lse;
   p.status = a.status;
-  const Scratch s = plan_scratch(p.n_kv, c.head_dim, p.n_seqs, p.n_tokens, p.G, a.max_q, p.shared > 0);
+  kv::Route r = kv::route(c.head_dim, p.n_kv, p.n_seqs, p.n_tokens, p.G, a.max_q, p.shared > 0);
   char* w = static_cast<char*>(a.ws);
-  p.plan = reinterpret_cast<int32_t*>(w + s.plan);
-  p.part_ml = reinterpret_cast<float2*>(w + s.ml);
-  p.part_o = reinterpret_cast<float*>(w + s.o);
-  p.n_slots = (int)s.slots;
-  const int nt = p.shared > 0 ? 4 : row_tiles(p.G, a.max_q);
-  const int64_t rts = ((int64_t)a.max_q * p.G + 8 * nt - 1) / (8 * nt);
-  const int64_t est = (int64_t)p.n_kv * p.n_seqs * rts * (a.max_len / 16 + 1);
-  if (a.type == JAB_FP16) return launch_type<half_t>(p, c.head_dim, c.bits, nt, est, sms, st);
-  return launch_type<bf16_t>(p, c.head_dim, c.bits, nt, est, sms, st);
+  r.keys.plan = reinterpret_cast<int32_t*>(w + r.keys_plan);
+  r.keys.part_ml = reinterpret_cast<float2*>(w + r.keys_ml);
+  r.keys.part_o = reinterpret_cast<float*>(w + r.keys_o);
+  r.tiles.plan = reinterpret_cast<int32_t*>(w + r.tiles_plan);
+  r.tiles.part_ml = reinterpret_cast<float2*>(w + r.tiles_ml);
+  r.tiles.part_o = reinterpret_cast<float*>(w + r.tiles_o);
+  const bool wide = c.head_dim == 128;
+  if (a.type == JAB_FP16)
+    return wide ? kv::launch_all<half_t, 128>(p, r, c.bits, a.type, a.max_q, a.max_len, sms, st)
+                : kv::launch_all<half_t, 64>(p, r, c.bits, a.type, a.max_q, a.max_len, sms, st);
+  return wide ? kv::launch_all<bf16_t, 128>(p, r, c.bits, a.type, a.max_q, a.max_len, sms, st)
+              : kv::launch_all<bf16_t, 64>(p, r, c.bits, a.type, a.max_q, a.max_len, sms, st);
 }
 
 }  // namespace jab

@@ -1,0 +1,294 @@
+// Shared by the kernels of attention over the quantised cache: arguments, the list of work and how it is cut.
+//
+// The work of a launch is a list of key tiles in the order (KV head, entry, row tile, key tile). An entry is a
+// sequence's queries over the keys of its own, or all queries over the keys that all sequences share; rows are
+// (token, query head of the KV head's group) pairs, R of them a tile. Block c of the grid takes the tiles [c per, (c
+// + 1) per), whatever the lengths: the blocks are all resident and finish together. An item (row tile of an entry)
+// that is cut, or whose rows have keys in another entry too, leaves its part (maximum, sum, unscaled output) in a
+// slot of the workspace for the joining kernel. Every block makes the plan for itself from the lengths on
+// the device.
+#pragma once
+
+#include "common.cuh"
+#include "serve.h"
+
+namespace jab {
+namespace kv {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+enum { kTotal = 0, kItems = 1, kPer = 2, kLo = 3, kHi = 4, kLoMax = 5, kHiMin = 6, kPlanHead = 8 };
+
+// One launch's list: which entries it has, and where its plan and parts are.
+struct List {
+  bool all;                // the shared keys' entry is on it
+  int min_rows, max_rows;  // sequences of that many rows are on it
+  int32_t* plan;           // kPlanHead scalars, then cum_t [E + 1], cum_i [E + 1]
+  float2* part_ml;         // [n_slots, R]: maximum, sum
+  float* part_o;           // [n_slots, R, head_dim]
+  int n_slots;
+  int used;                // (the joining kernel: whether the list was run)
+};
+
+struct AttnParams {
+  const uint8_t *k_codes, *v_codes;
+  const float *k_scales, *v_scales;
+  int n_kv, G, n_pages, max_pages, page;
+  FastDiv by_page, by_g;
+  const void* q;
+  int64_t ldq;
+  const int32_t *q_start, *pages, *lens;
+  int n_seqs, n_tokens, shared, window;
+  float scale_log2;
+  void* out;
+  int64_t ldo;
+  float* lse;
+  List list;
+  int* status;
+};
+
+struct Entry {
+  int tok0, nq, len, kbeg;
+  bool all;
+};
+
+__device__ __forceinline__ Entry sequence(const AttnParams& p, int b) {
+  Entry en;
+  en.all = false;
+  const int s0 = __ldg(p.q_start + b), s1 = __ldg(p.q_start + b + 1);
+  en.tok0 = min(max(s0, 0), p.n_tokens);
+  en.nq = min(max(s1, en.tok0), p.n_tokens) - en.tok0;
+  const int64_t room = min((int64_t)p.max_pages * p.page, (int64_t)INT32_MAX);
+  const int len = __ldg(p.lens + b);
+  en.len = (int)min((int64_t)max(len, 0), room);
+  en.kbeg = p.shared;
+  if (s0 != en.tok0 || s1 != en.tok0 + en.nq || len != en.len) report(p.status, JAB_ERR_INVALID_ARG);
+  return en;
+}
+
+__device__ __forceinline__ int entries(const AttnParams& p) { return p.n_seqs + (p.list.all ? 1 : 0); }
+
+// Entry e of the list; a sequence that is not on it has no rows.
+__device__ __forceinline__ Entry entry_of(const AttnParams& p, int e) {
+  if (p.list.all && e-- == 0) {
+    Entry en;
+    en.all = true;
+    en.tok0 = 0, en.nq = p.n_tokens, en.len = p.shared, en.kbeg = 0;
+    return en;
+  }
+  Entry en = sequence(p, e);
+  const int rows = en.nq * p.G;
+  if (rows < p.list.min_rows || rows > p.list.max_rows) en.nq = 0;
+  return en;
+}
+
+// First key tile (KT keys each) and number of key tiles of row tile rt (at least one: an item that sees
+// nothing still has its zeros to write).
+template <int R, int KT>
+__device__ __forceinline__ void key_tiles(const AttnParams& p, const Entry& en, int rt, const int* head, int& t0, int& n) {
+  int lo, hi;
+  if (en.all) {
+    lo = head[kLo], hi = head[kHi];
+  } else {
+    const int i0 = p.by_g.quot(rt * R), i1 = p.by_g.quot(min((rt + 1) * R, en.nq * p.G) - 1);
+    const int first = en.len - en.nq + 1;
+    hi = first + i1;
+    lo = max(p.window > 0 ? first + i0 - p.window : 0, en.kbeg);
+  }
+  t0 = max(lo, 0) / KT;
+  n = hi > lo ? max((hi + KT - 1) / KT - t0, 1) : 1;
+}
+
+// Keys that every row of [r0, r1) of the entry sees: those in [lo, hi).
+__device__ __forceinline__ void seen_by_all(const AttnParams& p, const Entry& en, int r0, int r1, const int* head, int& lo, int& hi) {
+  if (en.all) {
+    lo = head[kLoMax], hi = head[kHiMin];
+  } else {
+    const int first = en.len - en.nq + 1;
+    hi = first + p.by_g.quot(r0);
+    lo = max(p.window > 0 ? first + p.by_g.quot(max(r1 - 1, r0)) - p.window : 0, en.kbeg);
+  }
+}
+
+// Keys that a row sees: [lo, hi).
+__device__ __forceinline__ void seen_by_row(const AttnParams& p, const Entry& en, int pos, int& lo, int& hi) {
+  lo = max(en.kbeg, p.window > 0 ? pos + 1 - p.window : 0);
+  hi = min(pos + 1, en.len);
+}
+
+// Last e with cum[e] <= y (cum[0] = 0 <= y < cum[E]).
+__device__ __forceinline__ int find(const int* cum, int E, int y) {
+  int lo = 0, hi = E;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (cum[mid] <= y) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+// Sequence of a token.
+__device__ __forceinline__ int sequence_of(const AttnParams& p, int token) {
+  int lo = 0, hi = p.n_seqs;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (__ldg(p.q_start + mid) <= token) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+__device__ __forceinline__ int position_of(const AttnParams& p, int token) {
+  const Entry en = sequence(p, sequence_of(p, token));
+  return en.len - en.nq + token - en.tok0;
+}
+
+// The plan, by all WARPS * 32 threads of a block: cum_t[e], cum_i[e] = key tiles and items of a KV head before entry
+// e, head[] = the scalars. A block's share is a multiple of UNIT tiles.
+template <int R, int KT, int WARPS, int UNIT>
+__device__ void make_plan(const AttnParams& p, int* cum_t, int* cum_i, int* head) {
+  __shared__ int w_v[4][WARPS];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, E = entries(p);
+  if (p.list.all) {  // what the queries see of the shared keys: any of them, and all of them
+    int v[4] = {p.shared, 0, 0, p.shared};
+    for (int b = tid; b < p.n_seqs; b += 32 * WARPS) {
+      const Entry en = sequence(p, b);
+      if (en.nq > 0) {
+        const int first = en.len - en.nq + 1;
+        v[0] = min(v[0], p.window > 0 ? max(first - p.window, 0) : 0);
+        v[1] = max(v[1], min(en.len, p.shared));
+        v[2] = max(v[2], p.window > 0 ? en.len - p.window : 0);
+        v[3] = min(v[3], first);
+      }
+    }
+    v[0] = __reduce_min_sync(0xffffffffu, v[0]);
+    v[1] = __reduce_max_sync(0xffffffffu, v[1]);
+    v[2] = __reduce_max_sync(0xffffffffu, v[2]);
+    v[3] = __reduce_min_sync(0xffffffffu, v[3]);
+    if (lane == 0)
+      for (int i = 0; i < 4; ++i) w_v[i][warp] = v[i];
+    __syncthreads();
+    if (tid == 0) {
+      for (int w = 1; w < WARPS; ++w) {
+        v[0] = min(v[0], w_v[0][w]), v[1] = max(v[1], w_v[1][w]);
+        v[2] = max(v[2], w_v[2][w]), v[3] = min(v[3], w_v[3][w]);
+      }
+      head[kLo] = v[0], head[kHi] = v[1], head[kLoMax] = v[2], head[kHiMin] = v[3];
+    }
+    __syncthreads();
+  } else if (tid == 0) {
+    head[kLo] = head[kHi] = head[kLoMax] = head[kHiMin] = 0;
+  }
+  const int run = (E + 32 * WARPS - 1) / (32 * WARPS);
+  const int e0 = min(tid * run, E), e1 = min(e0 + run, E);
+  int st = 0, si = 0;
+  for (int pass = 0; pass < 2; ++pass) {
+    int at = 0, ai = 0;
+    if (pass == 1) {  // exclusive prefix over the threads
+      int t = st, i = si;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int ut = __shfl_up_sync(0xffffffffu, t, o), ui = __shfl_up_sync(0xffffffffu, i, o);
+        if (lane >= o) t += ut, i += ui;
+      }
+      if (lane == 31) w_v[0][warp] = t, w_v[1][warp] = i;
+      __syncthreads();
+      at = t - st, ai = i - si;
+      for (int w = 0; w < warp; ++w) at += w_v[0][w], ai += w_v[1][w];
+    }
+    for (int e = e0; e < e1; ++e) {
+      const Entry en = entry_of(p, e);
+      const int nrt = (en.nq * p.G + R - 1) / R;
+      if (pass == 1) cum_t[e] = at, cum_i[e] = ai;
+      int sum = 0, t0, n;
+      if (en.all) {
+        key_tiles<R, KT>(p, en, 0, head, t0, n);
+        sum = n * nrt;
+      } else {
+        for (int rt = 0; rt < nrt; ++rt) {
+          key_tiles<R, KT>(p, en, rt, head, t0, n);
+          sum += n;
+        }
+      }
+      at += sum, ai += nrt;
+    }
+    if (pass == 0) st = at, si = ai;
+  }
+  if (tid == 0) {
+    int t = 0, i = 0;
+    for (int w = 0; w < WARPS; ++w) t += w_v[0][w], i += w_v[1][w];
+    cum_t[E] = t, cum_i[E] = i;
+    head[kTotal] = t, head[kItems] = i;
+    const int64_t per = ((int64_t)t * p.n_kv + gridDim.x - 1) / gridDim.x;
+    head[kPer] = (int)min((per + UNIT - 1) / UNIT * UNIT, (int64_t)INT32_MAX);
+  }
+  __syncthreads();
+  if (blockIdx.x == 0) {
+    for (int i = tid; i < kPlanHead; i += 32 * WARPS) p.list.plan[i] = head[i];
+    for (int i = tid; i <= E; i += 32 * WARPS) p.list.plan[kPlanHead + i] = cum_t[i], p.list.plan[kPlanHead + E + 1 + i] = cum_i[i];
+  }
+}
+
+// The item that tile x of the list is in.
+struct Item {
+  Entry en;
+  int h, e, rt;     // KV head, entry, row tile
+  int t0, n;        // its first key tile and their number
+  int s0, s1;       // the part of them, counted from t0, that is this block's
+  int rows;         // rows of the tile in use
+};
+template <int R, int KT>
+__device__ __forceinline__ Item item_at(const AttnParams& p, const int* cum_t, const int* head, int64_t x, int64_t x1) {
+  Item it;
+  const int total = head[kTotal];
+  it.h = (int)(x / total);
+  const int y = (int)(x - (int64_t)it.h * total);
+  it.e = find(cum_t, entries(p), y);
+  it.en = entry_of(p, it.e);
+  int base = cum_t[it.e];
+  it.rt = 0;
+  key_tiles<R, KT>(p, it.en, 0, head, it.t0, it.n);
+  if (it.en.all) {
+    it.rt = (y - base) / it.n;
+    base += it.rt * it.n;
+  } else {
+    while (y >= base + it.n) {
+      base += it.n;
+      key_tiles<R, KT>(p, it.en, ++it.rt, head, it.t0, it.n);
+    }
+  }
+  it.s0 = y - base;
+  it.s1 = (int)min((int64_t)it.n, it.s0 + (x1 - x));
+  it.rows = min(R, it.en.nq * p.G - it.rt * R);
+  return it;
+}
+
+// Where a part goes. With shared keys every item leaves a part (block + item counts up along the list); without, only
+// the first and the last of a block can be cut.
+__device__ __forceinline__ int64_t slot_of(const AttnParams& p, int block, int item, bool first) {
+  return p.shared > 0 ? (int64_t)block + item : 2 * (int64_t)block + (first ? 0 : 1);
+}
+
+// 2^(a - b) with 2^(-inf - -inf) = 0.
+__device__ __forceinline__ float shift2(float a, float b) { return a == -INFINITY ? 0.f : exp2f(a - b); }
+
+template <class T>
+__device__ __forceinline__ void store_out(T* p, float v);
+template <>
+__device__ __forceinline__ void store_out<half_t>(half_t* p, float v) { *p = __float2half_rn(v); }
+template <>
+__device__ __forceinline__ void store_out<bf16_t>(bf16_t* p, float v) { *p = __float2bfloat16_rn(v); }
+
+// Power of two that brings a bf16 row whose largest magnitude has the bits `big` to [8, 16), and its inverse: fp16
+// then holds the row's elements exactly down to 2^-24 of the largest. Both are normal numbers.
+__device__ __forceinline__ void row_power(uint32_t big, float& by, float& back) {
+  const int e = min(max((int)(big >> 23), 4), 253);
+  by = __uint_as_float((uint32_t)(257 - e) << 23);   // 2^(130 - e)
+  back = __uint_as_float((uint32_t)(e - 3) << 23);   // 2^(e - 130)
+}
+
+// Tile kernel (kv_attn_tile.cu): 128 rows x 128 keys on the tensor cores.
+constexpr int kTileRows = 128, kTileKeys = 128;
+cudaError_t launch_tiles(const AttnParams& p, jab_dtype type, int dh, int bits, int64_t est_tiles, int sms, cudaStream_t st);
+
+}  // namespace kv
+}  // namespace jab

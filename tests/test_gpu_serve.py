@@ -400,3 +400,69 @@ def test_attention_bad_indices_are_reported():
     for pages, lens, start in ((i(9, 0), 20, (0, 1)), (i(-1, 0), 20, (0, 1)), (i(0, 1), 33, (0, 1)), (i(0, 1), -1, (0, 1)), (i(0, 1), 20, (0, 2)), (i(0, 1), 20, (-1, 1))):
         J.jab_kv_attention(cache, q, i(*start), pages.view(1, 2), i(lens), out, ws, 1, 64)
         assert J.jab_get_device_status() == 1, (pages, lens, start)
+
+
+# 128-row tiles round a weight once in key tiles that no mask cuts (2^-11 of it); the rest of the bound as above.
+def _attend_tiles(cache, kd, vd, q, q_lens, lens, pages, shared=0, window=0):
+    n, hq, dh = q.shape
+    q_start = torch.tensor([0] + list(torch.tensor(q_lens).cumsum(0)), dtype=torch.int32, device="cuda")
+    out, lse = torch.full_like(q, 77.0), torch.full((n, hq), 77.0, device="cuda")
+    ws = torch.full((J.jab_kv_attention_workspace_size(cache, len(lens), n, hq, max(q_lens), max(lens), shared),), 0xFF, dtype=torch.uint8,
+                    device="cuda")
+    J.jab_kv_attention(cache, q, q_start, pages, torch.tensor(lens, dtype=torch.int32, device="cuda"), out, ws, max(q_lens), max(lens),
+                       shared_len=shared, window=window, lse=lse)
+    assert J.jab_get_device_status() == 0
+    at, page, hkv = 0, cache.page_tokens, cache.n_kv_heads
+    for b, (nq, length) in enumerate(zip(q_lens, lens)):
+        if nq == 0:
+            continue
+        j = torch.arange(length, device="cuda")
+        ids = pages[b].long()[j // page]
+        k, v = kd[ids, j % page], vd[ids, j % page]
+        pos = torch.arange(length - nq, length, device="cuda")[:, None]
+        seen = (j <= pos) & ((j > pos - window) if window else torch.ones_like(j <= pos))
+        for h in range(hq):
+            s = (q[at:at + nq, h].double() @ k[:, h // (hq // hkv)].t() / math.sqrt(dh)).masked_fill(~seen, -math.inf)
+            ls = torch.logsumexp(s, -1)
+            w = torch.where(seen, torch.exp(s - torch.where(ls > -math.inf, ls, 0.0)[:, None]), 0.0)
+            vv = v[:, h // (hq // hkv)]
+            o, mag = w @ vv, w @ vv.abs()
+            tol = (2.0 ** -11 + 2.0 ** -16) * mag + length * 2.0 ** -25 * vv.abs().max() + HALF_ULP[q.dtype] * o.abs() + 1e-30
+            err = (out[at:at + nq, h].double() - o).abs()
+            assert bool((err <= tol).all()), (b, h, (err / tol).max().item())
+            fin = ls > -math.inf
+            got = lse[at:at + nq, h].double()
+            assert bool((got[~fin] == -math.inf).all()) and bool(((got - ls).abs()[fin] <= 2.0 ** -16 + 2.0 ** -21 * ls.abs()[fin]).all())
+        at += nq
+
+
+@pytest.mark.parametrize("q_lens,lens,shared,window", [
+    ([300, 77], [1000, 900], 0, 0),            # chunks behind a context, several row and key tiles
+    ([513], [513], 0, 0),                      # a prompt from its first token
+    ([129, 1, 40, 2], [700, 1500, 40, 3], 0, 0),   # a chunk, single tokens and a short prompt in one batch
+    ([260, 33], [1700, 500], 0, 200),          # sliding window: key tiles before it are skipped
+    ([100], [60], 0, 0),                       # more queries than tokens: the first rows see nothing
+    ([1] * 40, [520 + 7 * i for i in range(40)], 512, 0),     # single tokens behind a prefix
+    ([1] * 40, [520 + 7 * i for i in range(40)], 512, 300),
+    ([50, 3, 70], [900, 785, 1001], 768, 0),   # chunks behind a prefix
+    ([64, 64], [64, 300], 192, 0),             # a sequence shorter than the prefix
+])
+@pytest.mark.parametrize("dh,hq,hkv,bits,dt", [(128, 8, 2, 8, torch.float16), (64, 4, 4, 8, torch.bfloat16), (128, 6, 2, 4, torch.bfloat16),
+                                               (64, 4, 1, 4, torch.float16)])
+def test_attention_many_rows(q_lens, lens, shared, window, dh, hq, hkv, bits, dt):
+    g = _gen(sum(lens) + dh + bits)
+    page = 64 if shared else 48
+    cache, kd, vd = _filled(g, hkv, dh, bits, page, sum(-(-max(n, shared) // page) for n in lens) + 3)
+    q = torch.randn((sum(q_lens), hq, dh), generator=g, device="cuda").to(dt)
+    pages = _pages(g, [max(n, shared) for n in lens], page, cache.n_pages, shared)
+    for b, n in enumerate(lens):  # entries past a sequence's pages are not looked at
+        pages[b, -(-max(n, shared) // page):] = -1
+    _attend_tiles(cache, kd, vd, q, q_lens, lens, pages, shared=shared, window=window)
+
+
+def test_attention_unused_table_entries():
+    cache, kd, vd = _filled(_gen(1), 2, 64, 8, 16, 8)
+    pages = torch.full((3, 4), -1, dtype=torch.int32, device="cuda")
+    pages[1, 0], pages[2, :2] = 5, torch.tensor([1, 7], dtype=torch.int32, device="cuda")
+    q = torch.randn((3, 4, 64), generator=_gen(2), device="cuda").to(torch.float16)
+    _attend(cache, kd, vd, q, [1, 1, 1], [0, 9, 20], pages)
