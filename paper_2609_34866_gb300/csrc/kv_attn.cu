@@ -423,15 +423,30 @@ __device__ __forceinline__ bool join(AttnParams p, const List& list, int e, int 
   const int c0 = (int)(y0 / per), c1 = (int)((y1 - 1) / per);
   if (c0 == c1 && p.shared == 0) return false;  // written by its block
   const int item = h * head[kItems] + cum_i[e] + want;
-  for (int c = c0; c <= c1; ++c) {
-    const int64_t slot = slot_of(p, c, item, (int64_t)c * per >= y0);
-    if (slot >= list.n_slots) continue;
-    const float2 ml = list.part_ml[slot * R + r];
-    const float mn = fmaxf(mx, ml.x), fa = shift2(mx, mn), fb = shift2(ml.x, mn);
-    mx = mn;
-    l = l * fa + ml.y * fb;
+  // 32 parts at a time: a lane has the statistics of one, then all lanes add up the parts' rows
+  for (int c = c0; c <= c1; c += 32) {
+    const int mine = c + lane;
+    const int64_t slot = slot_of(p, mine, item, (int64_t)mine * per >= y0);
+    const bool have = mine <= c1 && slot < list.n_slots;
+    const float2 ml = have ? list.part_ml[slot * R + r] : make_float2(-INFINITY, 0.f);
+    float mn = ml.x;
 #pragma unroll
-    for (int i = 0; i < DH / 32; ++i) o[i] = o[i] * fa + fb * list.part_o[(slot * R + r) * DH + lane + 32 * i];
+    for (int w = 16; w > 0; w >>= 1) mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, w));
+    mn = fmaxf(mn, mx);
+    const float f = shift2(ml.x, mn), fa = shift2(mx, mn);
+    mx = mn;
+    l = l * fa + warp_sum(ml.y * f);
+#pragma unroll
+    for (int i = 0; i < DH / 32; ++i) o[i] *= fa;
+    const int64_t at = have ? (slot * R + r) * DH : 0;
+    const int k1 = min(32, c1 - c + 1);
+#pragma unroll 8
+    for (int k = 0; k < k1; ++k) {
+      const float fk = __shfl_sync(0xffffffffu, f, k);
+      const float* part = list.part_o + __shfl_sync(0xffffffffu, at, k) + lane;
+#pragma unroll
+      for (int i = 0; i < DH / 32; ++i) o[i] += fk == 0.f ? 0.f : fk * __ldcg(part + 32 * i);
+    }
   }
   return true;
 }
@@ -446,7 +461,7 @@ __global__ void __launch_bounds__(128) kv_merge_kernel(const __grid_constant__ A
   const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
   if (unit >= (int64_t)p.n_tokens * Hq) return;
   const int token = (int)(unit / Hq), qh = (int)(unit - (int64_t)token * Hq), h = qh / p.G, gi = qh - h * p.G;
-  const int b = sequence_of(p, token);
+  const int b = sequence_of_warp(p, token, lane);
   float mx = -INFINITY, l = 0.f, o[DH / 32] = {};
   bool any = false;
   if (by_keys.used && by_keys.all) any |= join<DH, R, 16>(p, by_keys, 0, token, h, gi, lane, mx, l, o);
@@ -585,6 +600,7 @@ cudaError_t launch_kv_attention(const KvAttnArgs& a, int sms, cudaStream_t st) {
   p.n_pages = (int)std::min<int64_t>(c.n_pages, INT32_MAX);
   p.max_pages = a.max_pages;
   p.page = c.page_tokens;
+  p.copy_keys = std::min(c.page_tokens & -c.page_tokens, kv::kTileKeys);
   p.by_page = FastDiv(p.page);
   p.by_g = FastDiv(p.G);
   p.q = a.q;

@@ -34,6 +34,7 @@ struct AttnParams {
   const uint8_t *k_codes, *v_codes;
   const float *k_scales, *v_scales;
   int n_kv, G, n_pages, max_pages, page;
+  int copy_keys;  // keys that are sure to lie in one page, from any multiple of it on: gcd(page, 128)
   FastDiv by_page, by_g;
   const void* q;
   int64_t ldq;
@@ -134,6 +135,18 @@ __device__ __forceinline__ int sequence_of(const AttnParams& p, int token) {
     const int mid = (lo + hi) >> 1;
     if (__ldg(p.q_start + mid) <= token) lo = mid;
     else hi = mid;
+  }
+  return lo;
+}
+// The same by a whole warp for one token: 32 places at a time instead of one.
+__device__ __forceinline__ int sequence_of_warp(const AttnParams& p, int token, int lane) {
+  int lo = 0, hi = p.n_seqs;
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 31) / 32, at = lo + lane * step;
+    const bool below = at < hi && __ldg(p.q_start + at) <= token;
+    const int last = max(31 - __clz(__ballot_sync(0xffffffffu, below)), 0);  // (lane 0 is below but for bad tables)
+    lo += last * step;
+    hi = min(lo + step, hi);
   }
   return lo;
 }
