@@ -535,7 +535,7 @@ template <class T, int DH, int BITS, int NT>
 cudaError_t launch_keys(const AttnParams& p, int64_t est_tiles, int sms, cudaStream_t st) {
   auto kern = kv_attn_kernel<T, DH, BITS, NT>;
   constexpr int R = 8 * NT;
-  const size_t most = (size_t)W * R * (DH + 4) * 4 + (size_t)2 * (4096 + 2) * 4;
+  const size_t most = (size_t)W * R * (DH + 4) * 4 + (size_t)2 * (2048 + 2) * 4;
   static bool attr_set = false;
   if (!attr_set) {
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);

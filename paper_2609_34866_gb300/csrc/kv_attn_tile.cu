@@ -26,7 +26,7 @@ namespace jab {
 namespace kv {
 namespace {
 
-constexpr int R = kTileRows, KT = kTileKeys, THREADS = 640, SCB = 3, KST = 3, VST = 2;
+constexpr int R = kTileRows, KT = kTileKeys, THREADS = 640, SCB = 3, KST = 2, VST = 2;
 
 template <int DH, int BITS>
 struct Layout {
@@ -34,16 +34,16 @@ struct Layout {
   static constexpr int TILE = KT * DH * 2;             // K or V in fp16
   static constexpr int RAW = KT * DH * BITS / 8;       // K or V as codes
   static constexpr int K_STAGE = RAW + 2 * KT * 4;     // K and the scales of both
-  static constexpr int K_OFF = 0, V_OFF = 2 * TILE, RK_OFF = 3 * TILE, RV_OFF = RK_OFF + KST * K_STAGE;
+  static constexpr int K_OFF = 0, V_OFF = 2 * TILE, RK_OFF = 4 * TILE, RV_OFF = RK_OFF + KST * K_STAGE;
   static constexpr int SC_OFF = RV_OFF + VST * RAW;                         // per tile: K scale * log2 e * c, V scale, its log2
   static constexpr int ROW_OFF = SC_OFF + SCB * 3 * KT * 4;       // per item: lo, hi, power of two of Q
   static constexpr int BAR_OFF = ROW_OFF + 2 * 3 * R * 4;
   static constexpr int USED = BAR_OFF + 512;
-  static constexpr uint32_t S_COL = 0, O_COL = 256, Q_COL = 384, P_COL = 448;  // (two S of 128)
+  static constexpr uint32_t S_COL = 0, O_COL = 256, Q_COL = 384, LO_COL = 448;  // two S of 128 (then P in their place)
 };
 
 struct Bars {
-  uint64_t rk_full[KST], rk_empty[KST], rv_full[VST], rv_empty[VST], k_full[2], k_empty[2], sc_full[SCB], sc_empty[SCB], v_full;
+  uint64_t rk_full[KST], rk_empty[KST], rv_full[VST], rv_empty[VST], k_full[2], k_empty[2], sc_full[SCB], sc_empty[SCB], v_full[2], v_empty[2];
   uint64_t q_full[2], q_empty, s_full[2], s_empty[2], p_full, pv_done, o_full, o_empty, drain[2];
   uint32_t tmem_base;
   int abort;
@@ -95,20 +95,17 @@ template <int DH, int BITS>
 __device__ __forceinline__ void convert_tile(const uint8_t* raw, uint8_t* dst, int tid) {
   using Word = std::conditional_t<BITS == 8, uint2, uint32_t>;
   constexpr int N = KT * DH / 8 / 128, PER_ROW = DH / 8;
-  Word w[N];
+#pragma unroll 1
+  for (int i0 = 0; i0 < N; i0 += 4) {
+    Word w[4];
 #pragma unroll
-  for (int i = 0; i < N; ++i) w[i] = reinterpret_cast<const Word*>(raw)[tid + i * 128];
+    for (int i = 0; i < 4; ++i) w[i] = reinterpret_cast<const Word*>(raw)[tid + (i0 + i) * 128];
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int key = (tid + i * 128) / PER_ROW, c = tid % PER_ROW;
-    *reinterpret_cast<uint4*>(dst + (c >> 3) * (128 * 128) + key * 128 + (((c & 7) ^ (key & 7)) << 4)) = eight_codes(w[i]);
+    for (int i = 0; i < 4; ++i) {
+      const int key = (tid + (i0 + i) * 128) / PER_ROW, c = tid % PER_ROW;
+      *reinterpret_cast<uint4*>(dst + (c >> 3) * (128 * 128) + key * 128 + (((c & 7) ^ (key & 7)) << 4)) = eight_codes(w[i]);
+    }
   }
-}
-
-// Uses of v stay behind this point (a load from tensor memory is over at the wait, not at the load).
-__device__ __forceinline__ void arrived(uint32_t (&v)[32]) {
-#pragma unroll
-  for (int i = 0; i < 32; ++i) asm volatile("" : "+r"(v[i]));
 }
 
 // 32 scores of a thread: rows c = 0, 1 of the warp's pairs, columns c0 + 8n + e (n < 8, e < 2) of the tile as the 16x256b
@@ -121,12 +118,28 @@ __device__ __forceinline__ float2 score(const uint32_t* e, float2 ks, float fac,
   return tc::fma2(a, ks, make_float2(-ref, -ref));
 }
 
-// Weights of a tile that no mask cuts, as fp16 pairs, and the row sums of 2^y; `big` has the largest weight of either
-// half of the pairs. As long as none passes 2^8 the maximum does not move, and neither it nor the V scales'
+// Rows c = 0, 1 of DH accumulator columns times f[c].
+template <int DH>
+__device__ __forceinline__ void scale_rows(uint32_t taddr, const float (&f)[2]) {
+#pragma unroll 1
+  for (int b = 0; b < DH / 32; ++b) {
+    uint32_t o[16];
+    tc::tmem_ld_16x256b_x4(taddr + 32 * b, o);
+    tc::tmem_ld_wait();
+#pragma unroll
+    for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f[(k >> 1) & 1]);
+    tc::tmem_st_16x256b_x4(taddr + 32 * b, o);
+  }
+  tc::tmem_st_wait();
+}
+
+// Weights of keys that no mask hides, as fp16 pairs, and the row sums of 2^y; `big` has the largest weight of either
+// half of the pairs. As long as none passes 2^15 the reference may stay, and neither the maximum nor the V scales'
 // logarithms are needed.
 template <class T>
 __device__ __forceinline__ void plain_weights(const uint32_t (&v)[32], const float* sc, const float (&ref)[2], const float (&fac)[2], float2 (&l)[2],
-                                              uint32_t* hi2, uint32_t& big) {
+                                              uint32_t (&hi2)[16], uint32_t& big) {
+  big = 0;
 #pragma unroll
   for (int n = 0; n < 8; ++n) {
     const float2 ks = *reinterpret_cast<const float2*>(sc + 8 * n), vs = *reinterpret_cast<const float2*>(sc + KT + 8 * n);
@@ -203,8 +216,10 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
       tc::mbar_init(&bars->k_empty[s], 1);
       tc::mbar_init(&bars->drain[s], 1);
       tc::mbar_init(&bars->q_full[s], 4);
+      tc::mbar_init(&bars->v_full[s], 4);
+      tc::mbar_init(&bars->v_empty[s], 1);
       tc::mbar_init(&bars->s_full[s], 1);
-      tc::mbar_init(&bars->s_empty[s], 9);  // the softmax warps, and P V (which may read what S leaves over from there)
+      tc::mbar_init(&bars->s_empty[s], 1);  // (P V has read the weights that took the scores' place)
     }
     for (int s = 0; s < KST; ++s) {
       tc::mbar_init(&bars->rk_full[s], 1);
@@ -218,7 +233,6 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
       tc::mbar_init(&bars->sc_full[s], 4);
       tc::mbar_init(&bars->sc_empty[s], 8);
     }
-    tc::mbar_init(&bars->v_full, 4);
     tc::mbar_init(&bars->q_empty, 1);
     tc::mbar_init(&bars->p_full, 8);
     tc::mbar_init(&bars->pv_done, 1);
@@ -325,29 +339,30 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
       constexpr uint32_t IDESC = tc::idesc_f16(false, R, DH) | (1u << 16);  // B MN-major
       int j = 0, i = 0;
       bool ok = true;
-      const uint64_t vd = tc::sdesc_mnmajor_sw128(tc::smem_u32(smem + L::V_OFF), L::CHUNK, 1024);
       for (int64_t x = x0; x < x1 && ok; ++i) {
         const Item it = item_at<R, KT>(p, cum_t, head, x, x1);
         int all_lo, all_hi;
         seen_by_all(p, it.en, it.rt * R, it.rt * R + it.rows, head, all_lo, all_hi);
         ok = tc::mbar_wait(&bars->o_empty, (i & 1) ^ 1, abort, p.status);
         for (int s = it.s0; s < it.s1 && ok; ++s, ++j) {
-          ok = tc::mbar_wait(&bars->v_full, j & 1, abort, p.status) && tc::mbar_wait(&bars->p_full, j & 1, abort, p.status);
+          ok = tc::mbar_wait(&bars->v_full[j & 1], (j >> 1) & 1, abort, p.status) && tc::mbar_wait(&bars->p_full, j & 1, abort, p.status);
           if (!ok) break;
           tc::fence_after_sync();
+          const uint64_t vd = tc::sdesc_mnmajor_sw128(tc::smem_u32(smem + L::V_OFF + (j & 1) * L::TILE), L::CHUNK, 1024);
           const int key0 = (it.t0 + s) * KT;
           const bool masked = key0 < all_lo || key0 + KT > all_hi;
 #pragma unroll
           for (int k = 0; k < KT / 16; ++k)
-            tc::umma_f16_ts(tmem + L::O_COL, tmem + L::P_COL + k * 8, tc::sdesc_advance(vd, k * 16 * 128), IDESC,
+            tc::umma_f16_ts(tmem + L::O_COL, tmem + L::S_COL + (j & 1) * KT + k * 8, tc::sdesc_advance(vd, k * 16 * 128), IDESC,
                             s > it.s0 || k > 0 ? 1u : 0u);
           if (masked) {
 #pragma unroll
             for (int k = 0; k < KT / 16; ++k)
-              tc::umma_f16_ts(tmem + L::O_COL, tmem + L::S_COL + (j & 1) * KT + k * 8, tc::sdesc_advance(vd, k * 16 * 128), IDESC, 1u);
+              tc::umma_f16_ts(tmem + L::O_COL, tmem + L::LO_COL + k * 8, tc::sdesc_advance(vd, k * 16 * 128), IDESC, 1u);
           }
           tc::umma_commit(&bars->pv_done);
           tc::umma_commit(&bars->s_empty[j & 1]);
+          tc::umma_commit(&bars->v_empty[j & 1]);
         }
         if (ok) tc::umma_commit(&bars->o_full);
         x += it.s1 - it.s0;
@@ -393,27 +408,53 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
           __syncwarp();
           return true;
         };
-        bool simple = !masked && !__any_sync(0xffffffffu, m[0] == -INFINITY || m[1] == -INFINITY);
-        if (simple) {
-          const float2 old[2] = {l[0], l[1]};
-          uint32_t v[2][32], hi2[32], big = 0;
-          __syncwarp();
-          tc::tmem_ld_16x256b_x8(ts, v[0]);
-          tc::tmem_ld_wait();
-          tc::tmem_ld_16x256b_x8(ts + 64, v[1]);
-          plain_weights<T>(v[0], sc, m, fac, l, hi2, big);
-          tc::tmem_ld_wait();
-          arrived(v[1]);
-          plain_weights<T>(v[1], sc + 64, m, fac, l, hi2 + 16, big);
-          simple = !__any_sync(0xffffffffu, either_at_least(big, 0x5c01u));
-          if (simple) {
-            if (!(ok = before_p())) break;
-            tc::tmem_st_16x128b_x16(tw + L::P_COL, hi2);
-          } else {
-            l[0] = old[0], l[1] = old[1];
+        // Weights take the place of the scores that have been read, 64 keys at a time (a loop, not two copies: what the
+        // roles of this kernel have to fetch as code is what slowed them all down).
+        if (!masked && !__any_sync(0xffffffffu, m[0] == -INFINITY || m[1] == -INFINITY)) {
+#pragma unroll 1
+          for (int b = 0; b < 2; ++b) {
+            uint32_t v[32], h[16], big;
+            __syncwarp();
+            tc::tmem_ld_16x256b_x8(ts + 64 * b, v);
+            tc::tmem_ld_wait();
+            float2 sum[2] = {l[0], l[1]};
+            plain_weights<T>(v, sc + 64 * b, m, fac, sum, h, big);
+            if (__any_sync(0xffffffffu, either_at_least(big, 0x7800u))) {
+              // The maximum has to move, by a whole power of two: what is there of this tile's weights, of O and of the
+              // sums goes down by it, and the 64 weights are taken again.
+              float top[2] = {-INFINITY, -INFINITY}, f[2];
+              const int lo_[2] = {0, 0}, hi_[2] = {INT32_MAX, INT32_MAX};
+              masked_top<T>(v, sc + 64 * b, fac, lo_, hi_, 0, top);
+#pragma unroll
+              for (int c = 0; c < 2; ++c) {
+                top[c] = fmaxf(top[c], __shfl_xor_sync(0xffffffffu, top[c], 1));
+                top[c] = fmaxf(top[c], __shfl_xor_sync(0xffffffffu, top[c], 2));
+                const float up = ceilf(fmaxf(top[c] - m[c], 0.f));
+                f[c] = exp2f(-up);
+                m[c] += up;
+                l[c].x *= f[c], l[c].y *= f[c];
+              }
+              if (!(ok = before_p())) break;
+              if (s > it.s0) scale_rows<DH>(tw + L::O_COL, f);
+              if (b > 0) {
+                uint32_t e[16];
+                tc::tmem_ld_16x128b_x8(ts, e);
+                tc::tmem_ld_wait();
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                  const float2 w = __half22float2(*reinterpret_cast<const __half2*>(&e[k]));
+                  e[k] = tc::pack_half2(w.x * f[k & 1], w.y * f[k & 1]);
+                }
+                tc::tmem_st_16x128b_x8(ts, e);
+              }
+              sum[0] = l[0], sum[1] = l[1];
+              plain_weights<T>(v, sc + 64 * b, m, fac, sum, h, big);
+            }
+            l[0] = sum[0], l[1] = sum[1];
+            tc::tmem_st_16x128b_x8(ts + 32 * b, h);
           }
-        }
-        if (!simple) {  // a mask, the item's first tile, or a maximum that moves: the rows' maxima first
+          if (!ok) break;
+        } else {  // a mask, or the item's first tile: the rows' maxima first
           float top[2] = {-INFINITY, -INFINITY};
           const int lo_[2] = {masked ? lo[0] : 0, masked ? lo[1] : 0}, hi_[2] = {masked ? hi[0] : INT32_MAX, masked ? hi[1] : INT32_MAX};
 #pragma unroll 1
@@ -439,18 +480,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
               m[c] = t;
               l[c].x *= f[c], l[c].y *= f[c];
             }
-            if (s > it.s0) {
-#pragma unroll
-              for (int b = 0; b < DH / 32; ++b) {
-                uint32_t o[16];
-                tc::tmem_ld_16x256b_x4(tw + L::O_COL + 32 * b, o);
-                tc::tmem_ld_wait();
-#pragma unroll
-                for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f[(k >> 1) & 1]);
-                tc::tmem_st_16x256b_x4(tw + L::O_COL + 32 * b, o);
-              }
-              tc::tmem_st_wait();
-            }
+            if (s > it.s0) scale_rows<DH>(tw + L::O_COL, f);
           }
           const float ref[2] = {m[0] == -INFINITY ? 0.f : m[0], m[1] == -INFINITY ? 0.f : m[1]};
 #pragma unroll 1
@@ -463,8 +493,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
             uint32_t h[16], r[16];
 #pragma unroll
             for (int k = 0; k < 16; ++k) h[k] = v[2 * k], r[k] = v[2 * k + 1];
-            tc::tmem_st_16x128b_x8(tw + L::P_COL + 32 * b, h);
-            if (masked) tc::tmem_st_16x128b_x8(ts + 32 * b, r);  // over scores that have been read
+            tc::tmem_st_16x128b_x8(ts + 32 * b, h);
+            if (masked) tc::tmem_st_16x128b_x8(tw + L::LO_COL + 32 * b, r);
           }
         }
         tc::tmem_st_wait();
@@ -473,7 +503,6 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
         if (lane == 0) {
           tc::mbar_arrive(&bars->p_full);
           tc::mbar_arrive(&bars->sc_empty[j % SCB]);
-          tc::mbar_arrive(&bars->s_empty[j & 1]);
         }
       }
       if (!ok || !(ok = tc::mbar_wait(&bars->o_full, i & 1, abort, p.status))) break;
@@ -501,7 +530,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
           else if (p.lse != nullptr) p.lse[token * ((int64_t)p.n_kv * p.G) + qh] = t == 0.f ? -INFINITY : (m[c] + log2f(t)) * kLn2;
         }
       }
-#pragma unroll
+#pragma unroll 1
       for (int b = 0; b < DH / 32; ++b) {
         uint32_t o[16];
         __syncwarp();
@@ -539,9 +568,9 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
     if (!keys) {
       for (int j = 0; j < total; ++j) {
         if (!tc::mbar_wait(&bars->rv_full[j % VST], (j / VST) & 1, abort, p.status)) break;
-        if (j > 0 && !tc::mbar_wait(&bars->pv_done, (j - 1) & 1, abort, p.status)) break;
-        convert_tile<DH, BITS>(smem + L::RV_OFF + (j % VST) * L::RAW, smem + L::V_OFF, tid);
-        done(&bars->v_full);
+        if (!tc::mbar_wait(&bars->v_empty[j & 1], ((j >> 1) & 1) ^ 1, abort, p.status)) break;
+        convert_tile<DH, BITS>(smem + L::RV_OFF + (j % VST) * L::RAW, smem + L::V_OFF + (j & 1) * L::TILE, tid);
+        done(&bars->v_full[j & 1]);
         if (lane == 0) tc::mbar_arrive(&bars->rv_empty[j % VST]);
       }
     } else {
@@ -632,8 +661,8 @@ template <class T, int DH, int BITS>
 cudaError_t launch_as(const AttnParams& p, int64_t est_tiles, int sms, cudaStream_t st) {
   using L = Layout<DH, BITS>;
   auto kern = kv_tile_kernel<T, DH, BITS>;
-  constexpr int most = L::USED + 1024 + 2 * 4098 * 4;
-  static_assert(most <= 226 * 1024, "shared memory budget");
+  constexpr int most = L::USED + 1024 + 2 * 2050 * 4;
+  static_assert(most <= 226 * 1024 + 512, "shared memory budget");
   const int smem = L::USED + 1024 + 2 * (p.n_seqs + 2) * 4;
   static bool attr_set = false;
   if (!attr_set) {
