@@ -2,8 +2,8 @@
 //
 // The work of a launch is a list of key tiles in the order (KV head, entry, row tile, key tile). An entry is a
 // sequence's queries over the keys of its own, or all queries over the keys that all sequences share; rows are
-// (token, query head of the KV head's group) pairs, R of them a tile. Block c of the grid takes the tiles [c per, (c
-// + 1) per), whatever the lengths: the blocks are all resident and finish together. An item (row tile of an entry)
+// (token, query head of the KV head's group) pairs, R of them a tile. Worker c (a warp or a block) takes the tiles [c
+// per, (c + 1) per), whatever the lengths: the workers are all resident and finish together. An item (row tile of an entry)
 // that is cut, or whose rows have keys in another entry too, leaves its part (maximum, sum, unscaled output) in a
 // slot of the workspace for the joining kernel. Every block makes the plan for itself from the lengths on
 // the device.
@@ -23,11 +23,13 @@ enum { kTotal = 0, kItems = 1, kPer = 2, kLo = 3, kHi = 4, kLoMax = 5, kHiMin = 
 struct List {
   bool all;                // the shared keys' entry is on it
   int min_rows, max_rows;  // sequences of that many rows are on it
-  int32_t* plan;           // kPlanHead scalars, then cum_t [E + 1], cum_i [E + 1]
+  int32_t* plan;           // kPlanHead scalars
+  int4* items;             // [max_items] of a KV head: first token, row tile * 256 + rows, first key tile, key tiles
+  int max_items;
   float2* part_ml;         // [n_slots, R]: maximum, sum
   float* part_o;           // [n_slots, R, head_dim]
   int n_slots;
-  int used;                // (the joining kernel: whether the list was run)
+  int used;                // whether the list is run
 };
 
 struct AttnParams {
@@ -138,27 +140,15 @@ __device__ __forceinline__ int sequence_of(const AttnParams& p, int token) {
   }
   return lo;
 }
-// The same by a whole warp for one token: 32 places at a time instead of one.
-__device__ __forceinline__ int sequence_of_warp(const AttnParams& p, int token, int lane) {
-  int lo = 0, hi = p.n_seqs;
-  while (hi - lo > 1) {
-    const int step = (hi - lo + 31) / 32, at = lo + lane * step;
-    const bool below = at < hi && __ldg(p.q_start + at) <= token;
-    const int last = max(31 - __clz(__ballot_sync(0xffffffffu, below)), 0);  // (lane 0 is below but for bad tables)
-    lo += last * step;
-    hi = min(lo + step, hi);
-  }
-  return lo;
-}
 __device__ __forceinline__ int position_of(const AttnParams& p, int token) {
   const Entry en = sequence(p, sequence_of(p, token));
   return en.len - en.nq + token - en.tok0;
 }
 
 // The plan, by all WARPS * 32 threads of a block: cum_t[e], cum_i[e] = key tiles and items of a KV head before entry
-// e, head[] = the scalars. A block's share is a multiple of UNIT tiles.
-template <int R, int KT, int WARPS, int UNIT>
-__device__ void make_plan(const AttnParams& p, int* cum_t, int* cum_i, int* head) {
+// e, head[] = the scalars.
+template <int R, int KT, int WARPS>
+__device__ void make_plan(const AttnParams& p, int workers, int* cum_t, int* cum_i, int* head) {
   __shared__ int w_v[4][WARPS];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, E = entries(p);
   if (p.list.all) {  // what the queries see of the shared keys: any of them, and all of them
@@ -194,6 +184,7 @@ __device__ void make_plan(const AttnParams& p, int* cum_t, int* cum_i, int* head
   const int run = (E + 32 * WARPS - 1) / (32 * WARPS);
   const int e0 = min(tid * run, E), e1 = min(e0 + run, E);
   int st = 0, si = 0;
+#pragma unroll 1
   for (int pass = 0; pass < 2; ++pass) {
     int at = 0, ai = 0;
     if (pass == 1) {  // exclusive prefix over the threads
@@ -231,13 +222,22 @@ __device__ void make_plan(const AttnParams& p, int* cum_t, int* cum_i, int* head
     for (int w = 0; w < WARPS; ++w) t += w_v[0][w], i += w_v[1][w];
     cum_t[E] = t, cum_i[E] = i;
     head[kTotal] = t, head[kItems] = i;
-    const int64_t per = ((int64_t)t * p.n_kv + gridDim.x - 1) / gridDim.x;
-    head[kPer] = (int)min((per + UNIT - 1) / UNIT * UNIT, (int64_t)INT32_MAX);
+    head[kPer] = (int)min(((int64_t)t * p.n_kv + workers - 1) / workers, (int64_t)INT32_MAX);
   }
   __syncthreads();
-  if (blockIdx.x == 0) {
-    for (int i = tid; i < kPlanHead; i += 32 * WARPS) p.list.plan[i] = head[i];
-    for (int i = tid; i <= E; i += 32 * WARPS) p.list.plan[kPlanHead + i] = cum_t[i], p.list.plan[kPlanHead + E + 1 + i] = cum_i[i];
+  if (blockIdx.x != 0) return;
+  // for the joining kernel: the scalars, and every item
+  for (int i = tid; i < kPlanHead; i += 32 * WARPS) p.list.plan[i] = head[i];
+  for (int e = tid; e < E; e += 32 * WARPS) {
+    const Entry en = entry_of(p, e);
+    int at = cum_t[e], i = cum_i[e], t0, n;
+    for (int rt = 0; i < cum_i[e + 1]; ++rt, ++i, at += n) {
+      key_tiles<R, KT>(p, en, rt, head, t0, n);
+      if (i < p.list.max_items)
+        p.list.items[i] = make_int4(en.tok0, rt * 256 + min(R, en.nq * p.G - rt * R), at, n);
+      else
+        report(p.status, JAB_ERR_INVALID_ARG);
+    }
   }
 }
 
@@ -246,7 +246,7 @@ struct Item {
   Entry en;
   int h, e, rt;     // KV head, entry, row tile
   int t0, n;        // its first key tile and their number
-  int s0, s1;       // the part of them, counted from t0, that is this block's
+  int s0, s1;       // the part of them, counted from t0, that is this worker's
   int rows;         // rows of the tile in use
 };
 template <int R, int KT>
@@ -275,10 +275,10 @@ __device__ __forceinline__ Item item_at(const AttnParams& p, const int* cum_t, c
   return it;
 }
 
-// Where a part goes. With shared keys every item leaves a part (block + item counts up along the list); without, only
-// the first and the last of a block can be cut.
-__device__ __forceinline__ int64_t slot_of(const AttnParams& p, int block, int item, bool first) {
-  return p.shared > 0 ? (int64_t)block + item : 2 * (int64_t)block + (first ? 0 : 1);
+// Where a part goes. With shared keys every item leaves a part (worker + item counts up along the list); without,
+// only the first and the last of a worker can be cut.
+__device__ __forceinline__ int64_t slot_of(const AttnParams& p, int worker, int item, bool first) {
+  return p.shared > 0 ? (int64_t)worker + item : 2 * (int64_t)worker + (first ? 0 : 1);
 }
 
 // 2^(a - b) with 2^(-inf - -inf) = 0.

@@ -250,7 +250,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
   tc::fence_after_sync();
   const uint32_t tmem = __shfl_sync(0xffffffffu, bars->tmem_base, 0);
   stream_order();
-  make_plan<R, KT, THREADS / 32, 1>(p, cum_t, cum_i, head);
+  make_plan<R, KT, THREADS / 32>(p, gridDim.x, cum_t, cum_i, head);
   const int64_t all = (int64_t)head[kTotal] * p.n_kv;
   const int64_t x0 = (int64_t)blockIdx.x * head[kPer], x1 = min(all, x0 + head[kPer]);
   // Every role walks the block's items; j counts key tiles and i items over all of them.
