@@ -310,32 +310,36 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
         for (int k = max(0, j - KST); k < j; ++k) drain_wait(&bars->rk_full[k % KST], (k / KST) & 1);
         for (int k = max(0, j - VST); k < j; ++k) drain_wait(&bars->rv_full[k % VST], (k / VST) & 1);
       }
-    } else if (warp == 1 && tc::elect_one()) {  // ---------------- S
+    } else if (warp == 1) {  // ---------------- S (the whole warp waits, one thread issues: see the projection's kernel)
       constexpr uint32_t IDESC = tc::idesc_f16(false, R, KT);
       int j = 0, i = 0;
       bool ok = true;
       for (int64_t x = x0; x < x1 && ok; ++i) {
         const Item it = item_at<R, KT>(p, cum_t, head, x, x1);
-        ok = tc::mbar_wait(&bars->q_full[i & 1], (i >> 1) & 1, abort, p.status);
+        ok = __all_sync(0xffffffffu, tc::mbar_wait(&bars->q_full[i & 1], (i >> 1) & 1, abort, p.status));
         for (int s = it.s0; s < it.s1 && ok; ++s, ++j) {
-          ok = tc::mbar_wait(&bars->k_full[j & 1], (j >> 1) & 1, abort, p.status) &&
-               tc::mbar_wait(&bars->s_empty[j & 1], ((j >> 1) & 1) ^ 1, abort, p.status);
-          if (!ok) break;
-          tc::fence_after_sync();
-          const uint64_t kd = tc::sdesc_kmajor_sw128(tc::smem_u32(smem + L::K_OFF + (j & 1) * L::TILE));
+          ok = __all_sync(0xffffffffu, tc::mbar_wait(&bars->k_full[j & 1], (j >> 1) & 1, abort, p.status) &&
+                                           tc::mbar_wait(&bars->s_empty[j & 1], ((j >> 1) & 1) ^ 1, abort, p.status));
+          if (ok && tc::elect_one()) {
+            tc::fence_after_sync();
+            const uint64_t kd = tc::sdesc_kmajor_sw128(tc::smem_u32(smem + L::K_OFF + (j & 1) * L::TILE));
 #pragma unroll
-          for (int k = 0; k < DH / 16; ++k)
-            tc::umma_f16_ts(tmem + L::S_COL + (j & 1) * KT, tmem + L::Q_COL + k * 8, tc::sdesc_advance(kd, (k >> 2) * L::CHUNK + (k & 3) * 32), IDESC,
-                            k > 0 ? 1u : 0u);
-          tc::umma_commit(&bars->s_full[j & 1]);
-          tc::umma_commit(&bars->k_empty[j & 1]);
+            for (int k = 0; k < DH / 16; ++k)
+              tc::umma_f16_ts(tmem + L::S_COL + (j & 1) * KT, tmem + L::Q_COL + k * 8, tc::sdesc_advance(kd, (k >> 2) * L::CHUNK + (k & 3) * 32), IDESC,
+                              k > 0 ? 1u : 0u);
+            tc::umma_commit(&bars->s_full[j & 1]);
+            tc::umma_commit(&bars->k_empty[j & 1]);
+            if (s + 1 == it.s1) tc::umma_commit(&bars->q_empty);
+          }
+          __syncwarp();
         }
-        if (ok) tc::umma_commit(&bars->q_empty);
         x += it.s1 - it.s0;
       }
-      tc::umma_commit(&bars->drain[0]);
-      drain_wait(&bars->drain[0], 0);
-    } else if (warp == 2 && tc::elect_one()) {  // ---------------- P V
+      if (tc::elect_one()) {
+        tc::umma_commit(&bars->drain[0]);
+        drain_wait(&bars->drain[0], 0);
+      }
+    } else if (warp == 2) {  // ---------------- P V
       constexpr uint32_t IDESC = tc::idesc_f16(false, R, DH) | (1u << 16);  // B MN-major
       int j = 0, i = 0;
       bool ok = true;
@@ -343,32 +347,37 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
         const Item it = item_at<R, KT>(p, cum_t, head, x, x1);
         int all_lo, all_hi;
         seen_by_all(p, it.en, it.rt * R, it.rt * R + it.rows, head, all_lo, all_hi);
-        ok = tc::mbar_wait(&bars->o_empty, (i & 1) ^ 1, abort, p.status);
+        ok = __all_sync(0xffffffffu, tc::mbar_wait(&bars->o_empty, (i & 1) ^ 1, abort, p.status));
         for (int s = it.s0; s < it.s1 && ok; ++s, ++j) {
-          ok = tc::mbar_wait(&bars->v_full[j & 1], (j >> 1) & 1, abort, p.status) && tc::mbar_wait(&bars->p_full, j & 1, abort, p.status);
-          if (!ok) break;
-          tc::fence_after_sync();
-          const uint64_t vd = tc::sdesc_mnmajor_sw128(tc::smem_u32(smem + L::V_OFF + (j & 1) * L::TILE), L::CHUNK, 1024);
-          const int key0 = (it.t0 + s) * KT;
-          const bool masked = key0 < all_lo || key0 + KT > all_hi;
-#pragma unroll
-          for (int k = 0; k < KT / 16; ++k)
-            tc::umma_f16_ts(tmem + L::O_COL, tmem + L::S_COL + (j & 1) * KT + k * 8, tc::sdesc_advance(vd, k * 16 * 128), IDESC,
-                            s > it.s0 || k > 0 ? 1u : 0u);
-          if (masked) {
+          ok = __all_sync(0xffffffffu, tc::mbar_wait(&bars->v_full[j & 1], (j >> 1) & 1, abort, p.status) &&
+                                           tc::mbar_wait(&bars->p_full, j & 1, abort, p.status));
+          if (ok && tc::elect_one()) {
+            tc::fence_after_sync();
+            const uint64_t vd = tc::sdesc_mnmajor_sw128(tc::smem_u32(smem + L::V_OFF + (j & 1) * L::TILE), L::CHUNK, 1024);
+            const int key0 = (it.t0 + s) * KT;
+            const bool masked = key0 < all_lo || key0 + KT > all_hi;
 #pragma unroll
             for (int k = 0; k < KT / 16; ++k)
-              tc::umma_f16_ts(tmem + L::O_COL, tmem + L::LO_COL + k * 8, tc::sdesc_advance(vd, k * 16 * 128), IDESC, 1u);
+              tc::umma_f16_ts(tmem + L::O_COL, tmem + L::S_COL + (j & 1) * KT + k * 8, tc::sdesc_advance(vd, k * 16 * 128), IDESC,
+                              s > it.s0 || k > 0 ? 1u : 0u);
+            if (masked) {
+#pragma unroll
+              for (int k = 0; k < KT / 16; ++k)
+                tc::umma_f16_ts(tmem + L::O_COL, tmem + L::LO_COL + k * 8, tc::sdesc_advance(vd, k * 16 * 128), IDESC, 1u);
+            }
+            tc::umma_commit(&bars->pv_done);
+            tc::umma_commit(&bars->s_empty[j & 1]);
+            tc::umma_commit(&bars->v_empty[j & 1]);
+            if (s + 1 == it.s1) tc::umma_commit(&bars->o_full);
           }
-          tc::umma_commit(&bars->pv_done);
-          tc::umma_commit(&bars->s_empty[j & 1]);
-          tc::umma_commit(&bars->v_empty[j & 1]);
+          __syncwarp();
         }
-        if (ok) tc::umma_commit(&bars->o_full);
         x += it.s1 - it.s0;
       }
-      tc::umma_commit(&bars->drain[1]);
-      drain_wait(&bars->drain[1], 0);
+      if (tc::elect_one()) {
+        tc::umma_commit(&bars->drain[1]);
+        drain_wait(&bars->drain[1], 0);
+      }
     }
   } else if (warp < 12) {  // ---------------- softmax
     more_registers<128>();

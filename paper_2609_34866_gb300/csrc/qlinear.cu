@@ -7,16 +7,14 @@
 // 1024 < 2^24, and 128^2 * 1024 = 2^24). The accumulator is therefore read out every 1024 of K and added up in
 // int32: the sum is exact, in any order of its parts, at the fp16 rate of the tensor cores.
 //
-// Two launches: the rows of X become codes (held in fp16, the operand's type) and scales; then a persistent
-// kernel with the output channels on the accumulator's 128 lanes and the tokens on its columns. The weights
-// travel as the bytes that they are: TMA brings a 128 x 64 tile of codes to shared memory, converter warps
-// turn it into fp16 in tensor memory (a byte under the exponent of 1024, less 1152), and the products take
-// it from there as their A operand. One layout serves one token and thousands: what changes with M is the
-// number of columns and the K range of a unit.
-//   warp 0        TMA producer
-//   warp 1        tensor memory owner, issues the products
-//   warps 4..7    epilogue: accumulators to int32 sums in registers, scaling, output
-//   warps 8..15   converters, two groups that take K blocks in turn
+// Two launches: the rows of X become codes (held in fp16, the operand's type) and scales; then the product, with the output
+// channels on the accumulator's 128 lanes and the tokens on its columns. The weights travel as the bytes that they
+// are: TMA brings a 128 x 64 tile of codes to shared memory, converter warps turn it into fp16 in tensor memory (a
+// byte under the exponent of 1024, less 1152), and the products take it from there as their A operand. One layout
+// serves one token and thousands; the product is one of two kernels:
+//   few tiles   one tile a block, K split over a cluster whose blocks add their sums through shared memory; all
+//               accumulators of a block (1024 of K each) stay in tensor memory to the end
+//   many tiles  persistent blocks, two accumulators in turn, sums in registers
 #include <cudaTypedefs.h>
 
 #include <algorithm>
@@ -41,8 +39,6 @@ struct TokenParams {
   int K, Kp;
   half_t* xh;     // [M, Kp]
   float* sx;      // [M]
-  int* zero;      // the product's partial sums and counters, to 0
-  int64_t n_zero;
   int* status;
 };
 
@@ -60,6 +56,26 @@ __device__ __forceinline__ void unpack8(const uint4& u, float (&v)[8]) {
   }
 }
 
+// Scale of a row whose largest magnitude has the bits `big`; NaN where that is an infinity or a NaN.
+template <class T>
+__device__ __forceinline__ float row_scale(uint32_t big) {
+  constexpr bool HALF = std::is_same<T, half_t>::value;
+  const float a = HALF ? __half2float(__ushort_as_half((unsigned short)big)) : __uint_as_float(big << 16);
+  return big < (HALF ? kHalfInf : kBf16Inf) ? __fdiv_rn(a, 127.f) : __uint_as_float(0x7fc00000u);
+}
+// Codes of 8 elements as fp16; 0 where the scale is 0 or NaN.
+template <class T>
+__device__ __forceinline__ uint4 row_codes(const uint4& u, float s) {
+  float v[8];
+  unpack8<T>(u, v);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float r = fminf(fmaxf(rintf(__fdiv_rn(v[j], s)), -127.f), 127.f);
+    v[j] = s > 0.f ? r : 0.f;
+  }
+  return make_uint4(tc::pack_half2(v[0], v[1]), tc::pack_half2(v[2], v[3]), tc::pack_half2(v[4], v[5]), tc::pack_half2(v[6], v[7]));
+}
+
 // A block per row; the row's first KEEP chunks of 8 elements a thread stay in registers between the maximum and
 // the codes, what is longer is read again.
 template <class T>
@@ -68,7 +84,6 @@ __global__ void __launch_bounds__(256) quantize_tokens_kernel(const __grid_const
   __shared__ uint32_t top[8];
   stream_order();
   const int tid = threadIdx.x, n8 = p.K / 8, n8p = p.Kp / 8;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + tid; i < p.n_zero; i += (int64_t)gridDim.x * 256) p.zero[i] = 0;
   for (int64_t m = blockIdx.x; m < p.M; m += gridDim.x) {
     const uint4* row = reinterpret_cast<const uint4*>(static_cast<const T*>(p.x) + m * p.ldx);
     uint4 keep[KEEP];
@@ -90,28 +105,16 @@ __global__ void __launch_bounds__(256) quantize_tokens_kernel(const __grid_const
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < 8; ++w) big = max(big, top[w]);
-    const bool fine = big < (std::is_same<T, half_t>::value ? kHalfInf : kBf16Inf);
-    const float a = std::is_same<T, half_t>::value ? __half2float(__ushort_as_half((unsigned short)big)) : __uint_as_float(big << 16);
-    const float s = fine ? __fdiv_rn(a, 127.f) : __uint_as_float(0x7fc00000u);
+    const float s = row_scale<T>(big);
     if (tid == 0) {
       p.sx[m] = s;
-      if (!fine) report(p.status, JAB_ERR_NONFINITE);
+      if (!(s >= 0.f)) report(p.status, JAB_ERR_NONFINITE);
     }
     uint4* out = reinterpret_cast<uint4*>(p.xh + m * p.Kp);
-    auto put = [&](int i, const uint4& u) {
-      float v[8];
-      unpack8<T>(u, v);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float r = fminf(fmaxf(rintf(__fdiv_rn(v[j], s)), -127.f), 127.f);
-        v[j] = fine && s > 0.f ? r : 0.f;
-      }
-      out[i] = make_uint4(tc::pack_half2(v[0], v[1]), tc::pack_half2(v[2], v[3]), tc::pack_half2(v[4], v[5]), tc::pack_half2(v[6], v[7]));
-    };
 #pragma unroll
     for (int c = 0; c < KEEP; ++c)
-      if (c * 256 + tid < n8) put(c * 256 + tid, keep[c]);
-    for (int i = KEEP * 256 + tid; i < n8; i += 256) put(i, __ldg(row + i));
+      if (c * 256 + tid < n8) out[c * 256 + tid] = row_codes<T>(keep[c], s);
+    for (int i = KEEP * 256 + tid; i < n8; i += 256) out[i] = row_codes<T>(__ldg(row + i), s);
     for (int i = n8 + tid; i < n8p; i += 256) out[i] = make_uint4(0u, 0u, 0u, 0u);
   }
 }
@@ -119,12 +122,10 @@ __global__ void __launch_bounds__(256) quantize_tokens_kernel(const __grid_const
 // ------------------------------------------------------------------ the product
 struct LinParams {
   int64_t M, ldy;
-  int N, k_blocks, tiles_n, tiles_m, splits;
-  FastDiv by_tiles, by_n;
+  int N, k_blocks, tiles_n, tiles_m;
+  FastDiv by_n;
   const float *sx, *sw;
   void* y;
-  int* part;      // int32 [M, N], zeroed (splits > 1)
-  int* counters;  // [tiles, 4], zeroed (splits > 1)
   int* status;
 };
 
@@ -148,14 +149,6 @@ __device__ __forceinline__ void drain_wait(uint64_t* bar, uint32_t parity) {
   const uint64_t t0 = tc::globaltimer();
   while (!tc::mbar_test(bar, parity))
     if (tc::globaltimer() - t0 > tc::kWaitLimitNs) break;
-}
-
-__device__ __forceinline__ void unit_of(const LinParams& p, int unit, int& nt, int& mt, int& kb0, int& kb1) {
-  int ks, t;
-  p.by_tiles.divmod(unit, ks, t);
-  p.by_n.divmod(t, mt, nt);
-  kb0 = (int)((int64_t)p.k_blocks * ks / p.splits);
-  kb1 = (int)((int64_t)p.k_blocks * (ks + 1) / p.splits);
 }
 
 template <class T>
@@ -195,7 +188,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   uint8_t* x_smem = smem + WST * W_BYTES;
   Bars* bars = reinterpret_cast<Bars*>(x_smem + AST * XB);
   const int warp = tc::warp_index(), lane = threadIdx.x & 31;
-  const int total = p.tiles_n * p.tiles_m * p.splits;
+  const int total = p.tiles_n * p.tiles_m;
   volatile int* abort = &bars->abort;
   if (threadIdx.x == 0) {
     for (int s = 0; s < WST; ++s) {
@@ -233,9 +226,9 @@ __global__ void __launch_bounds__(THREADS, 1)
       int i = 0;
       bool ok = true;
       for (int unit = blockIdx.x; unit < total && ok; unit += gridDim.x) {
-        int nt, mt, kb0, kb1;
-        unit_of(p, unit, nt, mt, kb0, kb1);
-        for (int kb = kb0; kb < kb1; ++kb, ++i) {
+        int nt, mt;
+        p.by_n.divmod(unit, mt, nt);
+        for (int kb = 0; kb < p.k_blocks; ++kb, ++i) {
           const int ws = i % WST, xs = i % AST;
           if (!tc::mbar_wait(&bars->wempty[ws], ((i / WST) & 1) ^ 1, abort, p.status)) { ok = false; break; }
           tc::mbar_expect_tx(&bars->wfull[ws], W_BYTES);
@@ -253,36 +246,38 @@ __global__ void __launch_bounds__(THREADS, 1)
         for (int j = max(0, i - WST); j < i; ++j) drain_wait(&bars->wfull[j % WST], (j / WST) & 1);
         for (int j = max(0, i - AST); j < i; ++j) drain_wait(&bars->xfull[j % AST], (j / AST) & 1);
       }
-    } else if (warp == 1 && tc::elect_one()) {  // ---------------- products
+    } else if (warp == 1) {  // ---------------- products
+      // The whole warp waits, one thread issues: behind a wait of its own a single thread issued four products in 450
+      // clocks (the compiler no longer knows it to be alone and loops over every operand), this way in 210; they take 256.
       constexpr uint32_t IDESC = tc::idesc_f16(false, TM, NTOK);
       int i = 0, d = 0;
       bool ok = true;
       for (int unit = blockIdx.x; unit < total && ok; unit += gridDim.x) {
-        int nt, mt, kb0, kb1;
-        unit_of(p, unit, nt, mt, kb0, kb1);
-        for (int c0 = kb0; c0 < kb1 && ok; c0 += kExactBlocks, ++d) {
-          if (!tc::mbar_wait(&bars->tempty[d & 1], ((d >> 1) & 1) ^ 1, abort, p.status)) { ok = false; break; }
-          const int c1 = min(c0 + kExactBlocks, kb1);
-          for (int kb = c0; kb < c1; ++kb, ++i) {
+        for (int c0 = 0; c0 < p.k_blocks && ok; c0 += kExactBlocks, ++d) {
+          ok = __all_sync(0xffffffffu, tc::mbar_wait(&bars->tempty[d & 1], ((d >> 1) & 1) ^ 1, abort, p.status));
+          const int n = min(kExactBlocks, p.k_blocks - c0);
+          for (int b = 0; b < n && ok; ++b, ++i) {
             const int s = i % AST;
-            if (!tc::mbar_wait(&bars->xfull[s], (i / AST) & 1, abort, p.status) ||
-                !tc::mbar_wait(&bars->afull[s], (i / AST) & 1, abort, p.status)) {
-              ok = false;
-              break;
-            }
-            tc::fence_after_sync();
-            const uint64_t xd = tc::sdesc_kmajor_sw128(tc::smem_u32(x_smem + s * XB));
+            ok = __all_sync(0xffffffffu, tc::mbar_wait(&bars->xfull[s], (i / AST) & 1, abort, p.status) &&
+                                             tc::mbar_wait(&bars->afull[s], (i / AST) & 1, abort, p.status));
+            if (ok && tc::elect_one()) {
+              tc::fence_after_sync();
+              const uint64_t xd = tc::sdesc_kmajor_sw128(tc::smem_u32(x_smem + s * XB));
 #pragma unroll
-            for (int k = 0; k < BK / 16; ++k)
-              tc::umma_f16_ts(tmem + (d & 1) * C::D_COLS, tmem + A_COL + s * 32 + k * 8, tc::sdesc_advance(xd, k * 32),
-                              IDESC, kb > c0 || k > 0 ? 1u : 0u);
-            tc::umma_commit(&bars->empty[s]);
+              for (int k = 0; k < BK / 16; ++k)
+                tc::umma_f16_ts(tmem + (d & 1) * C::D_COLS, tmem + A_COL + s * 32 + k * 8, tc::sdesc_advance(xd, k * 32), IDESC,
+                                b > 0 || k > 0 ? 1u : 0u);
+              tc::umma_commit(&bars->empty[s]);
+              if (b + 1 == n) tc::umma_commit(&bars->tfull[d & 1]);
+            }
+            __syncwarp();
           }
-          if (ok) tc::umma_commit(&bars->tfull[d & 1]);
         }
       }
-      tc::umma_commit(&bars->drain);
-      drain_wait(&bars->drain, 0);
+      if (tc::elect_one()) {
+        tc::umma_commit(&bars->drain);
+        drain_wait(&bars->drain, 0);
+      }
     }
   } else if (warp < 8) {  // ---------------- epilogue
     more_registers<216>();
@@ -290,12 +285,12 @@ __global__ void __launch_bounds__(THREADS, 1)
     int d = 0;
     bool ok = true;
     for (int unit = blockIdx.x; unit < total && ok; unit += gridDim.x) {
-      int nt, mt, kb0, kb1;
-      unit_of(p, unit, nt, mt, kb0, kb1);
+      int nt, mt;
+      p.by_n.divmod(unit, mt, nt);
       int acc[NTOK];
 #pragma unroll
       for (int c = 0; c < NTOK; ++c) acc[c] = 0;
-      for (int c0 = kb0; c0 < kb1; c0 += kExactBlocks, ++d) {
+      for (int c0 = 0; c0 < p.k_blocks; c0 += kExactBlocks, ++d) {
         if (!tc::mbar_wait(&bars->tfull[d & 1], (d >> 1) & 1, abort, p.status)) { ok = false; break; }
         tc::fence_after_sync();
         const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (d & 1) * C::D_COLS;
@@ -316,26 +311,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       const int n = nt * TM + row;
       const int64_t m0 = (int64_t)mt * NTOK;
       const int cols = (int)min((int64_t)NTOK, p.M - m0);
-      bool mine = true;
-      if (p.splits > 1) {  // parts of the sum meet in memory; of the warps of these rows the last scales and stores
-        if (n < p.N) {
-#pragma unroll
-          for (int c = 0; c < NTOK; ++c)
-            if (c < cols) atomicAdd(p.part + (m0 + c) * p.N + n, acc[c]);
-        }
-        __threadfence();
-        __syncwarp();
-        int before = 0;
-        if (lane == 0) before = atomicAdd(p.counters + (mt * p.tiles_n + nt) * 4 + quarter, 1);
-        mine = __shfl_sync(0xffffffffu, before, 0) == p.splits - 1;
-        __threadfence();
-        if (mine && n < p.N) {
-#pragma unroll
-          for (int c = 0; c < NTOK; ++c)
-            if (c < cols) acc[c] = __ldcg(p.part + (m0 + c) * p.N + n);
-        }
-      }
-      if (mine && n < p.N) {
+      if (n < p.N) {
         const float wn = __ldg(p.sw + n);
         T* y = static_cast<T*>(p.y) + m0 * p.ldy + n;
 #pragma unroll
@@ -349,9 +325,9 @@ __global__ void __launch_bounds__(THREADS, 1)
     int i = 0;
     bool ok = true;
     for (int unit = blockIdx.x; unit < total && ok; unit += gridDim.x) {
-      int nt, mt, kb0, kb1;
-      unit_of(p, unit, nt, mt, kb0, kb1);
-      for (int kb = kb0; kb < kb1; ++kb, ++i) {
+      int nt, mt;
+      p.by_n.divmod(unit, mt, nt);
+      for (int kb = 0; kb < p.k_blocks; ++kb, ++i) {
         if ((i & 1) != grp) continue;
         const int ws = i % WST, s = i % AST;
         if (!tc::mbar_wait(&bars->wfull[ws], (i / WST) & 1, abort, p.status)) { ok = false; break; }
@@ -389,6 +365,268 @@ __global__ void __launch_bounds__(THREADS, 1)
   }
 }
 
+// ------------------------------------------------------------------ few tiles
+// Blocks of a cluster take K ranges of one tile. Loads of weights start before the codes of X are there (the weights
+// were not written by the kernel before this one). Converters (16 warps, four groups that take K blocks in turn) become
+// the epilogue: 8 columns at a time, the sums of a range's accumulators go to the shared memory of the block that has
+// those columns, are added there and scaled. Loops over 8 columns rather than unrolled tiles: these calls are a few
+// microseconds, and a cold SM fetches their code (unrolled, with the parts added in global memory: 14 us where the
+// launch with everything in it takes 7, 37 tokens x 2304 x 768).
+// FUSED: up to 16 tokens, whose rows every block quantises for itself (four more warps), its own K range into shared
+// memory: the first launch and its end would be a third of the time.
+constexpr int S_GROUPS = 4, S_THREADS = 32 * (4 + 4 * S_GROUPS), kMaxRanges = 8, kMaxA = 8, kFusedBlocks = 24;
+
+template <int NTOK, bool FUSED>
+struct SCfg {
+  static constexpr int WST = NTOK <= 32 ? 16 : NTOK == 64 ? 10 : 8, XST = FUSED ? kFusedBlocks : NTOK == 128 ? 4 : AST;  // stages of weights and tokens
+  static constexpr int X_BYTES = NTOK * BK * 2;
+  static constexpr int D_COLS = NTOK < 32 ? 32 : NTOK, D_BUFS = NTOK == 128 ? 2 : 4, OCTS = NTOK / 8;
+  static constexpr int SUM_BYTES = (OCTS + kMaxRanges - 1) * 8 * TM * 4;  // >= ranges * ceil(OCTS / ranges) octets
+  static constexpr int SMEM = WST * W_BYTES + XST * X_BYTES + SUM_BYTES + 1024 + 1024;
+};
+static_assert(SCfg<128, false>::SMEM <= 226 * 1024 && SCfg<64, false>::SMEM <= 226 * 1024 && SCfg<32, false>::SMEM <= 226 * 1024 && SCfg<16, true>::SMEM <= 226 * 1024, "shared memory budget");
+
+struct SBars {
+  uint64_t wfull[16], wempty[16], xfull[AST], xempty[AST], afull[kMaxA], aempty[kMaxA], done, xready;
+  uint32_t tmem_base;
+  int abort;
+  float sx[16];
+};
+static_assert(sizeof(SBars) <= 1024, "barrier block");
+
+// 32 lanes x 8 columns.
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&r)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr));
+}
+__device__ __forceinline__ void store_cluster(uint32_t at, int v) { asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(at), "r"(v) : "memory"); }
+
+// Rows of X (up to 16, by 128 threads): scales into sx, codes of K blocks [kb0, kb0 + n_kb) into x_smem.
+template <class T>
+__device__ __forceinline__ void quantize_range(const TokenParams& t, int kb0, int n_kb, uint8_t* x_smem, float* sx, int tid, int warp, int lane) {
+  const int n8 = t.K / 8;
+  // a warp has rows warp, warp + 4, ...
+#pragma unroll 1
+  for (int m = warp; m < t.M; m += 4) {
+    const uint4* row = reinterpret_cast<const uint4*>(static_cast<const T*>(t.x) + m * t.ldx);
+    uint32_t big = 0;
+#pragma unroll 1
+    for (int i0 = lane; i0 < n8; i0 += 32 * 8) {
+      uint4 u[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) u[j] = i0 + 32 * j < n8 ? __ldg(row + i0 + 32 * j) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) big = max_abs_f16x2(max_abs_f16x2(max_abs_f16x2(max_abs_f16x2(big, u[j].x), u[j].y), u[j].z), u[j].w);
+    }
+    big = __reduce_max_sync(0xffffffffu, max(big & 0xffffu, big >> 16));
+    const float s = row_scale<T>(big);
+    if (lane == 0) {
+      sx[m] = s;
+      if (!(s >= 0.f)) report(t.status, JAB_ERR_NONFINITE);
+    }
+#pragma unroll 1
+    for (int i = lane; i < n_kb * 8; i += 32) {
+      const int k8 = kb0 * 8 + i;
+      const uint4 c = k8 < n8 ? row_codes<T>(__ldg(row + k8), s) : make_uint4(0u, 0u, 0u, 0u);
+      *reinterpret_cast<uint4*>(x_smem + (i >> 3) * (16 * BK * 2) + m * 128 + (((i & 7) ^ (m & 7)) << 4)) = c;
+    }
+  }
+}
+
+template <class T, class TX, int NTOK, bool FUSED>
+__global__ void __launch_bounds__(FUSED ? S_THREADS + 128 : S_THREADS, 1)
+    qlinear_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const __grid_constant__ LinParams p,
+                       const __grid_constant__ TokenParams tok, int ranges) {
+  using C = SCfg<NTOK, FUSED>;
+  constexpr int WST = C::WST, XST = C::XST, XB = C::X_BYTES;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* w_smem = smem;
+  uint8_t* x_smem = smem + WST * W_BYTES;
+  int* sums = reinterpret_cast<int*>(x_smem + XST * XB);  // [range, own octet, 8, TM]
+  SBars* bars = reinterpret_cast<SBars*>(x_smem + XST * XB + C::SUM_BYTES);
+  const int warp = tc::warp_index(), lane = threadIdx.x & 31;
+  const int rank = (int)tc::cluster_ctarank(), unit = blockIdx.x / ranges;
+  const int mt = p.by_n.quot(unit), nt = unit - mt * p.tiles_n;
+  const int kb0 = p.k_blocks * rank / ranges, n_kb = p.k_blocks * (rank + 1) / ranges - kb0;
+  // The four products of a K block go to D_BUFS accumulators in turn; A takes the columns behind them
+  constexpr uint32_t a_col = C::D_BUFS * C::D_COLS;
+  constexpr int na = kMaxA;
+  static_assert(a_col + na * 32 <= 512, "tensor memory");
+  volatile int* abort = &bars->abort;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < WST; ++s) {
+      tc::mbar_init(&bars->wfull[s], 1);
+      tc::mbar_init(&bars->wempty[s], 4);
+    }
+    for (int s = 0; s < AST; ++s) {
+      tc::mbar_init(&bars->xfull[s], 1);
+      tc::mbar_init(&bars->xempty[s], 1);
+    }
+    for (int s = 0; s < kMaxA; ++s) {
+      tc::mbar_init(&bars->afull[s], 4);
+      tc::mbar_init(&bars->aempty[s], 1);
+    }
+    tc::mbar_init(&bars->done, 1);
+    tc::mbar_init(&bars->xready, 4);
+    bars->abort = 0;
+    tc::fence_mbar_init();
+    if (FUSED) stream_order();  // (weights too may have been written by the kernel before)
+    for (int i = 0; i < min(WST, n_kb); ++i) {
+      tc::mbar_expect_tx(&bars->wfull[i], W_BYTES);
+      tc::tma_load_2d(w_smem + i * W_BYTES, &tmW, &bars->wfull[i], (kb0 + i) * BK, nt * TM);
+    }
+  }
+  if (warp == 1) {
+    tc::tmem_alloc(&bars->tmem_base, 512);
+    tc::tmem_relinquish();
+  }
+  tc::fence_before_sync();
+  __syncthreads();
+  tc::fence_after_sync();
+  const uint32_t tmem = __shfl_sync(0xffffffffu, bars->tmem_base, 0);
+  stream_order();
+
+  if (warp == 0) {
+    if (tc::elect_one()) {  // ---------------- TMA producer
+      int w_next = min(WST, n_kb), i = 0;
+      for (; i < n_kb; ++i) {
+        if (!FUSED) {
+          const int xs = i % XST;
+          if (!tc::mbar_wait(&bars->xempty[xs], ((i / XST) & 1) ^ 1, abort, p.status)) break;
+          tc::mbar_expect_tx(&bars->xfull[xs], XB);
+          tc::tma_load_2d(x_smem + xs * XB, &tmX, &bars->xfull[xs], (kb0 + i) * BK, mt * NTOK);
+        }
+        if (w_next < n_kb && w_next < i + WST) {
+          const int ws = w_next % WST;
+          if (!tc::mbar_wait(&bars->wempty[ws], ((w_next / WST) & 1) ^ 1, abort, p.status)) {
+            ++i;
+            break;
+          }
+          tc::mbar_expect_tx(&bars->wfull[ws], W_BYTES);
+          tc::tma_load_2d(w_smem + ws * W_BYTES, &tmW, &bars->wfull[ws], (kb0 + w_next) * BK, nt * TM);
+          ++w_next;
+        }
+      }
+      if (*abort) {  // every copy issued has landed before shared memory goes to another block
+        for (int j = max(0, w_next - WST); j < w_next; ++j) drain_wait(&bars->wfull[j % WST], (j / WST) & 1);
+        if (!FUSED)
+          for (int j = max(0, i - XST); j < i; ++j) drain_wait(&bars->xfull[j % XST], (j / XST) & 1);
+      }
+    }
+  } else if (warp == 1) {  // ---------------- products (the whole warp waits, as below)
+    constexpr uint32_t IDESC = tc::idesc_f16(false, TM, NTOK);
+    bool ok = !FUSED || __all_sync(0xffffffffu, tc::mbar_wait(&bars->xready, 0, abort, p.status));
+    for (int i = 0; i < n_kb && ok; ++i) {
+      const int s = i % na, xs = i % XST;
+      ok = __all_sync(0xffffffffu, (FUSED || tc::mbar_wait(&bars->xfull[xs], (i / XST) & 1, abort, p.status)) &&
+                                       tc::mbar_wait(&bars->afull[s], (i / na) & 1, abort, p.status));
+      if (ok && tc::elect_one()) {
+        tc::fence_after_sync();
+        const uint64_t xd = tc::sdesc_kmajor_sw128(tc::smem_u32(x_smem + xs * XB));
+#pragma unroll
+        for (int k = 0; k < BK / 16; ++k)
+          tc::umma_f16_ts(tmem + k % C::D_BUFS * C::D_COLS, tmem + a_col + s * 32 + k * 8, tc::sdesc_advance(xd, k * 32), IDESC,
+                          i > 0 || k >= C::D_BUFS ? 1u : 0u);
+        tc::umma_commit(&bars->aempty[s]);
+        if (!FUSED) tc::umma_commit(&bars->xempty[xs]);
+      }
+      __syncwarp();
+    }
+    if (tc::elect_one()) {
+      tc::umma_commit(&bars->done);
+      drain_wait(&bars->done, 0);
+    }
+  } else if (FUSED && warp >= 4 + 4 * S_GROUPS) {  // ---------------- tokens
+    quantize_range<TX>(tok, kb0, n_kb, x_smem, bars->sx, threadIdx.x - S_THREADS, warp - 4 - 4 * S_GROUPS, lane);
+    tc::fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) tc::mbar_arrive(&bars->xready);
+  } else if (warp >= 4) {  // ---------------- converters, then epilogue
+    const int quarter = warp & 3, grp = (warp - 4) >> 2, row = quarter * 32 + lane;
+    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+    bool ok = true;
+    for (int i = grp; i < n_kb && ok; i += S_GROUPS) {
+      const int ws = i % WST, s = i % na;
+      if (!(ok = tc::mbar_wait(&bars->wfull[ws], (i / WST) & 1, abort, p.status))) break;
+      const uint4* src = reinterpret_cast<const uint4*>(w_smem + ws * W_BYTES + row * BK);
+      uint4 v[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) v[c] = src[c ^ ((row >> 1) & 3)];  // TMA's 64-byte swizzle
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(&bars->wempty[ws]);
+      uint32_t a[32];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        codes_h2(v[c].x, a[8 * c], a[8 * c + 1]);
+        codes_h2(v[c].y, a[8 * c + 2], a[8 * c + 3]);
+        codes_h2(v[c].z, a[8 * c + 4], a[8 * c + 5]);
+        codes_h2(v[c].w, a[8 * c + 6], a[8 * c + 7]);
+      }
+      if (!(ok = tc::mbar_wait(&bars->aempty[s], ((i / na) & 1) ^ 1, abort, p.status))) break;
+      tc::fence_after_sync();
+      __syncwarp();
+      tc::tmem_st32(tmem + lanes + a_col + s * 32, a);
+      tc::tmem_st_wait();
+      tc::fence_before_sync();
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(&bars->afull[s]);
+    }
+    ok = ok && tc::mbar_wait(&bars->done, 0, abort, p.status);
+    tc::fence_after_sync();
+    const int own = (C::OCTS + ranges - 1) / ranges;
+#pragma unroll 1
+    for (int oct = grp; oct < C::OCTS && ok && (int64_t)mt * NTOK + oct * 8 < p.M; oct += S_GROUPS) {
+      int acc[8] = {};
+#pragma unroll 1
+      for (int b = 0; b < C::D_BUFS; ++b) {
+        uint32_t v[8];
+        __syncwarp();
+        tmem_ld8(tmem + lanes + b * C::D_COLS + oct * 8, v);
+        tc::tmem_ld_wait();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] += __float2int_rn(__uint_as_float(v[j]));
+      }
+      // to the block that has these columns
+      const int place = oct / ranges, owner = oct - place * ranges;
+      const uint32_t at = tc::mapa_shared(tc::smem_u32(sums + ((rank * own + place) * 8) * TM + row), owner);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) store_cluster(at + j * TM * 4, acc[j]);
+    }
+  }
+  tc::fence_before_sync();
+  __syncwarp();
+  tc::cluster_sync();  // every block's sums are where they belong
+  tc::fence_after_sync();
+  if (warp >= 4 && warp < 4 + 4 * S_GROUPS) {
+    const int quarter = warp & 3, grp = (warp - 4) >> 2, row = quarter * 32 + lane, n = nt * TM + row;
+    const int own = (C::OCTS + ranges - 1) / ranges;
+    const float wn = n < p.N ? __ldg(p.sw + n) : 0.f;
+#pragma unroll 1
+    for (int place = grp; place < own; place += S_GROUPS) {
+      const int oct = place * ranges + rank;
+      const int64_t m0 = (int64_t)mt * NTOK + oct * 8;
+      if (oct >= C::OCTS || m0 >= p.M) break;
+      int acc[8] = {};
+#pragma unroll 1
+      for (int q = 0; q < ranges; ++q)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] += sums[((q * own + place) * 8 + j) * TM + row];
+      if (n >= p.N) continue;
+      T* y = static_cast<T*>(p.y) + m0 * p.ldy + n;
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (m0 + j < p.M) y[j * p.ldy] = out_as<T>(__fmul_rn(__fmul_rn((float)acc[j], FUSED ? bars->sx[m0 + j] : __ldcg(p.sx + m0 + j)), wn));
+    }
+  }
+  __syncthreads();
+  if (warp == 1) {
+    __syncwarp();
+    tc::tmem_dealloc(tmem, 512);
+  }
+}
+
 // ------------------------------------------------------------------ host side
 PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
   static PFN_cuTensorMapEncodeTiled_v12000 fn = [] {
@@ -415,42 +653,116 @@ bool make_map(CUtensorMap* m, CUtensorMapDataType type, const void* base, uint64
 // Tokens of a tile: the smallest that holds them all, 128 at most.
 int tile_tokens(int64_t M) { return M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128; }
 
-constexpr int kMaxSplitTiles = 256;  // tiles that a split K is worth while for (fewer than the SMs)
-
 struct Scratch {
-  size_t sx, zero, xh, total;
-  int64_t parts;  // int32 of partial sums that may be needed
+  size_t sx, xh, total;
 };
 Scratch plan_scratch(int64_t M, int N, int K) {
   const int64_t Kp = (K + 63) / 64 * 64;
-  const int64_t tiles = (N + TM - 1) / TM * ((M + tile_tokens(M) - 1) / tile_tokens(M));
   Scratch s;
-  s.parts = tiles <= kMaxSplitTiles ? M * N : 0;
   s.sx = 0;
-  s.zero = ((size_t)M * 4 + 255) / 256 * 256;
-  s.xh = s.zero + ((size_t)(4 * kMaxSplitTiles + s.parts) * 4 + 255) / 256 * 256;
+  s.xh = ((size_t)M * 4 + 255) / 256 * 256;
   s.total = s.xh + (size_t)M * Kp * 2;
   return s;
 }
 
-template <class T, int NTOK>
-cudaError_t launch_as(const CUtensorMap& tw, const CUtensorMap& tx, const LinParams& p, int sms, cudaStream_t st) {
-  auto kern = qlinear_kernel<T, NTOK>;
+// K ranges of the few-tiles kernel: as many as leave no cluster waiting for another to end; 0: the other kernel's case.
+template <class C, class Kernel>
+int ranges_of(Kernel kern, int threads, const LinParams& p, int sms, int (&fit)[kMaxRanges + 1]) {
+  const int64_t tiles = (int64_t)p.tiles_n * p.tiles_m;
+  if (tiles > sms) return 0;
+  for (int s = (int)std::min<int64_t>({kMaxRanges, sms / tiles, std::max(1, p.k_blocks / 2)}); s >= 1; --s) {
+    if ((p.k_blocks + s - 1) / s > kExactBlocks * C::D_BUFS) continue;  // (1024 products an accumulator)
+    if (fit[s] == 0) {  // clusters of that many blocks that are resident at once
+      cudaLaunchConfig_t cfg = {};
+      cudaLaunchAttribute at[1];
+      at[0].id = cudaLaunchAttributeClusterDimension;
+      at[0].val.clusterDim.x = s;
+      at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+      cfg.gridDim = dim3((unsigned)(sms / s * s));
+      cfg.blockDim = dim3(threads);
+      cfg.dynamicSmemBytes = C::SMEM;
+      cfg.attrs = at;
+      cfg.numAttrs = 1;
+      int n = 0;
+      if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess) cudaGetLastError();
+      fit[s] = std::max(n, s == 1 ? sms : 1);
+    }
+    if (tiles <= fit[s]) return s;
+  }
+  return 0;
+}
+
+// The few-tiles kernel, if it is its case: *done says so.
+template <class T, class TX, int NTOK, bool FUSED>
+cudaError_t launch_few(const CUtensorMap& tw, const CUtensorMap& tx, const LinParams& p, const TokenParams& t, int sms, cudaStream_t st, bool* done) {
+  using C = SCfg<NTOK, FUSED>;
+  auto kern = qlinear_few_kernel<T, TX, NTOK, FUSED>;
+  constexpr int threads = FUSED ? S_THREADS + 128 : S_THREADS;
   static bool attr_set = false;
+  static int fit[kMaxRanges + 1] = {};
   if (!attr_set) {
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<NTOK>::SMEM);
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
     if (e != cudaSuccess) return e;
     attr_set = true;
   }
-  const int64_t total = (int64_t)p.tiles_n * p.tiles_m * p.splits;
-  return launch_after(kern, (unsigned)std::min<int64_t>(total, sms), THREADS, Cfg<NTOK>::SMEM, st, tw, tx, p);
+  const int ranges = ranges_of<C>(kern, threads, p, sms, fit);
+  *done = ranges > 0 && !(FUSED && (p.k_blocks + ranges - 1) / ranges > kFusedBlocks);
+  if (!*done) return cudaSuccess;
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = ranges;
+  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.gridDim = dim3((unsigned)((int64_t)p.tiles_n * p.tiles_m * ranges));
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = C::SMEM;
+  cfg.stream = st;
+  cfg.attrs = at;
+  cfg.numAttrs = 2;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, tw, tx, p, t, ranges);
+  if (e != cudaSuccess) cudaGetLastError();
+  return e;
 }
-template <class T>
-cudaError_t launch_tokens(const CUtensorMap& tw, const CUtensorMap& tx, const LinParams& p, int ntok, int sms, cudaStream_t st) {
-  return ntok == 16   ? launch_as<T, 16>(tw, tx, p, sms, st)
-         : ntok == 32 ? launch_as<T, 32>(tw, tx, p, sms, st)
-         : ntok == 64 ? launch_as<T, 64>(tw, tx, p, sms, st)
-                      : launch_as<T, 128>(tw, tx, p, sms, st);
+
+template <class TX>
+cudaError_t quantize_tokens(const TokenParams& t, int sms, cudaStream_t st) {
+  return launch_after(quantize_tokens_kernel<TX>, (unsigned)std::min<int64_t>(t.M, (int64_t)sms * 8), 256, 0, st, t);
+}
+
+template <class T, class TX, int NTOK>
+cudaError_t launch_as(const CUtensorMap& tw, const CUtensorMap& tx, const LinParams& p, const TokenParams& t, int sms, cudaStream_t st) {
+  bool done = false;
+  cudaError_t e;
+  if constexpr (NTOK == 16) {
+    e = launch_few<T, TX, NTOK, true>(tw, tx, p, t, sms, st, &done);
+    if (e != cudaSuccess || done) return e;
+  }
+  if ((e = quantize_tokens<TX>(t, sms, st)) != cudaSuccess) return e;
+  e = launch_few<T, half_t, NTOK, false>(tw, tx, p, t, sms, st, &done);
+  if (e != cudaSuccess || done) return e;
+  auto many = qlinear_kernel<T, NTOK>;
+  static bool attr_set = false;
+  if (!attr_set) {
+    e = cudaFuncSetAttribute(many, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<NTOK>::SMEM);
+    if (e != cudaSuccess) return e;
+    attr_set = true;
+  }
+  return launch_after(many, (unsigned)std::min<int64_t>((int64_t)p.tiles_n * p.tiles_m, sms), THREADS, Cfg<NTOK>::SMEM, st, tw, tx, p);
+}
+template <class T, class TX>
+cudaError_t launch_tokens(const CUtensorMap& tw, const CUtensorMap& tx, const LinParams& p, const TokenParams& t, int ntok, int sms, cudaStream_t st) {
+  return ntok == 16   ? launch_as<T, TX, 16>(tw, tx, p, t, sms, st)
+         : ntok == 32 ? launch_as<T, TX, 32>(tw, tx, p, t, sms, st)
+         : ntok == 64 ? launch_as<T, TX, 64>(tw, tx, p, t, sms, st)
+                      : launch_as<T, TX, 128>(tw, tx, p, t, sms, st);
+}
+template <class TX>
+cudaError_t launch_out(const CUtensorMap& tw, const CUtensorMap& tx, const LinParams& p, const TokenParams& t, jab_dtype y, int ntok, int sms, cudaStream_t st) {
+  return y == JAB_FP16   ? launch_tokens<half_t, TX>(tw, tx, p, t, ntok, sms, st)
+         : y == JAB_BF16 ? launch_tokens<bf16_t, TX>(tw, tx, p, t, ntok, sms, st)
+                         : launch_tokens<float, TX>(tw, tx, p, t, ntok, sms, st);
 }
 
 }  // namespace
@@ -470,15 +782,10 @@ cudaError_t launch_quantized_linear(const QLinearArgs& a, int sms, cudaStream_t 
   p.tiles_m = (int)((a.M + ntok - 1) / ntok);
   const int64_t tiles = (int64_t)p.tiles_n * p.tiles_m;
   if (tiles >= (int64_t)1 << 29) return cudaErrorInvalidValue;
-  // K is split while tiles leave SMs idle, in ranges of at least four blocks
-  p.splits = s.parts > 0 ? (int)std::max<int64_t>(1, std::min<int64_t>(sms / tiles, p.k_blocks / 4)) : 1;
-  p.by_tiles = FastDiv((int)tiles);
   p.by_n = FastDiv(p.tiles_n);
   p.sx = reinterpret_cast<const float*>(w + s.sx);
   p.sw = a.w_scales;
   p.y = a.y;
-  p.counters = reinterpret_cast<int*>(w + s.zero);
-  p.part = p.counters + 4 * kMaxSplitTiles;
   p.status = a.status;
   TokenParams t{};
   t.x = a.x;
@@ -488,20 +795,12 @@ cudaError_t launch_quantized_linear(const QLinearArgs& a, int sms, cudaStream_t 
   t.Kp = Kp;
   t.xh = reinterpret_cast<half_t*>(w + s.xh);
   t.sx = reinterpret_cast<float*>(w + s.sx);
-  t.zero = p.counters;
-  t.n_zero = p.splits > 1 ? 4 * kMaxSplitTiles + s.parts : 0;
   t.status = a.status;
   CUtensorMap tw, tx;
   if (!make_map(&tw, CU_TENSOR_MAP_DATA_TYPE_UINT8, a.codes, a.K, a.N, a.K, BK, TM, CU_TENSOR_MAP_SWIZZLE_64B) ||
       !make_map(&tx, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, t.xh, Kp, a.M, (uint64_t)Kp * 2, BK, ntok, CU_TENSOR_MAP_SWIZZLE_128B))
     return cudaErrorInvalidValue;
-  const unsigned rows = (unsigned)std::min<int64_t>(std::max<int64_t>(a.M, (t.n_zero + 2047) / 2048), (int64_t)sms * 8);
-  cudaError_t e = a.x_type == JAB_FP16 ? launch_after(quantize_tokens_kernel<half_t>, rows, 256, 0, st, t)
-                                       : launch_after(quantize_tokens_kernel<bf16_t>, rows, 256, 0, st, t);
-  if (e != cudaSuccess) return e;
-  if (a.y_type == JAB_FP16) return launch_tokens<half_t>(tw, tx, p, ntok, sms, st);
-  if (a.y_type == JAB_BF16) return launch_tokens<bf16_t>(tw, tx, p, ntok, sms, st);
-  return launch_tokens<float>(tw, tx, p, ntok, sms, st);
+  return a.x_type == JAB_FP16 ? launch_out<half_t>(tw, tx, p, t, a.y_type, ntok, sms, st) : launch_out<bf16_t>(tw, tx, p, t, a.y_type, ntok, sms, st);
 }
 
 }  // namespace jab
