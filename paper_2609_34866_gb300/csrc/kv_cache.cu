@@ -11,33 +11,14 @@
 
 #include "common.cuh"
 #include "serve.h"
+#include "tc.cuh"
 
 namespace jab {
 namespace {
 
-template <class T>
-__device__ __forceinline__ void load8(const T* p, float (&v)[8]);
-template <>
-__device__ __forceinline__ void load8<float>(const float* p, float (&v)[8]) {
+__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
   const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
   v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-}
-template <>
-__device__ __forceinline__ void load8<half_t>(const half_t* p, float (&v)[8]) {
-  const uint4 u = __ldg(reinterpret_cast<const uint4*>(p));
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-    v[2 * i] = f.x, v[2 * i + 1] = f.y;
-  }
-}
-template <>
-__device__ __forceinline__ void load8<bf16_t>(const bf16_t* p, float (&v)[8]) {
-  const uint4 u = __ldg(reinterpret_cast<const uint4*>(p));
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(w[i] << 16), v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
 }
 
 __device__ __forceinline__ uint32_t pack2(float a, float b, half_t) {
@@ -63,8 +44,8 @@ __device__ __forceinline__ void store(float* p, const float (&v)[N]) {
 
 struct WriteParams {
   const void* x;
-  int64_t ldx, units, n_slots;
-  int n_heads, n_q, n_kv, page;
+  int64_t ldx, n_tokens, n_slots;
+  int n_heads, n_q, n_kv, page, page_shift;  // page_shift: log2 of page, or -1
   const int64_t* slots;
   const int32_t* positions;
   const float *cos_t, *sin_t;
@@ -75,111 +56,188 @@ struct WriteParams {
   int* status;
 };
 
-// A row of DH elements by DH / 16 threads, each with elements [8t, 8t + 8) of either half: the rotation's
-// partners are in the same thread, all loads and stores of Q are 16 bytes.
-template <class T, int DH, int BITS>
-__global__ void __launch_bounds__(256) kv_write_kernel(const __grid_constant__ WriteParams p) {
-  constexpr int LANES = DH / 16, QMAX = (1 << (BITS - 1)) - 1;
-  stream_order();
-  const int t = threadIdx.x % LANES;
-  const int64_t step = (int64_t)gridDim.x * (256 / LANES);
-  const int64_t first = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
-  // whole warps go round together: the rows' maxima are exchanged by shuffles
-  const int64_t rounds = (p.units + step - 1) / step;
-  for (int64_t it = 0; it < rounds; ++it) {
-    const int64_t unit = first + it * step;
-    bool live = unit < p.units;
-    const int64_t token = live ? unit / p.n_heads : 0;
-    const int head = live ? (int)(unit - token * p.n_heads) : 0;
-    const int64_t slot = live ? __ldg(p.slots + token) : -1;
-    live = slot >= 0;
-    const bool is_q = head < p.n_q, turn = p.positions != nullptr && head < p.n_q + p.n_kv;
-    if (live && slot >= p.n_slots) {
-      report(p.status, JAB_ERR_INVALID_ARG);
-      live = false;
-    }
-    int pos = 0;
-    if (live && turn) {
-      pos = __ldg(p.positions + token);
-      if (pos < 0 || pos >= p.rope_len) {
-        report(p.status, JAB_ERR_INVALID_ARG);
-        live = false;
-      }
-    }
-    if (is_q && p.q_out == nullptr) live = false;
-    float a[8] = {}, b[8] = {};
-    if (live) {
-      const T* row = static_cast<const T*>(p.x) + token * p.ldx + (int64_t)head * DH + 8 * t;
-      load8(row, a);
-      load8(row + DH / 2, b);
-      if (turn) {
-        float c[8], s[8];
-        load8(p.cos_t + (int64_t)pos * (DH / 2) + 8 * t, c);
-        load8(p.sin_t + (int64_t)pos * (DH / 2) + 8 * t, s);
+// fl32(x / s) for two x, with r = fl32(1 / s): the quotient corrected twice by its exact remainder. The first leaves it
+// within a unit in the last place, from where the second gives the IEEE quotient (Markstein, "Computation of elementary
+// functions on the IBM RISC System/6000 processor", 1990), as long as nothing leaves the normal range.
+__device__ __forceinline__ float2 quotients(float2 x, float2 r, float2 minus_s) {
+  float2 q = tc::mul2(x, r);
+  q = tc::fma2(tc::fma2(q, minus_s, x), r, q);
+  return tc::fma2(tc::fma2(q, minus_s, x), r, q);
+}
+
+// Codes of 8 elements of a row with scale s (> 0), offset by 2^(BITS - 1): bytes, or halves of bytes.
+template <int BITS>
+__device__ __forceinline__ void codes8(const float (&x)[8], float s, uint32_t (&w)[BITS / 4]) {
+  constexpr float OFFSET = BITS == 8 ? 128.f : 8.f;
+  uint32_t u[8];
+  if (s >= 7.8886091e-31f && s <= 1.2676506e30f) {  // 2^-100 .. 2^100: |x / s| is at most qmax and a rounding, or far below 1/2
+    const float r1 = __frcp_rn(s);
+    const float2 r = make_float2(r1, r1), ms = make_float2(-s, -s);
+    const float2 magic = make_float2(12582912.f, 12582912.f), off = make_float2(OFFSET, OFFSET);  // 1.5 * 2^23: to whole numbers, half to even
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float u = __fsub_rn(__fmul_rn(a[i], c[i]), __fmul_rn(b[i], s[i]));
-          b[i] = __fadd_rn(__fmul_rn(b[i], c[i]), __fmul_rn(a[i], s[i]));
-          a[i] = u;
+    for (int i = 0; i < 8; i += 2) {
+      const float2 q = tc::add2(tc::add2(quotients(make_float2(x[i], x[i + 1]), r, ms), magic), off);
+      u[i] = __float_as_uint(q.x), u[i + 1] = __float_as_uint(q.y);  // (the low bits are the number)
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) u[i] = (uint32_t)((int)fminf(fmaxf(rintf(__fdiv_rn(x[i], s)), 1.f - OFFSET), OFFSET - 1.f) + (int)OFFSET);
+  }
+  if constexpr (BITS == 8) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      w[i] = __byte_perm(__byte_perm(u[4 * i], u[4 * i + 1], 0x0040), __byte_perm(u[4 * i + 2], u[4 * i + 3], 0x0040), 0x5410);
+  } else {
+    const uint32_t even = __byte_perm(__byte_perm(u[0], u[2], 0x0040), __byte_perm(u[4], u[6], 0x0040), 0x5410);
+    const uint32_t odd = __byte_perm(__byte_perm(u[1], u[3], 0x0040), __byte_perm(u[5], u[7], 0x0040), 0x5410);
+    w[0] = (even & 0x0f0f0f0fu) | (odd & 0x0f0f0f0fu) << 4;
+  }
+}
+
+// Eight elements of a row as they lie in memory.
+template <class T>
+struct Raw8 {
+  uint4 w[sizeof(T) / 2];
+  __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = __ldcs(reinterpret_cast<const uint4*>(p) + i);
+  }
+  __device__ __forceinline__ void numbers(float (&x)[8]) const {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        x[4 * i] = __uint_as_float(w[i].x), x[4 * i + 1] = __uint_as_float(w[i].y), x[4 * i + 2] = __uint_as_float(w[i].z), x[4 * i + 3] = __uint_as_float(w[i].w);
+    } else {
+      const uint32_t u[4] = {w[0].x, w[0].y, w[0].z, w[0].w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (std::is_same<T, half_t>::value) {
+          const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u[i]));
+          x[2 * i] = f.x, x[2 * i + 1] = f.y;
+        } else {
+          x[2 * i] = __uint_as_float(u[i] << 16), x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
         }
       }
     }
-    uint32_t big = 0;  // magnitude bits of the row's largest (an infinity or a NaN is larger than all others)
+  }
+};
+
+// The largest magnitude of three, or NaN if one is NaN.
+__device__ __forceinline__ float largest(float a, float b, float c) {
+  float d;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+
+// Blocks go over the tokens and a token's heads, a row of DH elements by DH / 16 threads, each with elements [8t, 8t + 8)
+// of either half: the rotation's partners are in the same thread, all loads and stores of Q are 16 bytes. The next row,
+// the next token's angles and the slot and position of the one after are under way while a row is worked on. Long inputs
+// are bound by instructions as much as by bytes: with a grid-stride loop over rows, its 64-bit divisions and a division of
+// every element, 8 x 2048 tokens of 48 heads of 128 (370 MB) took 108 us, with a token a block and no row ahead 90, like this 67 (5.5 TB/s).
+template <class T, int DH, int BITS>
+__global__ void __launch_bounds__(384, sizeof(T) == 2 ? 2 : 1) kv_write_kernel(const __grid_constant__ WriteParams p) {
+  constexpr int LANES = DH / 16;
+  stream_order();
+  const int t = threadIdx.x % LANES, head0 = threadIdx.x / LANES, heads = blockDim.x / LANES;
+  Raw8<T> lo, hi;
+  float c[8], s[8];
+  int64_t slot = -1, next_slot = -1;
+  int pos = 0, next_pos = 0;
+  auto place = [&](int64_t token) {
+    next_slot = __ldg(p.slots + token);
+    if (p.positions != nullptr) next_pos = __ldg(p.positions + token);
+  };
+  auto angles = [&] {
+    slot = next_slot, pos = next_pos;
+    if (p.positions != nullptr && pos >= 0 && pos < p.rope_len) {
+      load8(p.cos_t + (int64_t)pos * (DH / 2) + 8 * t, c);
+      load8(p.sin_t + (int64_t)pos * (DH / 2) + 8 * t, s);
+    }
+  };
+  auto fetch = [&](int64_t token, int head) {
+    if (head < p.n_heads && (head >= p.n_q || p.q_out != nullptr)) {
+      const T* row = static_cast<const T*>(p.x) + token * p.ldx + (int64_t)head * DH + 8 * t;
+      lo.load(row), hi.load(row + DH / 2);
+    }
+  };
+  int64_t token = blockIdx.x;
+  int head = head0;
+  place(token);
+  fetch(token, head);
+  angles();
+  if (token + gridDim.x < p.n_tokens) place(token + gridDim.x);
+  // (whole warps go round together: the rows' maxima are exchanged by shuffles)
+  while (token < p.n_tokens) {
+    float a[8], b[8];
+    lo.numbers(a), hi.numbers(b);
+    const int64_t now = token, to = slot;
+    const int row = head;
+    const bool is_q = row < p.n_q, is_k = row < p.n_q + p.n_kv, turn = p.positions != nullptr && is_k;
+    const bool placed = to >= 0 && to < p.n_slots, turnable = p.positions == nullptr || (pos >= 0 && pos < p.rope_len);
+    const bool live = placed && row < p.n_heads && (!turn || turnable) && !(is_q && p.q_out == nullptr);
+    if (threadIdx.x == 0 && to >= 0 && (!placed || !turnable)) report(p.status, JAB_ERR_INVALID_ARG);
+    if (live && turn) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      big = max(big, max(__float_as_uint(a[i]) & 0x7fffffffu, __float_as_uint(b[i]) & 0x7fffffffu));
-    if (is_q) {
-      if (live) {
-        T* out = static_cast<T*>(p.q_out) + (token * p.n_q + head) * DH + 8 * t;
+      for (int i = 0; i < 8; ++i) {  // every product and every sum rounded: no contraction, which packed forms were seen to get
+        const float x = a[i], y = b[i];
+        a[i] = __fsub_rn(__fmul_rn(x, c[i]), __fmul_rn(y, s[i]));
+        b[i] = __fadd_rn(__fmul_rn(y, c[i]), __fmul_rn(x, s[i]));
+      }
+    }
+    head += heads;
+    if (head - head0 >= p.n_heads) {
+      head = head0, token += gridDim.x;
+      if (token < p.n_tokens) angles();
+      if (token + gridDim.x < p.n_tokens) place(token + gridDim.x);
+    }
+    if (token < p.n_tokens) fetch(token, head);
+    float big = 0.f;
+    if (live) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) big = largest(big, a[i], b[i]);
+      if (is_q) {
+        T* out = static_cast<T*>(p.q_out) + (now * p.n_q + row) * DH + 8 * t;
         store(out, a);
         store(out + DH / 2, b);
-        // finite, but not in Q's type: from halfway past the largest fp16 (65504) on
-        if (sizeof(T) == 2 && std::is_same<T, half_t>::value && big >= 0x477ff000u) report(p.status, JAB_ERR_RANGE);
+        // finite, but not in Q's type (or neither): from halfway past the largest fp16 (65504) on
+        if (std::is_same<T, half_t>::value && !(big < 65520.f)) report(p.status, JAB_ERR_RANGE);
       }
     }
 #pragma unroll
-    for (int o = LANES / 2; o > 0; o >>= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, o));
+    for (int o = LANES / 2; o > 0; o >>= 1) big = largest(big, __shfl_xor_sync(0xffffffffu, big, o), 0.f);
     if (is_q || !live) continue;
-    const bool fine = big < 0x7f800000u;
+    const bool fine = big < INFINITY;
     if (!fine) report(p.status, JAB_ERR_NONFINITE);
-    const float s = fine ? __fdiv_rn(__uint_as_float(big), (float)QMAX) : __uint_as_float(0x7fc00000u);
-    int q[16];
+    const float scale = fine ? __fdiv_rn(big, (float)((1 << (BITS - 1)) - 1)) : __uint_as_float(0x7fc00000u);
+    uint32_t w[2][BITS / 4];
+    if (scale > 0.f) {
+      codes8<BITS>(a, scale, w[0]);
+      codes8<BITS>(b, scale, w[1]);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const float x = i < 8 ? a[i] : b[i - 8];
-      const float r = fminf(fmaxf(rintf(__fdiv_rn(x, s)), (float)-QMAX), (float)QMAX);
-      q[i] = (fine && s > 0.f ? (int)r : 0) + QMAX + 1;
+      for (int i = 0; i < BITS / 4; ++i) w[0][i] = w[1][i] = BITS == 8 ? 0x80808080u : 0x88888888u;
     }
-    const bool is_k = head < p.n_q + p.n_kv;
-    const int h = head - p.n_q - (is_k ? 0 : p.n_kv);
-    const int64_t pg = slot / p.page;
-    const int64_t r = (pg * p.n_kv + h) * p.page + (slot - pg * p.page);
-    uint8_t* codes = (is_k ? p.k_codes : p.v_codes) + r * (DH * BITS / 8);
+    const int h = row - p.n_q - (is_k ? 0 : p.n_kv);
+    const int64_t pg = p.page_shift >= 0 ? to >> p.page_shift : to / p.page;
+    const int64_t r = (pg * p.n_kv + h) * p.page + (to - pg * p.page);
+    uint8_t* codes = (is_k ? p.k_codes : p.v_codes) + r * (DH * BITS / 8) + t * BITS;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
-      const int* c = q + 8 * half;
-      if (BITS == 8) {
-        uint2 w;
-        w.x = c[0] | c[1] << 8 | c[2] << 16 | (uint32_t)c[3] << 24;
-        w.y = c[4] | c[5] << 8 | c[6] << 16 | (uint32_t)c[7] << 24;
-        *reinterpret_cast<uint2*>(codes + half * (DH / 2) + 8 * t) = w;
-      } else {
-        uint32_t w = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) w |= (uint32_t)c[i] << (4 * i);
-        *reinterpret_cast<uint32_t*>(codes + half * (DH / 4) + 4 * t) = w;
-      }
+      if constexpr (BITS == 8)
+        *reinterpret_cast<uint2*>(codes + half * (DH / 2)) = make_uint2(w[half][0], w[half][1]);
+      else
+        *reinterpret_cast<uint32_t*>(codes + half * (DH / 4)) = w[half][0];
     }
-    if (t == 0) (is_k ? p.k_scales : p.v_scales)[r] = s;
+    if (t == 0) (is_k ? p.k_scales : p.v_scales)[r] = scale;
   }
 }
 
 struct ReadParams {
   const uint8_t *k_codes, *v_codes;
   const float *k_scales, *v_scales;
-  int64_t rows;  // n_seqs * T * n_kv
+  int64_t tokens;  // n_seqs * T
   int64_t n_pages;
-  int n_kv, page, T, max_pages;
+  int n_kv, page, page_shift, T, max_pages;
   const int32_t *pages, *starts, *counts;
   void *k, *v;
   int* status;
@@ -203,21 +261,25 @@ __device__ __forceinline__ void decode(const uint8_t* p, float s, float (&v)[N])
   }
 }
 
-// A thread stores 16 bytes of K and 16 of V.
+// A thread stores 16 bytes of K and 16 of V of the block's tokens in turn.
 template <class T, int DH, int BITS>
-__global__ void __launch_bounds__(256) kv_read_kernel(const __grid_constant__ ReadParams p) {
+__global__ void __launch_bounds__(256) kv_read_kernel(const __grid_constant__ ReadParams p, int per_block) {
   constexpr int N = 16 / sizeof(T), LANES = DH / N;
   stream_order();
-  const int t = threadIdx.x % LANES;
-  const int64_t step = (int64_t)gridDim.x * (256 / LANES);
-  for (int64_t row = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES; row < p.rows; row += step) {
-    const int64_t bt = row / p.n_kv;
-    const int h = (int)(row - bt * p.n_kv);
-    const int b = (int)(bt / p.T), j = (int)(bt - (int64_t)b * p.T);
+  const int units = p.n_kv * LANES;
+  const int64_t t0 = (int64_t)blockIdx.x * per_block;
+  const int n = (int)min((int64_t)per_block, p.tokens - t0);
+  int b = (int)(t0 / p.T), j = (int)(t0 - (int64_t)b * p.T);
+  // places of 16 bytes of the tokens' rows: u counts over (token, head, lane)
+  int token = threadIdx.x / units, u = threadIdx.x - token * units;
+  j += token;
+  while (token < n) {
+    while (j >= p.T) j -= p.T, ++b;
+    const int h = u / LANES, t = u % LANES;
     float k[N] = {}, v[N] = {};
     if (j < __ldg(p.counts + b)) {
       const int64_t at = (int64_t)j + (p.starts != nullptr ? __ldg(p.starts + b) : 0);
-      const int64_t pg = at / p.page;
+      const int64_t pg = p.page_shift >= 0 ? at >> p.page_shift : at / p.page;
       const int id = at >= 0 && pg < p.max_pages ? __ldg(p.pages + (int64_t)b * p.max_pages + pg) : -1;
       if (id >= 0 && id < p.n_pages) {
         const int64_t r = ((int64_t)id * p.n_kv + h) * p.page + (at - pg * p.page);
@@ -228,15 +290,22 @@ __global__ void __launch_bounds__(256) kv_read_kernel(const __grid_constant__ Re
         report(p.status, JAB_ERR_INVALID_ARG);
       }
     }
-    store(static_cast<T*>(p.k) + row * DH + t * N, k);
-    store(static_cast<T*>(p.v) + row * DH + t * N, v);
+    const int64_t o = ((t0 + token) * p.n_kv + h) * DH + t * N;
+    store(static_cast<T*>(p.k) + o, k);
+    store(static_cast<T*>(p.v) + o, v);
+    for (u += 256; u >= units; u -= units) ++token, ++j;
   }
 }
 
 template <class T, int DH, int BITS>
 cudaError_t write_as(const WriteParams& p, int sms, cudaStream_t st) {
-  const int64_t blocks = (p.units + 256 / (DH / 16) - 1) / (256 / (DH / 16));
-  return launch_after(kv_write_kernel<T, DH, BITS>, (unsigned)std::min<int64_t>(blocks, (int64_t)sms * 32), 256, 0, st, p);
+  // few tokens: a block has a token's heads, or as many of them as 384 threads take. Many (32 for every SM): a third of
+  // that, which loads a token's angles once for its rows in turn
+  constexpr int PER_SM = sizeof(T) == 2 ? 768 : 512;
+  const int want = p.n_heads * (DH / 16), limit = p.n_tokens >= 32 * (int64_t)sms ? std::max(64, want / 3) : 384;
+  const int threads = (std::min(want, limit) + 31) / 32 * 32;
+  const int64_t blocks = std::min<int64_t>(p.n_tokens, (int64_t)sms * std::min(32, std::max(1, PER_SM / threads)));
+  return launch_after(kv_write_kernel<T, DH, BITS>, (unsigned)blocks, threads, 0, st, p);
 }
 template <class T>
 cudaError_t write_type(const WriteParams& p, int dh, int bits, int sms, cudaStream_t st) {
@@ -246,9 +315,11 @@ cudaError_t write_type(const WriteParams& p, int dh, int bits, int sms, cudaStre
 
 template <class T, int DH, int BITS>
 cudaError_t read_as(const ReadParams& p, int sms, cudaStream_t st) {
-  constexpr int ROWS = 256 / (DH * (int)sizeof(T) / 16);
-  return launch_after(kv_read_kernel<T, DH, BITS>, (unsigned)std::min<int64_t>((p.rows + ROWS - 1) / ROWS, (int64_t)sms * 32),
-                      256, 0, st, p);
+  // four passes of a block's threads, fewer where the SMs would not all have one
+  const int64_t places = p.tokens * p.n_kv * (DH * (int64_t)sizeof(T) / 16);
+  const int64_t passes = std::max<int64_t>(1, std::min<int64_t>(4, places / (256 * (int64_t)sms)));
+  const int per_block = (int)std::max<int64_t>(1, passes * 256 / (p.n_kv * (DH * (int64_t)sizeof(T) / 16)));
+  return launch_after(kv_read_kernel<T, DH, BITS>, (unsigned)((p.tokens + per_block - 1) / per_block), 256, 0, st, p, per_block);
 }
 template <class T>
 cudaError_t read_type(const ReadParams& p, int dh, int bits, int sms, cudaStream_t st) {
@@ -266,8 +337,9 @@ cudaError_t launch_kv_write(const KvWriteArgs& a, int sms, cudaStream_t st) {
   p.n_q = a.n_q_heads;
   p.n_kv = c.n_kv_heads;
   p.n_heads = p.n_q + 2 * p.n_kv;
-  p.units = a.n_tokens * p.n_heads;
+  p.n_tokens = a.n_tokens;
   p.page = c.page_tokens;
+  p.page_shift = (p.page & (p.page - 1)) == 0 ? 31 - __builtin_clz(p.page) : -1;
   p.n_slots = c.n_pages * c.page_tokens;
   p.slots = a.slots;
   p.positions = a.positions;
@@ -292,7 +364,8 @@ cudaError_t launch_kv_read(const KvReadArgs& a, int sms, cudaStream_t st) {
   p.v_codes = static_cast<const uint8_t*>(c.v_codes);
   p.k_scales = c.k_scales;
   p.v_scales = c.v_scales;
-  p.rows = (int64_t)a.n_seqs * a.T * c.n_kv_heads;
+  p.tokens = (int64_t)a.n_seqs * a.T;
+  p.page_shift = (c.page_tokens & (c.page_tokens - 1)) == 0 ? 31 - __builtin_clz(c.page_tokens) : -1;
   p.n_pages = c.n_pages;
   p.n_kv = c.n_kv_heads;
   p.page = c.page_tokens;
