@@ -129,16 +129,17 @@ struct LinParams {
   int* status;
 };
 
+constexpr int LK = 2 * BK, LST = 4;  // many tiles: K of a stage, and stages of X and of A
 template <int NTOK>
 struct Cfg {
-  static constexpr int WST = NTOK == 128 ? 8 : 16;  // stages of weight codes
-  static constexpr int X_BYTES = NTOK * BK * 2;
+  static constexpr int WST = NTOK == 128 ? 4 : 8;  // stages of weight codes
+  static constexpr int W_STAGE = TM * LK, X_STAGE = NTOK * LK * 2;
   static constexpr int D_COLS = NTOK < 32 ? 32 : NTOK;
-  static constexpr int SMEM = WST * W_BYTES + AST * X_BYTES + 1024 + 512;
+  static constexpr int SMEM = WST * W_STAGE + LST * X_STAGE + 1024 + 512;
 };
 
 struct Bars {
-  uint64_t wfull[16], wempty[16], xfull[AST], afull[AST], empty[AST], tfull[2], tempty[2], drain;
+  uint64_t wfull[8], wempty[8], xfull[LST], ready[LST], empty[LST], tfull[2], tempty[2], drain;
   uint32_t tmem_base;
   int abort;
 };
@@ -180,24 +181,24 @@ template <class T, int NTOK>
 __global__ void __launch_bounds__(THREADS, 1)
     qlinear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const __grid_constant__ LinParams p) {
   using C = Cfg<NTOK>;
-  constexpr int WST = C::WST, XB = C::X_BYTES;
+  constexpr int WST = C::WST;
   constexpr uint32_t A_COL = 2 * C::D_COLS;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* w_smem = smem;
-  uint8_t* x_smem = smem + WST * W_BYTES;
-  Bars* bars = reinterpret_cast<Bars*>(x_smem + AST * XB);
+  uint8_t* x_smem = smem + WST * C::W_STAGE;
+  Bars* bars = reinterpret_cast<Bars*>(x_smem + LST * C::X_STAGE);
   const int warp = tc::warp_index(), lane = threadIdx.x & 31;
-  const int total = p.tiles_n * p.tiles_m;
+  const int total = p.tiles_n * p.tiles_m, stages = (p.k_blocks + 1) / 2;
   volatile int* abort = &bars->abort;
   if (threadIdx.x == 0) {
     for (int s = 0; s < WST; ++s) {
       tc::mbar_init(&bars->wfull[s], 1);
       tc::mbar_init(&bars->wempty[s], 4);
     }
-    for (int s = 0; s < AST; ++s) {
+    for (int s = 0; s < LST; ++s) {
       tc::mbar_init(&bars->xfull[s], 1);
-      tc::mbar_init(&bars->afull[s], 4);
+      tc::mbar_init(&bars->ready[s], 4);
       tc::mbar_init(&bars->empty[s], 1);
     }
     for (int a = 0; a < 2; ++a) {
@@ -228,45 +229,49 @@ __global__ void __launch_bounds__(THREADS, 1)
       for (int unit = blockIdx.x; unit < total && ok; unit += gridDim.x) {
         int nt, mt;
         p.by_n.divmod(unit, mt, nt);
-        for (int kb = 0; kb < p.k_blocks; ++kb, ++i) {
-          const int ws = i % WST, xs = i % AST;
+        for (int kb = 0; kb < stages; ++kb, ++i) {
+          const int ws = i % WST, xs = i % LST;
           if (!tc::mbar_wait(&bars->wempty[ws], ((i / WST) & 1) ^ 1, abort, p.status)) { ok = false; break; }
-          tc::mbar_expect_tx(&bars->wfull[ws], W_BYTES);
-          tc::tma_load_2d(w_smem + ws * W_BYTES, &tmW, &bars->wfull[ws], kb * BK, nt * TM);
-          if (!tc::mbar_wait(&bars->empty[xs], ((i / AST) & 1) ^ 1, abort, p.status)) {
+          tc::mbar_expect_tx(&bars->wfull[ws], C::W_STAGE);
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            tc::tma_load_2d(w_smem + ws * C::W_STAGE + h * W_BYTES, &tmW, &bars->wfull[ws], kb * LK + h * BK, nt * TM);
+          if (!tc::mbar_wait(&bars->empty[xs], ((i / LST) & 1) ^ 1, abort, p.status)) {
             drain_wait(&bars->wfull[ws], (i / WST) & 1);
             ok = false;
             break;
           }
-          tc::mbar_expect_tx(&bars->xfull[xs], XB);
-          tc::tma_load_2d(x_smem + xs * XB, &tmX, &bars->xfull[xs], kb * BK, mt * NTOK);
+          tc::mbar_expect_tx(&bars->xfull[xs], C::X_STAGE);
+#pragma unroll
+          for (int h = 0; h < 2; ++h)  // (the second half of a last stage can lie past the end: zeros)
+            tc::tma_load_2d(x_smem + xs * C::X_STAGE + h * (C::X_STAGE / 2), &tmX, &bars->xfull[xs], kb * LK + h * BK, mt * NTOK);
         }
       }
       if (*abort) {  // every copy issued has landed before shared memory goes to another block
         for (int j = max(0, i - WST); j < i; ++j) drain_wait(&bars->wfull[j % WST], (j / WST) & 1);
-        for (int j = max(0, i - AST); j < i; ++j) drain_wait(&bars->xfull[j % AST], (j / AST) & 1);
+        for (int j = max(0, i - LST); j < i; ++j) drain_wait(&bars->xfull[j % LST], (j / LST) & 1);
       }
     } else if (warp == 1) {  // ---------------- products
       // The whole warp waits, one thread issues: behind a wait of its own a single thread issued four products in 450
       // clocks (the compiler no longer knows it to be alone and loops over every operand), this way in 210; they take 256.
+      // One wait for eight products (the converters vouch for X): a wait is near 90 clocks.
       constexpr uint32_t IDESC = tc::idesc_f16(false, TM, NTOK);
       int i = 0, d = 0;
       bool ok = true;
       for (int unit = blockIdx.x; unit < total && ok; unit += gridDim.x) {
-        for (int c0 = 0; c0 < p.k_blocks && ok; c0 += kExactBlocks, ++d) {
+        for (int c0 = 0; c0 < stages && ok; c0 += kExactBlocks / 2, ++d) {
           ok = __all_sync(0xffffffffu, tc::mbar_wait(&bars->tempty[d & 1], ((d >> 1) & 1) ^ 1, abort, p.status));
-          const int n = min(kExactBlocks, p.k_blocks - c0);
+          const int n = min(kExactBlocks / 2, stages - c0);
           for (int b = 0; b < n && ok; ++b, ++i) {
-            const int s = i % AST;
-            ok = __all_sync(0xffffffffu, tc::mbar_wait(&bars->xfull[s], (i / AST) & 1, abort, p.status) &&
-                                             tc::mbar_wait(&bars->afull[s], (i / AST) & 1, abort, p.status));
+            const int s = i % LST;
+            ok = __all_sync(0xffffffffu, tc::mbar_wait(&bars->ready[s], (i / LST) & 1, abort, p.status));
             if (ok && tc::elect_one()) {
               tc::fence_after_sync();
-              const uint64_t xd = tc::sdesc_kmajor_sw128(tc::smem_u32(x_smem + s * XB));
+              const uint64_t xd = tc::sdesc_kmajor_sw128(tc::smem_u32(x_smem + s * C::X_STAGE));
 #pragma unroll
-              for (int k = 0; k < BK / 16; ++k)
-                tc::umma_f16_ts(tmem + (d & 1) * C::D_COLS, tmem + A_COL + s * 32 + k * 8, tc::sdesc_advance(xd, k * 32), IDESC,
-                                b > 0 || k > 0 ? 1u : 0u);
+              for (int k = 0; k < LK / 16; ++k)
+                tc::umma_f16_ts(tmem + (d & 1) * C::D_COLS, tmem + A_COL + s * (LK / 2) + k * 8,
+                                tc::sdesc_advance(xd, (k & 3) * 32 + (k >> 2) * (C::X_STAGE / 2)), IDESC, b > 0 || k > 0 ? 1u : 0u);
               tc::umma_commit(&bars->empty[s]);
               if (b + 1 == n) tc::umma_commit(&bars->tfull[d & 1]);
             }
@@ -290,7 +295,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       int acc[NTOK];
 #pragma unroll
       for (int c = 0; c < NTOK; ++c) acc[c] = 0;
-      for (int c0 = 0; c0 < p.k_blocks; c0 += kExactBlocks, ++d) {
+      for (int c0 = 0; c0 < stages; c0 += kExactBlocks / 2, ++d) {
         if (!tc::mbar_wait(&bars->tfull[d & 1], (d >> 1) & 1, abort, p.status)) { ok = false; break; }
         tc::fence_after_sync();
         const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (d & 1) * C::D_COLS;
@@ -327,33 +332,43 @@ __global__ void __launch_bounds__(THREADS, 1)
     for (int unit = blockIdx.x; unit < total && ok; unit += gridDim.x) {
       int nt, mt;
       p.by_n.divmod(unit, mt, nt);
-      for (int kb = 0; kb < p.k_blocks; ++kb, ++i) {
+      for (int kb = 0; kb < stages; ++kb, ++i) {
         if ((i & 1) != grp) continue;
-        const int ws = i % WST, s = i % AST;
+        const int ws = i % WST, s = i % LST;
         if (!tc::mbar_wait(&bars->wfull[ws], (i / WST) & 1, abort, p.status)) { ok = false; break; }
-        const uint4* src = reinterpret_cast<const uint4*>(w_smem + ws * W_BYTES + row * BK);
-        uint4 v[4];
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+          const uint4* src = reinterpret_cast<const uint4*>(w_smem + ws * C::W_STAGE + h * W_BYTES + row * BK);
+          uint4 v[4];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) v[c] = src[c ^ ((row >> 1) & 3)];  // TMA's 64-byte swizzle
-        __syncwarp();
-        if (lane == 0) tc::mbar_arrive(&bars->wempty[ws]);
-        uint32_t a[32];
+          for (int c = 0; c < 4; ++c) v[c] = src[c ^ ((row >> 1) & 3)];  // TMA's 64-byte swizzle
+          if (h == 1) {
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(&bars->wempty[ws]);
+          }
+          uint32_t a[32];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          codes_h2(v[c].x, a[8 * c], a[8 * c + 1]);
-          codes_h2(v[c].y, a[8 * c + 2], a[8 * c + 3]);
-          codes_h2(v[c].z, a[8 * c + 4], a[8 * c + 5]);
-          codes_h2(v[c].w, a[8 * c + 6], a[8 * c + 7]);
+          for (int c = 0; c < 4; ++c) {
+            codes_h2(v[c].x, a[8 * c], a[8 * c + 1]);
+            codes_h2(v[c].y, a[8 * c + 2], a[8 * c + 3]);
+            codes_h2(v[c].z, a[8 * c + 4], a[8 * c + 5]);
+            codes_h2(v[c].w, a[8 * c + 6], a[8 * c + 7]);
+          }
+          if (h == 0) {
+            if (!tc::mbar_wait(&bars->empty[s], ((i / LST) & 1) ^ 1, abort, p.status)) { ok = false; break; }
+            tc::fence_after_sync();
+            __syncwarp();
+          }
+          tc::tmem_st32(tmem + ((uint32_t)(quarter * 32) << 16) + A_COL + s * (LK / 2) + h * 32, a);
         }
-        if (!tc::mbar_wait(&bars->empty[s], ((i / AST) & 1) ^ 1, abort, p.status)) { ok = false; break; }
-        tc::fence_after_sync();
-        __syncwarp();
-        tc::tmem_st32(tmem + ((uint32_t)(quarter * 32) << 16) + A_COL + s * 32, a);
+        if (!ok) break;
         tc::tmem_st_wait();
         tc::fence_before_sync();
+        if (quarter == 0 && !tc::mbar_wait(&bars->xfull[s], (i / LST) & 1, abort, p.status)) { ok = false; break; }
         __syncwarp();
-        if (lane == 0) tc::mbar_arrive(&bars->afull[s]);
+        if (lane == 0) tc::mbar_arrive(&bars->ready[s]);
       }
+      if (!ok) break;
     }
   }
   tc::fence_before_sync();
