@@ -30,7 +30,7 @@ constexpr int TM = 128, BK = 64;      // output channels of a tile, K of a block
 constexpr int kExactBlocks = 16;      // K blocks that one accumulator may take (1024 products)
 constexpr int AST = 8;                // A buffers in tensor memory and X stages
 constexpr int W_BYTES = TM * BK;
-constexpr int THREADS = 512;
+constexpr int THREADS = 640;
 
 // ------------------------------------------------------------------ tokens to codes
 struct TokenParams {
@@ -135,7 +135,7 @@ struct Cfg {
   static constexpr int WST = NTOK == 128 ? 4 : 8;  // stages of weight codes
   static constexpr int W_STAGE = TM * LK, X_STAGE = NTOK * LK * 2;
   static constexpr int D_COLS = NTOK < 32 ? 32 : NTOK;
-  static constexpr int SMEM = WST * W_STAGE + LST * X_STAGE + 1024 + 512;
+  static constexpr int SMEM = WST * W_STAGE + LST * X_STAGE + 1024 + 512 + 8 * (NTOK / 2) * 4;
 };
 
 struct Bars {
@@ -160,6 +160,12 @@ template <>
 __device__ __forceinline__ half_t out_as<half_t>(float v) { return __float2half_rn(v); }
 template <>
 __device__ __forceinline__ bf16_t out_as<bf16_t>(float v) { return __float2bfloat16_rn(v); }
+
+__device__ __forceinline__ uint32_t pair_as(float a, float b, half_t) { return tc::pack_half2(a, b); }
+__device__ __forceinline__ uint32_t pair_as(float a, float b, bf16_t) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
 
 // 4 signed bytes as two fp16 pairs.
 __device__ __forceinline__ void codes_h2(uint32_t w, uint32_t& lo, uint32_t& hi) {
@@ -188,6 +194,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   uint8_t* w_smem = smem;
   uint8_t* x_smem = smem + WST * C::W_STAGE;
   Bars* bars = reinterpret_cast<Bars*>(x_smem + LST * C::X_STAGE);
+  float* token_scales = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(bars) + 512);
   const int warp = tc::warp_index(), lane = threadIdx.x & 31;
   const int total = p.tiles_n * p.tiles_m, stages = (p.k_blocks + 1) / 2;
   volatile int* abort = &bars->abort;
@@ -203,7 +210,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     }
     for (int a = 0; a < 2; ++a) {
       tc::mbar_init(&bars->tfull[a], 1);
-      tc::mbar_init(&bars->tempty[a], 4);
+      tc::mbar_init(&bars->tempty[a], 8);
     }
     tc::mbar_init(&bars->drain, 1);
     bars->abort = 0;
@@ -284,49 +291,68 @@ __global__ void __launch_bounds__(THREADS, 1)
         drain_wait(&bars->drain, 0);
       }
     }
-  } else if (warp < 8) {  // ---------------- epilogue
-    more_registers<216>();
-    const int quarter = warp & 3, row = quarter * 32 + lane;
+  } else if (warp < 12) {  // ---------------- epilogue: a warp has 32 channels and half of the tokens
+    more_registers<128>();
+    constexpr int HALF = NTOK / 2;
+    const int quarter = warp & 3, row = quarter * 32 + lane, first = warp < 8 ? 0 : HALF;
+    float* sx = token_scales + (warp - 4) * HALF;
+    // two channels of a token in one store, where they lie together in a word
+    const bool words = sizeof(T) == 2 && p.ldy % 2 == 0 && (reinterpret_cast<uintptr_t>(p.y) & 3) == 0;
     int d = 0;
     bool ok = true;
     for (int unit = blockIdx.x; unit < total && ok; unit += gridDim.x) {
       int nt, mt;
       p.by_n.divmod(unit, mt, nt);
-      int acc[NTOK];
+      const int n = nt * TM + row;
+      const int64_t m0 = (int64_t)mt * NTOK + first;
+      const int cols = (int)max((int64_t)0, min((int64_t)HALF, p.M - m0));
+      const float wn = n < p.N ? __ldg(p.sw + n) : 0.f;
+      __syncwarp();
+      for (int c = lane; c < cols; c += 32) sx[c] = p.sx[m0 + c];
+      int acc[HALF];
 #pragma unroll
-      for (int c = 0; c < NTOK; ++c) acc[c] = 0;
+      for (int c = 0; c < HALF; ++c) acc[c] = 0;
       for (int c0 = 0; c0 < stages; c0 += kExactBlocks / 2, ++d) {
         if (!tc::mbar_wait(&bars->tfull[d & 1], (d >> 1) & 1, abort, p.status)) { ok = false; break; }
         tc::fence_after_sync();
-        const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (d & 1) * C::D_COLS;
+        const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (d & 1) * C::D_COLS + first;
 #pragma unroll
-        for (int c = 0; c < NTOK; c += 32) {
-          uint32_t r[32];  // (16 columns: the rest of the 32 belongs to nobody)
+        for (int c = 0; c < HALF; c += 32) {
+          uint32_t r[32];  // (8 or 16 columns: the rest of the 32 is not used)
           __syncwarp();
           tc::tmem_ld32(taddr + c, r);
           tc::tmem_ld_wait();
 #pragma unroll
-          for (int j = 0; j < 32 && c + j < NTOK; ++j) acc[c + j] += __float2int_rn(__uint_as_float(r[j]));
+          for (int j = 0; j < 32 && c + j < HALF; ++j) acc[c + j] += __float2int_rn(__uint_as_float(r[j]));
         }
         tc::fence_before_sync();
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(&bars->tempty[d & 1]);
       }
       if (!ok) break;
-      const int n = nt * TM + row;
-      const int64_t m0 = (int64_t)mt * NTOK;
-      const int cols = (int)min((int64_t)NTOK, p.M - m0);
-      if (n < p.N) {
-        const float wn = __ldg(p.sw + n);
-        T* y = static_cast<T*>(p.y) + m0 * p.ldy + n;
+      __syncwarp();
+      T* y = static_cast<T*>(p.y) + m0 * p.ldy + n;
+      if (words && cols == HALF && (nt + 1) * TM <= p.N) {
+        // lanes 2i and 2i + 1 exchange a token: the even one stores the first of two, the odd one the second
+        const bool odd = lane & 1;
+        y += odd ? p.ldy - 1 : 0;
 #pragma unroll
-        for (int c = 0; c < NTOK; ++c)
-          if (c < cols) y[c * p.ldy] = out_as<T>(__fmul_rn(__fmul_rn((float)acc[c], p.sx[m0 + c]), wn));
+        for (int c = 0; c < HALF; c += 2) {
+          const float2 s = *reinterpret_cast<const float2*>(sx + c);
+          const float u = __fmul_rn(__fmul_rn((float)acc[c], s.x), wn), v = __fmul_rn(__fmul_rn((float)acc[c + 1], s.y), wn);
+          const float other = __shfl_xor_sync(0xffffffffu, odd ? u : v, 1);
+          if constexpr (sizeof(T) == 2) *reinterpret_cast<uint32_t*>(y) = odd ? pair_as(other, v, T()) : pair_as(u, other, T());
+          y += 2 * p.ldy;
+        }
+      } else if (n < p.N) {
+#pragma unroll
+        for (int c = 0; c < HALF; ++c)
+          if (c < cols) y[c * p.ldy] = out_as<T>(__fmul_rn(__fmul_rn((float)acc[c], sx[c]), wn));
       }
     }
   } else {  // ---------------- converters
-    fewer_registers<104>();
-    const int quarter = warp & 3, grp = (warp - 8) >> 2, row = quarter * 32 + lane;
+    fewer_registers<88>();
+    const int quarter = warp & 3, grp = (warp - 12) >> 2, row = quarter * 32 + lane;
     int i = 0;
     bool ok = true;
     for (int unit = blockIdx.x; unit < total && ok; unit += gridDim.x) {
