@@ -10,8 +10,8 @@
 #include <algorithm>
 
 #include "common.cuh"
+#include "quotient.cuh"
 #include "serve.h"
-#include "tc.cuh"
 
 namespace jab {
 namespace {
@@ -56,24 +56,15 @@ struct WriteParams {
   int* status;
 };
 
-// fl32(x / s) for two x, with r = fl32(1 / s): the quotient corrected twice by its exact remainder. The first leaves it
-// within a unit in the last place, from where the second gives the IEEE quotient (Markstein, "Computation of elementary
-// functions on the IBM RISC System/6000 processor", 1990), as long as nothing leaves the normal range.
-__device__ __forceinline__ float2 quotients(float2 x, float2 r, float2 minus_s) {
-  float2 q = tc::mul2(x, r);
-  q = tc::fma2(tc::fma2(q, minus_s, x), r, q);
-  return tc::fma2(tc::fma2(q, minus_s, x), r, q);
-}
-
 // Codes of 8 elements of a row with scale s (> 0), offset by 2^(BITS - 1): bytes, or halves of bytes.
 template <int BITS>
 __device__ __forceinline__ void codes8(const float (&x)[8], float s, uint32_t (&w)[BITS / 4]) {
   constexpr float OFFSET = BITS == 8 ? 128.f : 8.f;
   uint32_t u[8];
-  if (s >= 7.8886091e-31f && s <= 1.2676506e30f) {  // 2^-100 .. 2^100: |x / s| is at most qmax and a rounding, or far below 1/2
+  if (usual_scale(s)) {
     const float r1 = __frcp_rn(s);
     const float2 r = make_float2(r1, r1), ms = make_float2(-s, -s);
-    const float2 magic = make_float2(12582912.f, 12582912.f), off = make_float2(OFFSET, OFFSET);  // 1.5 * 2^23: to whole numbers, half to even
+    const float2 magic = make_float2(kToWhole, kToWhole), off = make_float2(OFFSET, OFFSET);
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
       const float2 q = tc::add2(tc::add2(quotients(make_float2(x[i], x[i + 1]), r, ms), magic), off);

@@ -20,6 +20,7 @@
 #include <algorithm>
 
 #include "kernels.h"
+#include "quotient.cuh"
 #include "serve.h"
 #include "tc.cuh"
 
@@ -68,6 +69,17 @@ template <class T>
 __device__ __forceinline__ uint4 row_codes(const uint4& u, float s) {
   float v[8];
   unpack8<T>(u, v);
+  if (usual_scale(s)) {
+    const float r1 = __frcp_rn(s);
+    const float2 r = make_float2(r1, r1), ms = make_float2(-s, -s), up = make_float2(kToWhole, kToWhole);
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 q = tc::sub2(tc::add2(quotients(make_float2(v[2 * j], v[2 * j + 1]), r, ms), up), up);
+      w[j] = tc::pack_half2(q.x, q.y);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     const float r = fminf(fmaxf(rintf(__fdiv_rn(v[j], s)), -127.f), 127.f);
@@ -494,6 +506,7 @@ __global__ void __launch_bounds__(FUSED ? S_THREADS + 128 : S_THREADS, 1)
   // The four products of a K block go to D_BUFS accumulators in turn; A takes the columns behind them
   constexpr uint32_t a_col = C::D_BUFS * C::D_COLS;
   constexpr int na = kMaxA;
+  constexpr bool SAME = XST == na;  // X's stages are free when A's are
   static_assert(a_col + na * 32 <= 512, "tensor memory");
   volatile int* abort = &bars->abort;
   if (threadIdx.x == 0) {
@@ -535,7 +548,7 @@ __global__ void __launch_bounds__(FUSED ? S_THREADS + 128 : S_THREADS, 1)
       for (; i < n_kb; ++i) {
         if (!FUSED) {
           const int xs = i % XST;
-          if (!tc::mbar_wait(&bars->xempty[xs], ((i / XST) & 1) ^ 1, abort, p.status)) break;
+          if (!tc::mbar_wait(SAME ? &bars->aempty[xs] : &bars->xempty[xs], ((i / XST) & 1) ^ 1, abort, p.status)) break;
           tc::mbar_expect_tx(&bars->xfull[xs], XB);
           tc::tma_load_2d(x_smem + xs * XB, &tmX, &bars->xfull[xs], (kb0 + i) * BK, mt * NTOK);
         }
@@ -561,8 +574,7 @@ __global__ void __launch_bounds__(FUSED ? S_THREADS + 128 : S_THREADS, 1)
     bool ok = !FUSED || __all_sync(0xffffffffu, tc::mbar_wait(&bars->xready, 0, abort, p.status));
     for (int i = 0; i < n_kb && ok; ++i) {
       const int s = i % na, xs = i % XST;
-      ok = __all_sync(0xffffffffu, (FUSED || tc::mbar_wait(&bars->xfull[xs], (i / XST) & 1, abort, p.status)) &&
-                                       tc::mbar_wait(&bars->afull[s], (i / na) & 1, abort, p.status));
+      ok = __all_sync(0xffffffffu, tc::mbar_wait(&bars->afull[s], (i / na) & 1, abort, p.status));
       if (ok && tc::elect_one()) {
         tc::fence_after_sync();
         const uint64_t xd = tc::sdesc_kmajor_sw128(tc::smem_u32(x_smem + xs * XB));
@@ -571,7 +583,7 @@ __global__ void __launch_bounds__(FUSED ? S_THREADS + 128 : S_THREADS, 1)
           tc::umma_f16_ts(tmem + k % C::D_BUFS * C::D_COLS, tmem + a_col + s * 32 + k * 8, tc::sdesc_advance(xd, k * 32), IDESC,
                           i > 0 || k >= C::D_BUFS ? 1u : 0u);
         tc::umma_commit(&bars->aempty[s]);
-        if (!FUSED) tc::umma_commit(&bars->xempty[xs]);
+        if (!FUSED && !SAME) tc::umma_commit(&bars->xempty[xs]);
       }
       __syncwarp();
     }
@@ -611,6 +623,8 @@ __global__ void __launch_bounds__(FUSED ? S_THREADS + 128 : S_THREADS, 1)
       tc::tmem_st32(tmem + lanes + a_col + s * 32, a);
       tc::tmem_st_wait();
       tc::fence_before_sync();
+      // (vouches for X: one wait less for the warp that issues)
+      if (!FUSED && quarter == 0 && !(ok = tc::mbar_wait(&bars->xfull[i % XST], (i / XST) & 1, abort, p.status))) break;
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(&bars->afull[s]);
     }
