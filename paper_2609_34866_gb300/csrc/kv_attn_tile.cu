@@ -44,7 +44,7 @@ struct Layout {
 
 struct Bars {
   uint64_t rk_full[KST], rk_empty[KST], rv_full[VST], rv_empty[VST], k_full[2], k_empty[2], sc_full[SCB], sc_empty[SCB], v_full[2], v_empty[2];
-  uint64_t q_full[2], q_empty, s_full[2], s_empty[2], p_full, pv_done, o_full, o_empty, drain[2];
+  uint64_t q_full[2], q_empty, rows_empty[2], s_full[2], s_empty[2], p_full[2], pv_done, o_full, o_empty, drain[2];
   uint32_t tmem_base;
   int abort;
 };
@@ -216,6 +216,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
       tc::mbar_init(&bars->k_empty[s], 1);
       tc::mbar_init(&bars->drain[s], 1);
       tc::mbar_init(&bars->q_full[s], 4);
+      tc::mbar_init(&bars->rows_empty[s], 8);
+      tc::mbar_init(&bars->p_full[s], 8);
       tc::mbar_init(&bars->v_full[s], 4);
       tc::mbar_init(&bars->v_empty[s], 1);
       tc::mbar_init(&bars->s_full[s], 1);
@@ -234,7 +236,6 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
       tc::mbar_init(&bars->sc_empty[s], 8);
     }
     tc::mbar_init(&bars->q_empty, 1);
-    tc::mbar_init(&bars->p_full, 8);
     tc::mbar_init(&bars->pv_done, 1);
     tc::mbar_init(&bars->o_full, 1);
     tc::mbar_init(&bars->o_empty, 8);
@@ -350,7 +351,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
         ok = __all_sync(0xffffffffu, tc::mbar_wait(&bars->o_empty, (i & 1) ^ 1, abort, p.status));
         for (int s = it.s0; s < it.s1 && ok; ++s, ++j) {
           ok = __all_sync(0xffffffffu, tc::mbar_wait(&bars->v_full[j & 1], (j >> 1) & 1, abort, p.status) &&
-                                           tc::mbar_wait(&bars->p_full, j & 1, abort, p.status));
+                                           tc::mbar_wait(&bars->p_full[j & 1], (j >> 1) & 1, abort, p.status));
           if (ok && tc::elect_one()) {
             tc::fence_after_sync();
             const uint64_t vd = tc::sdesc_mnmajor_sw128(tc::smem_u32(smem + L::V_OFF + (j & 1) * L::TILE), L::CHUNK, 1024);
@@ -401,6 +402,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
         lo[c] = rows_lo[r0 + g + 8 * c], hi[c] = rows_lo[R + r0 + g + 8 * c];
         fac[c] = __int_as_float(rows_lo[2 * R + r0 + g + 8 * c]);
       }
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(&bars->rows_empty[i & 1]);
       for (int s = it.s0; s < it.s1; ++s, ++j) {
         const float* sc = reinterpret_cast<const float*>(smem + L::SC_OFF + (j % SCB) * 3 * KT * 4) + 2 * q4;
         if (!(ok = tc::mbar_wait(&bars->sc_full[j % SCB], (j / SCB) & 1, abort, p.status) &&
@@ -510,7 +513,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
         tc::fence_before_sync();
         __syncwarp();
         if (lane == 0) {
-          tc::mbar_arrive(&bars->p_full);
+          tc::mbar_arrive(&bars->p_full[j & 1]);  // (two tiles can be ready before P V takes the first: V may be late)
           tc::mbar_arrive(&bars->sc_empty[j % SCB]);
         }
       }
@@ -628,6 +631,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
             tc::tmem_st32(tq + 32 * b, a);
           }
           tc::tmem_st_wait();
+          // (with items of one tile, S is done with the next one's Q while the softmax writes the output of the one before)
+          if (!(ok = tc::mbar_wait(&bars->rows_empty[i & 1], ((i >> 1) & 1) ^ 1, abort, p.status))) break;
           int* rows = reinterpret_cast<int*>(smem + L::ROW_OFF + (i & 1) * 3 * R * 4);
           rows[tid] = lo, rows[R + tid] = hi, rows[2 * R + tid] = __float_as_int(back);
           tc::fence_before_sync();

@@ -466,3 +466,32 @@ def test_attention_unused_table_entries():
     pages[1, 0], pages[2, :2] = 5, torch.tensor([1, 7], dtype=torch.int32, device="cuda")
     q = torch.randn((3, 4, 64), generator=_gen(2), device="cuda").to(torch.float16)
     _attend(cache, kd, vd, q, [1, 1, 1], [0, 9, 20], pages)
+
+
+@pytest.mark.parametrize("dh,bits,page,q,longest,window", [(64, 8, 64, 33, 127, 0), (128, 4, 16, 34, 128, 0), (64, 4, 32, 40, 250, 20), (128, 8, 128, 33, 300, 0)])
+def test_attention_many_short_items(dh, bits, page, q, longest, window):
+    """Several row tiles of one or a few key tiles for every block: the parts of the kernel run ahead of each other."""
+    g = _gen(q + longest)
+    B, h = 84, 8
+    lens = [q + (i * 37) % (longest - q + 1) for i in range(B)]
+    cache, kd, vd = _filled(g, h, dh, bits, page, sum(-(-n // page) for n in lens) + 1)
+    qs = torch.randn((B * q, h, dh), generator=g, device="cuda").to(torch.bfloat16)
+    pages = _pages(g, lens, page, cache.n_pages)
+    outs = []
+    for _ in range(20):
+        out, lse = torch.empty_like(qs), torch.empty((B * q, h), device="cuda")
+        start = torch.arange(B + 1, dtype=torch.int32, device="cuda") * q
+        ln = torch.tensor(lens, dtype=torch.int32, device="cuda")
+        ws = torch.empty(J.jab_kv_attention_workspace_size(cache, B, B * q, h, q, longest), dtype=torch.uint8, device="cuda")
+        J.jab_kv_attention(cache, qs, start, pages, ln, out, ws, q, longest, window=window, lse=lse)
+        outs.append((out, lse))
+    assert J.jab_get_device_status() == 0
+    assert all(torch.equal(o, outs[0][0]) and torch.equal(l, outs[0][1]) for o, l in outs)
+    at = torch.arange(longest, device="cuda")
+    for b in range(0, B, 9):
+        n = lens[b]
+        ids = pages[b].long()[at[:n] // page]
+        o, ls, mag = R.attention(qs[b * q:(b + 1) * q].double(), kd[ids, at[:n] % page], vd[ids, at[:n] % page], window, 1 / math.sqrt(dh))
+        tol = (2.0 ** -11 + 2.0 ** -16) * mag + n * 2.0 ** -25 * vd.abs().max() + HALF_ULP[qs.dtype] * o.abs() + 1e-30
+        assert bool(((outs[0][0][b * q:(b + 1) * q].double() - o).abs() <= tol).all()), b
+        assert bool(((outs[0][1][b * q:(b + 1) * q].double() - ls).abs() <= 2.0 ** -16 + 2.0 ** -21 * ls.abs()).all()), b
