@@ -290,10 +290,11 @@ __global__ void __launch_bounds__(256) kv_read_kernel(const __grid_constant__ Re
 
 template <class T, int DH, int BITS>
 cudaError_t write_as(const WriteParams& p, int sms, cudaStream_t st) {
-  // few tokens: a block has a token's heads, or as many of them as 384 threads take. Many (32 for every SM): a third of
-  // that, which loads a token's angles once for its rows in turn
+  // A block has a token's heads, or as many of them as 384 threads take. With four tokens for every SM and more, a
+  // third of that where it leaves no thread idle: it loads a token's angles once for its rows in turn (2048 tokens of 48
+  // heads of 128: 19 us for writing and reading, 22 without; but 64 tokens 4.9 instead of 4.5).
   constexpr int PER_SM = sizeof(T) == 2 ? 768 : 512;
-  const int want = p.n_heads * (DH / 16), limit = p.n_tokens >= 32 * (int64_t)sms ? std::max(64, want / 3) : 384;
+  const int want = p.n_heads * (DH / 16), limit = p.n_tokens >= 4 * (int64_t)sms && want % 96 == 0 ? want / 3 : 384;
   const int threads = (std::min(want, limit) + 31) / 32 * 32;
   const int64_t blocks = std::min<int64_t>(p.n_tokens, (int64_t)sms * std::min(32, std::max(1, PER_SM / threads)));
   return launch_after(kv_write_kernel<T, DH, BITS>, (unsigned)blocks, threads, 0, st, p);
