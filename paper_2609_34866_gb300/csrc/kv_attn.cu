@@ -343,7 +343,8 @@ __global__ void __launch_bounds__(32 * W) kv_attn_kernel(const __grid_constant__
     const Item it = item_at<R, KT>(p, cum_t, head, x, x1);
     const Entry& en = it.en;
     const int h = it.h, rt = it.rt;
-    // Q, and what its rows see; rows past the end see all, of a Q of zeros
+    // Q, and what its rows see; rows past the end see, with a Q of zeros, only keys that no mask could hide: what lies in
+    // hidden places must not move the references that the rows of a warp change together
     int all_lo, all_hi, lo[NT][2], hi[NT][2];
     seen_by_all(p, en, rt * R, rt * R + it.rows, head, all_lo, all_hi);
     uint32_t qf[NT][DH / 8];
@@ -353,7 +354,7 @@ __global__ void __launch_bounds__(32 * W) kv_attn_kernel(const __grid_constant__
       const int r = 8 * j + g, rr = rt * R + r, i = p.by_g.quot(rr), token = en.tok0 + i;
       const T* row = static_cast<const T*>(p.q) + (int64_t)token * p.ldq + (int64_t)(h * p.G + rr - i * p.G) * DH;
       const float back = load_q<T, DH, BITS>(row, q4, r < it.rows, qf[j]) * p.scale_log2;
-      int row_lo = 0, row_hi = INT32_MAX;
+      int row_lo = 0, row_hi = 0;
       if (r < it.rows) seen_by_row(p, en, en.all ? position_of(p, token) : en.len - en.nq + i, row_lo, row_hi);
 #pragma unroll
       for (int c = 0; c < 2; ++c) {

@@ -596,7 +596,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
         tc::fence_after_sync();
         {
           const bool live = tid < it.rows;
-          int lo = 0, hi = INT32_MAX;
+          int lo = 0, hi = 0;  // (a row past the item's sees no key that a mask could hide: what lies there must not move the references of its warp)
           const int rr = it.rt * R + tid, q = p.by_g.quot(rr), token = it.en.tok0 + q;
           if (live) seen_by_row(p, it.en, it.en.all ? position_of(p, token) : it.en.len - it.en.nq + q, lo, hi);
           const uint4* row = reinterpret_cast<const uint4*>(static_cast<const T*>(p.q) + (int64_t)token * p.ldq + (int64_t)(it.h * p.G + rr - q * p.G) * DH);
