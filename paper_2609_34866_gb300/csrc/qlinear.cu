@@ -144,6 +144,9 @@ template <int NTOK>
 struct Cfg {
   static constexpr int WST = NTOK == 128 ? 4 : 8;  // stages of weight codes
   static constexpr int W_STAGE = TM * LK, X_STAGE = NTOK * LK * 2;
+  // Rows of a box of weights: half as many requests for the copy engine at 128 bytes (64 tokens x 6144 x 4096: 14.7 us, at 64
+  // bytes 15.2), but the largest calls like the converters' reads of 64 better (8192 tokens: 293 us, at 128 bytes 305).
+  static constexpr int W_ROW = NTOK == 128 ? BK : LK;
   static constexpr int D_COLS = NTOK < 32 ? 32 : NTOK;
   static constexpr int GROUPS = NTOK == 128 ? 2 : 4, THREADS = 32 * (4 + 8 + 4 * GROUPS);
   static constexpr int EPI_REGS = NTOK == 128 ? 128 : 96, CONV_REGS = NTOK == 128 ? 88 : 64;
@@ -232,7 +235,9 @@ __global__ void __launch_bounds__(Cfg<NTOK>::THREADS, 1)
   volatile int* abort = &bars->abort;
   auto load_w = [&](int ws, int kb, int nt) {
     tc::mbar_expect_tx(&bars->wfull[ws], C::W_STAGE);
-    tc::tma_load_2d(w_smem + ws * C::W_STAGE, &tmW, &bars->wfull[ws], (st0 + kb) * LK, nt * TM);  // (past the end of K: zeros)
+#pragma unroll
+    for (int h = 0; h < LK / C::W_ROW; ++h)  // (past the end of K: zeros)
+      tc::tma_load_2d(w_smem + ws * C::W_STAGE + h * TM * C::W_ROW, &tmW, &bars->wfull[ws], (st0 + kb) * LK + h * C::W_ROW, nt * TM);
   };
   if (threadIdx.x == 0) {
     for (int s = 0; s < WST; ++s) {
@@ -440,10 +445,10 @@ __global__ void __launch_bounds__(Cfg<NTOK>::THREADS, 1)
         if (!tc::mbar_wait(&bars->wfull[ws], (i / WST) & 1, abort, p.status)) { ok = false; break; }
 #pragma unroll 1
         for (int h = 0; h < 2; ++h) {
-          const uint4* src = reinterpret_cast<const uint4*>(w_smem + ws * C::W_STAGE + row * LK);
+          const uint4* src = reinterpret_cast<const uint4*>(w_smem + ws * C::W_STAGE + (C::W_ROW == LK ? 0 : h * TM * BK) + row * C::W_ROW);
           uint4 v[4];
 #pragma unroll
-          for (int c = 0; c < 4; ++c) v[c] = src[(4 * h + c) ^ (row & 7)];  // TMA's 128-byte swizzle
+          for (int c = 0; c < 4; ++c) v[c] = src[C::W_ROW == LK ? (4 * h + c) ^ (row & 7) : c ^ ((row >> 1) & 3)];  // TMA's swizzle of such rows
           if (h == 1) {
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(&bars->wempty[ws]);
@@ -624,7 +629,8 @@ cudaError_t launch_quantized_linear(const QLinearArgs& a, int sms, cudaStream_t 
   t.sx = reinterpret_cast<float*>(w + s.sx);
   t.status = a.status;
   CUtensorMap tw, tx;
-  if (!make_map(&tw, CU_TENSOR_MAP_DATA_TYPE_UINT8, a.codes, a.K, a.N, a.K, LK, TM, CU_TENSOR_MAP_SWIZZLE_128B) ||
+  if (!make_map(&tw, CU_TENSOR_MAP_DATA_TYPE_UINT8, a.codes, a.K, a.N, a.K, ntok == 128 ? Cfg<128>::W_ROW : Cfg<16>::W_ROW, TM,
+                ntok == 128 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B) ||
       !make_map(&tx, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, t.xh, Kp, a.M, (uint64_t)Kp * 2, BK, ntok, CU_TENSOR_MAP_SWIZZLE_128B))
     return cudaErrorInvalidValue;
   const cudaError_t e = a.x_type == JAB_FP16 ? quantize_tokens<half_t>(t, sms, st) : quantize_tokens<bf16_t>(t, sms, st);
