@@ -389,8 +389,8 @@ jab_status jab_rope_table(int32_t length, int32_t head_dim, float theta, float* 
  * position (rotate-half; each product and sum rounded to fp32), K and V quantised per (token, head) and
  * written to the token's slot.
  *   X_dev          type [n_tokens, (n_q_heads + 2 n_kv_heads) * head_dim], pitch ldx
- *   slots_dev      int64 [n_tokens]: page * page_tokens + place in the page; < 0: padding, of which
- *                  nothing is read or written. Two tokens must not share a slot.
+ *   slots_dev      int64 [n_tokens]: page * page_tokens + place in the page; < 0: padding: whatever its
+ *                  row holds, nothing of it is written. Two tokens must not share a slot.
  *   positions_dev, cos_dev, sin_dev   int32 [n_tokens] and fp32 [rope_len, head_dim / 2]; all NULL: no
  *                  rotation
  *   Q_dev          out type [n_tokens, n_q_heads * head_dim] (no pitch), or NULL

@@ -20,6 +20,10 @@
 // a warp takes its share by itself, with no barrier, its copies running ahead of it across the share's items. Keys
 // shared by all sequences are one more entry of the list, whose rows are those of all sequences. A second kernel
 // joins the parts of items that went to several warps.
+//
+// Bound: the cache's bytes; 64 sequences of up to 8192 keys of 8 heads of 128 (328 MB) are read at 5.2 TB/s in 63 us, joined
+// in 10. In 4 bits the conversion of codes takes as long as their bytes would (4 sequences of up to 65536 keys, 227 MB:
+// 3.5 TB/s with 51 % of the issue slots in use).
 #include <algorithm>
 #include <type_traits>
 
@@ -74,7 +78,7 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
 // cache (V's of a group in the order (0, 2, 4, 6), (1, 3, 5, 7), (8, ...), (9, ...), as the lanes take them), their
 // 16-byte pieces exchanged so that neither the copies nor the reads meet in a bank; then a pair of scales per key.
 // Copies go along the rows, whole lines at a time: by the lanes that use the bytes, 4 rows of V an eighth of the warp,
-// they took 59 us where these take 40 (64 sequences of up to 8192 keys, without arithmetic).
+// they took 59 us where these took 40 (64 sequences of up to 8192 keys, arithmetic left out for the comparison).
 constexpr int DEPTH = 2;
 template <int DH, int BITS, int NS>
 struct Tile {
@@ -504,7 +508,7 @@ __global__ void __launch_bounds__(32 * W) kv_attn_kernel(const __grid_constant__
 
 // ------------------------------------------------------------------ joining
 // N floats at p (N 2 or 4) if `there`, else zeros; not from this SM's cache: other SMs wrote them. (volatile: a batch of
-// them is under way at once. Reading some one place instead of none brings all SMs to the same line: 35 us instead of 4.)
+// them is under way at once. Reading some one place instead of none would bring all SMs to the same line.)
 template <int N>
 __device__ __forceinline__ void load_part(const float* p, bool there, float (&v)[N]) {
 #pragma unroll
@@ -534,8 +538,9 @@ struct Joined {
 // no items. A trip to memory that other SMs wrote takes 0.6 us here, so that what counts is their number: the plan and
 // the item's record, then statistics and rows of BATCH parts at once. (One block per item over a chain of five trips took
 // 13 us for 64 sequences of up to 8192 keys.)
-// BATCH: parts of a row on their way at once; 16 for calls with few rows, which have many parts, 4 where many blocks an SM
-// are worth more.
+// BATCH: parts of a row on their way at once; 16 for calls with few rows, which have many parts (4 sequences of 65536
+// keys: 69 us in all, 81 with 4), 4 where many blocks an SM are worth more (64 behind a shared prefix of 8192: 76, 77 with
+// 16).
 template <class T, int DH, int BATCH>
 __global__ void __launch_bounds__(32 * MW, BATCH == 4 ? 6 : 2)
     kv_merge_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Joined j0, const __grid_constant__ Joined j1) {
@@ -658,7 +663,10 @@ int n_tiles_of_rows(int64_t rows) { return rows <= 8 ? 1 : rows <= 16 ? 2 : 4; }
 
 // Which kernel takes what. Sequences of up to kFewRows (token, head) rows go by 16-key tiles: the cache's bytes bound
 // them, not the products. Longer ones fill 128-row tiles; where lengths are mixed, those of up to 8 rows still go
-// by keys, in a launch of their own.
+// by keys, in a launch of their own. Measured, both ways (heads of 128, 8 bits, G = 4, up to 2048 keys): 64 sequences of 32
+// rows 116 us by keys and 165 by tiles, of 16 rows 61 and 163, of 36 rows 189 and 166, of 64 rows 200 and 170; 4 of 36
+// behind 8192 keys 58 and 44. (With heads of 64 and G = 1 the bound would lie higher: 64 sequences of 40 rows 170 and
+// 224, but 4 of 40 behind 8192 keys 54 and 47.)
 struct Route {
   List keys, tiles;
   int nt;  // 8-row blocks of the by-keys kernel

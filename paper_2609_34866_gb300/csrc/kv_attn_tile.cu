@@ -4,7 +4,7 @@
 // The codes of a key tile come as the bytes that they are, by bulk copies of the keys that share a page, and become
 // fp16 in shared memory once per tile; the scales stay outside of the products as they do there. (Loaded straight to
 // the converters' registers they would pass shared memory once less, but 128 threads have too few bytes in flight:
-// 2 x 512 queries behind 5000 keys took 292 us instead of 167.)
+// 2 x 512 queries behind 5000 keys took 292 us, by bulk copies 167 at that time.)
 // Both products are M128 N128 with their A operand in tensor memory:
 //   S = Q K^T   A = Q (fp16, written to tensor memory row by row), B = K as converted (K-major)
 //   O += P V    A = P (fp16 weights, written by the softmax), B = V as converted (MN-major: the same layout)
@@ -16,6 +16,8 @@
 //   warps 4..11   softmax: 16 rows a warp, four threads a row (16x256b shape); at an item's end the output
 //   warps 12..15  converters of K, a tile ahead; of Q at an item's start, and of the keys' scales
 //   warps 16..19  converters of V
+// Bound: no unit; a tile passes five stages that each wait for another (2 x 512 queries behind 5000 keys, 32 heads of 128:
+// 125 us and 28 to join, tensor pipe 21 % busy, issue slots 48 %), and instructions that a stage has to fetch again.
 #include <algorithm>
 #include <type_traits>
 

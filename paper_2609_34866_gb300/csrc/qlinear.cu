@@ -9,10 +9,15 @@
 //
 // Two launches: the rows of X become codes (held in fp16, the operand's type) and scales; then the product, with the output
 // channels on the accumulator's 128 lanes and the tokens on its columns. The weights travel as the bytes that they
-// are: TMA brings a 128 x 64 tile of codes to shared memory, converter warps turn it into fp16 in tensor memory (a
+// are: TMA brings a 128 x 128 tile of codes to shared memory, converter warps turn it into fp16 in tensor memory (a
 // byte under the exponent of 1024, less 1152), and the products take it from there as their A operand. One layout
 // serves one token and thousands. Many tiles: persistent blocks, two accumulators in turn, sums in registers. Few
 // tiles: one a cluster, whose blocks take K ranges of it and add their sums through shared memory.
+//
+// Bound: 8192 tokens x 6144 x 4096 take 293 us, 26 of them for the tokens' codes (0.7 of HBM's rate) and 265 for the
+// products, 1.56 PFLOP/s, 0.82 of the tensor cores' measured rate; without converters, drains and stores the products
+// alone took 237 in all. One token (25 MB of codes) takes 12 us where the bytes take 3.7: the chain of launches, copy,
+// conversion and products of 16 stages.
 #include <cudaTypedefs.h>
 
 #include <algorithm>
@@ -86,7 +91,8 @@ __device__ __forceinline__ uint4 row_codes(const uint4& u, float s) {
 }
 
 // A block per row; the row's first KEEP chunks of 8 elements a thread stay in registers between the maximum and
-// the codes, what is longer is read again.
+// the codes, what is longer is read again. Bound: bytes (8192 x 4096: 134 MB in 26 us; with a division for every element
+// 32).
 template <class T>
 __global__ void __launch_bounds__(256) quantize_tokens_kernel(const __grid_constant__ TokenParams p) {
   constexpr int KEEP = 2;
