@@ -13,6 +13,7 @@
 // show. In the others a weight is rounded once (2^-11 of it at most, over 128 keys and more).
 //   warp 0        bulk copies of codes and scales, rings of KST and VST tiles
 //   warp 1        tensor memory owner; issues S, a tile ahead of P V;   warp 2  issues P V
+//   warp 3        finds the block's items, ahead of all, and leaves them in a ring (each warp for itself: 1 to 2 us an item)
 //   warps 4..11   softmax: 16 rows a warp, four threads a row (16x256b shape); at an item's end the output
 //   warps 12..15  converters of K, a tile ahead; of Q at an item's start, and of the keys' scales
 //   warps 16..19  converters of V
@@ -28,7 +29,7 @@ namespace jab {
 namespace kv {
 namespace {
 
-constexpr int R = kTileRows, KT = kTileKeys, THREADS = 640, SCB = 3, KST = 2, VST = 2;
+constexpr int R = kTileRows, KT = kTileKeys, THREADS = 640, SCB = 3, KST = 2, VST = 2, IST = 4;
 
 template <int DH, int BITS>
 struct Layout {
@@ -40,17 +41,24 @@ struct Layout {
   static constexpr int SC_OFF = RV_OFF + VST * RAW;                         // per tile: K scale * log2 e * c, V scale, its log2
   static constexpr int ROW_OFF = SC_OFF + SCB * 3 * KT * 4;       // per item: lo, hi, power of two of Q
   static constexpr int BAR_OFF = ROW_OFF + 2 * 3 * R * 4;
-  static constexpr int USED = BAR_OFF + 512;
+  static constexpr int ITEM_OFF = BAR_OFF + 512;
+  static constexpr int USED = ITEM_OFF + IST * 64;
   static constexpr uint32_t S_COL = 0, O_COL = 256, Q_COL = 384, LO_COL = 448;  // two S of 128 (then P in their place)
 };
 
 struct Bars {
   uint64_t rk_full[KST], rk_empty[KST], rv_full[VST], rv_empty[VST], k_full[2], k_empty[2], sc_full[SCB], sc_empty[SCB], v_full[2], v_empty[2];
-  uint64_t q_full[2], q_empty, rows_empty[2], s_full[2], s_empty[2], p_full[2], pv_done, o_full, o_empty, drain[2];
+  uint64_t item_full[IST], item_empty[IST], q_full[2], q_empty, rows_empty[2], s_full[2], s_empty[2], p_full[2], pv_done, o_full, o_empty, drain[2];
   uint32_t tmem_base;
   int abort;
 };
 static_assert(sizeof(Bars) <= 512, "barrier block");
+
+// An item as warp 3 leaves it.
+struct Record {
+  int h, e, rt, t0, n, s0, s1, rows, tok0, nq, len, kbeg, all, lo, hi, part;  // lo, hi: keys that all rows see; part: item of the list
+};
+constexpr int kReaders = 3 + 8 + 4;  // warps that read it
 
 __device__ __forceinline__ void drain_wait(uint64_t* bar, uint32_t parity) {
   const uint64_t t0 = tc::globaltimer();
@@ -225,6 +233,10 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
       tc::mbar_init(&bars->s_full[s], 1);
       tc::mbar_init(&bars->s_empty[s], 1);  // (P V has read the weights that took the scores' place)
     }
+    for (int s = 0; s < IST; ++s) {
+      tc::mbar_init(&bars->item_full[s], 1);
+      tc::mbar_init(&bars->item_empty[s], kReaders);
+    }
     for (int s = 0; s < KST; ++s) {
       tc::mbar_init(&bars->rk_full[s], 1);
       tc::mbar_init(&bars->rk_empty[s], 4);
@@ -256,11 +268,20 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
   make_plan<R, KT, THREADS / 32>(p, gridDim.x, cum_t, cum_i, head);
   const int64_t all = (int64_t)head[kTotal] * p.n_kv;
   const int64_t x0 = (int64_t)blockIdx.x * head[kPer], x1 = min(all, x0 + head[kPer]);
+  Record* ring = reinterpret_cast<Record*>(smem + L::ITEM_OFF);
+  // The block's i-th item, for a warp that reads them all in turn.
+  auto take = [&](int i, Record& it) -> bool {
+    if (!__all_sync(0xffffffffu, tc::mbar_wait(&bars->item_full[i % IST], (i / IST) & 1, abort, p.status))) return false;
+    it = ring[i % IST];
+    __syncwarp();
+    if (lane == 0) tc::mbar_arrive(&bars->item_empty[i % IST]);
+    return true;
+  };
   // Every role walks the block's items; j counts key tiles and i items over all of them.
   if (warp < 4) {
     fewer_registers<48>();
     if (warp == 0) {  // ---------------- bulk copies
-      int j = 0;
+      int j = 0, i = 0;
       bool ok = true;
       // lane: one of K, its scales, V's scales, V; and a group of keys that lie in one page
       const int kind = lane >> 3, grp = lane & 7, size = p.copy_keys;
@@ -271,13 +292,14 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
       constexpr int ROW = DH * BITS / 8;
       const int row_bytes = kind == 1 || kind == 2 ? 4 : ROW;
       const int off = (kind == 1 ? L::RAW : kind == 2 ? L::RAW + KT * 4 : 0) + grp * size * row_bytes;
-      for (int64_t x = x0; x < x1 && ok;) {
-        const Item it = item_at<R, KT>(p, cum_t, head, x, x1);
-        const int32_t* table = p.pages + (it.en.all ? 0 : (int64_t)(it.e - (p.list.all ? 1 : 0)) * p.max_pages);
+      for (int64_t x = x0; x < x1 && ok; ++i) {
+        Record it;
+        if (!(ok = take(i, it))) break;
+        const int32_t* table = p.pages + (it.all ? 0 : (int64_t)(it.e - (p.list.all ? 1 : 0)) * p.max_pages);
         // Cache row of this lane's group of tile s; -1: past the keys (what is in its place is hidden).
         auto row_of = [&](int s) -> int64_t {
           const int key = (it.t0 + s) * KT + grp * size;
-          if (grp * size >= KT || key >= it.en.len || s >= it.s1) return -1;
+          if (grp * size >= KT || key >= it.len || s >= it.s1) return -1;
           const int pg = p.by_page.quot(key);
           int id = __ldg(table + pg);
           if (id < 0 || id >= p.n_pages) {
@@ -318,7 +340,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
       int j = 0, i = 0;
       bool ok = true;
       for (int64_t x = x0; x < x1 && ok; ++i) {
-        const Item it = item_at<R, KT>(p, cum_t, head, x, x1);
+        Record it;
+        if (!(ok = take(i, it))) break;
         ok = __all_sync(0xffffffffu, tc::mbar_wait(&bars->q_full[i & 1], (i >> 1) & 1, abort, p.status));
         for (int s = it.s0; s < it.s1 && ok; ++s, ++j) {
           ok = __all_sync(0xffffffffu, tc::mbar_wait(&bars->k_full[j & 1], (j >> 1) & 1, abort, p.status) &&
@@ -347,9 +370,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
       int j = 0, i = 0;
       bool ok = true;
       for (int64_t x = x0; x < x1 && ok; ++i) {
-        const Item it = item_at<R, KT>(p, cum_t, head, x, x1);
-        int all_lo, all_hi;
-        seen_by_all(p, it.en, it.rt * R, it.rt * R + it.rows, head, all_lo, all_hi);
+        Record it;
+        if (!(ok = take(i, it))) break;
         ok = __all_sync(0xffffffffu, tc::mbar_wait(&bars->o_empty, (i & 1) ^ 1, abort, p.status));
         for (int s = it.s0; s < it.s1 && ok; ++s, ++j) {
           ok = __all_sync(0xffffffffu, tc::mbar_wait(&bars->v_full[j & 1], (j >> 1) & 1, abort, p.status) &&
@@ -358,7 +380,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
             tc::fence_after_sync();
             const uint64_t vd = tc::sdesc_mnmajor_sw128(tc::smem_u32(smem + L::V_OFF + (j & 1) * L::TILE), L::CHUNK, 1024);
             const int key0 = (it.t0 + s) * KT;
-            const bool masked = key0 < all_lo || key0 + KT > all_hi;
+            const bool masked = key0 < it.lo || key0 + KT > it.hi;
 #pragma unroll
             for (int k = 0; k < KT / 16; ++k)
               tc::umma_f16_ts(tmem + L::O_COL, tmem + L::S_COL + (j & 1) * KT + k * 8, tc::sdesc_advance(vd, k * 16 * 128), IDESC,
@@ -382,6 +404,22 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
         drain_wait(&bars->drain[1], 0);
       }
     }
+    else if (warp == 3) {  // ---------------- items
+      int i = 0;
+      for (int64_t x = x0; x < x1; ++i) {
+        const Item it = item_at<R, KT>(p, cum_t, head, x, x1);
+        Record rec{it.h, it.e, it.rt, it.t0, it.n, it.s0, it.s1, it.rows, it.en.tok0, it.en.nq, it.en.len, it.en.kbeg, it.en.all, 0, 0, 0};
+        seen_by_all(p, it.en, it.rt * R, it.rt * R + it.rows, head, rec.lo, rec.hi);
+        rec.part = it.h * head[kItems] + cum_i[it.e] + it.rt;
+        if (!__all_sync(0xffffffffu, tc::mbar_wait(&bars->item_empty[i % IST], ((i / IST) & 1) ^ 1, abort, p.status))) break;
+        if (lane == 0) {
+          ring[i % IST] = rec;
+          tc::mbar_arrive(&bars->item_full[i % IST]);
+        }
+        __syncwarp();
+        x += it.s1 - it.s0;
+      }
+    }
   } else if (warp < 12) {  // ---------------- softmax
     more_registers<128>();
     const int quarter = warp & 3, g = lane >> 2, q4 = lane & 3;
@@ -390,9 +428,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
     int j = 0, i = 0;
     bool ok = true;
     for (int64_t x = x0; x < x1 && ok; ++i) {
-      const Item it = item_at<R, KT>(p, cum_t, head, x, x1);
-      int all_lo, all_hi;
-      seen_by_all(p, it.en, it.rt * R, it.rt * R + it.rows, head, all_lo, all_hi);
+      Record it;
+      if (!(ok = take(i, it))) break;
       float m[2] = {-INFINITY, -INFINITY};
       float2 l[2] = {};
       if (!(ok = tc::mbar_wait(&bars->q_full[i & 1], (i >> 1) & 1, abort, p.status))) break;  // (the rows' bounds are written before it)
@@ -413,7 +450,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
           break;
         tc::fence_after_sync();
         const int key0 = (it.t0 + s) * KT;
-        const bool masked = key0 < all_lo || key0 + KT > all_hi;
+        const bool masked = key0 < it.lo || key0 + KT > it.hi;
         const uint32_t ts = tw + L::S_COL + (j & 1) * KT;
         // P V of the tile before is done: O may be rescaled and P written
         auto before_p = [&]() -> bool {
@@ -523,7 +560,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
       tc::fence_after_sync();
       // the item's rows: output, or a part
       const bool whole = it.s0 == 0 && it.s1 == it.n && p.shared == 0;
-      const int64_t slot = slot_of(p, blockIdx.x, it.h * head[kItems] + cum_i[it.e] + it.rt, x == x0);
+      const int64_t slot = slot_of(p, blockIdx.x, it.part, x == x0);
       const bool fits = slot < p.list.n_slots;
       if (!whole && !fits) report(p.status, JAB_ERR_INVALID_ARG);
       float inv[2];
@@ -535,7 +572,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
         t += __shfl_xor_sync(0xffffffffu, t, 1);
         t += __shfl_xor_sync(0xffffffffu, t, 2);
         const int r = r0 + g + 8 * c, rr = it.rt * R + r, q = p.by_g.quot(rr), qh = it.h * p.G + rr - q * p.G;
-        const int64_t token = it.en.tok0 + q;
+        const int64_t token = it.tok0 + q;
         live[c] = r < it.rows && (whole || fits);
         inv[c] = whole ? (t == 0.f ? 0.f : 1.f / t) : 1.f;
         out[c] = whole ? token * p.ldo + (int64_t)qh * DH : (slot * R + r) * DH;
@@ -592,15 +629,19 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
       int i = 0, j = 0;
       bool ok = true;
       for (int64_t x = x0; x < x1 && ok; ++i) {
-        const Item it = item_at<R, KT>(p, cum_t, head, x, x1);
+        Record it;
+        if (!(ok = take(i, it))) break;
         // Q of the item, once the products of the one before have read theirs
         if (!(ok = tc::mbar_wait(&bars->q_empty, (i & 1) ^ 1, abort, p.status))) break;
         tc::fence_after_sync();
         {
           const bool live = tid < it.rows;
           int lo = 0, hi = 0;  // (a row past the item's sees no key that a mask could hide: what lies there must not move the references of its warp)
-          const int rr = it.rt * R + tid, q = p.by_g.quot(rr), token = it.en.tok0 + q;
-          if (live) seen_by_row(p, it.en, it.en.all ? position_of(p, token) : it.en.len - it.en.nq + q, lo, hi);
+          const int rr = it.rt * R + tid, q = p.by_g.quot(rr), token = it.tok0 + q;
+          if (live) {
+            const Entry en{it.tok0, it.nq, it.len, it.kbeg, it.all != 0};
+            seen_by_row(p, en, it.all ? position_of(p, token) : it.len - it.nq + q, lo, hi);
+          }
           const uint4* row = reinterpret_cast<const uint4*>(static_cast<const T*>(p.q) + (int64_t)token * p.ldq + (int64_t)(it.h * p.G + rr - q * p.G) * DH);
           float by = 1.f, back = 1.f;
           if constexpr (std::is_same<T, bf16_t>::value) {
