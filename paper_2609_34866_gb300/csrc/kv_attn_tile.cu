@@ -165,6 +165,12 @@ __device__ __forceinline__ void plain_weights(const uint32_t (&v)[32], const flo
   }
 }
 
+__device__ __forceinline__ uint32_t pair_as(float a, float b, half_t) { return tc::pack_half2(a, b); }
+__device__ __forceinline__ uint32_t pair_as(float a, float b, bf16_t) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
 // Whether the row with bounds [lo, hi) sees keys k, k + 1.
 struct Sees {
   bool x, y;
@@ -574,7 +580,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
         const int r = r0 + g + 8 * c, rr = it.rt * R + r, q = p.by_g.quot(rr), qh = it.h * p.G + rr - q * p.G;
         const int64_t token = it.tok0 + q;
         live[c] = r < it.rows && (whole || fits);
-        inv[c] = whole ? (t == 0.f ? 0.f : 1.f / t) : 1.f;
+        inv[c] = t == 0.f ? 0.f : 1.f / t;  // (of a whole item; a part stays as it is)
         out[c] = whole ? token * p.ldo + (int64_t)qh * DH : (slot * R + r) * DH;
         if (live[c] && q4 == 0) {
           if (!whole) p.list.part_ml[slot * R + r] = make_float2(m[c], t);
@@ -587,17 +593,31 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
         __syncwarp();
         tc::tmem_ld_16x256b_x4(tw + L::O_COL + 32 * b, o);
         tc::tmem_ld_wait();
+        if (whole) {
+          // the four lanes of a row exchange their pairs, so that each stores eight columns of its own at once
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int c = k & 1, d = 32 * b + 8 * (k >> 1) + 2 * q4;
-          const float a0 = __uint_as_float(o[2 * k]) * inv[c], a1 = __uint_as_float(o[2 * k + 1]) * inv[c];
-          if (!live[c]) continue;
-          if (whole) {
-            T two[2];
-            store_out(two, a0), store_out(two + 1, a1);
-            *reinterpret_cast<uint32_t*>(static_cast<T*>(p.out) + out[c] + d) = *reinterpret_cast<const uint32_t*>(two);
-          } else {
-            *reinterpret_cast<float2*>(p.list.part_o + out[c] + d) = make_float2(a0, a1);
+          for (int c = 0; c < 2; ++c) {
+            uint32_t w[4];
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+              w[n] = pair_as(__uint_as_float(o[4 * n + 2 * c]) * inv[c], __uint_as_float(o[4 * n + 2 * c + 1]) * inv[c], T());
+#pragma unroll
+            for (int n = 0; n < 4; n += 2) {
+              const uint32_t other = __shfl_xor_sync(0xffffffffu, q4 & 1 ? w[n] : w[n + 1], 1);
+              w[n] = q4 & 1 ? other : w[n], w[n + 1] = q4 & 1 ? w[n + 1] : other;
+            }
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+              const uint32_t other = __shfl_xor_sync(0xffffffffu, q4 & 2 ? w[n] : w[n + 2], 2);
+              w[n] = q4 & 2 ? other : w[n], w[n + 2] = q4 & 2 ? w[n + 2] : other;
+            }
+            if (live[c]) *reinterpret_cast<uint4*>(static_cast<T*>(p.out) + out[c] + 32 * b + 8 * q4) = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const int c = k & 1, d = 32 * b + 8 * (k >> 1) + 2 * q4;
+            if (live[c]) *reinterpret_cast<uint2*>(p.list.part_o + out[c] + d) = make_uint2(o[2 * k], o[2 * k + 1]);
           }
         }
       }
