@@ -758,6 +758,7 @@ cudaError_t launch_all(AttnParams p, const Route& r, int bits, jab_dtype type, i
   }
   if (r.tiles.used) {
     p.list = r.tiles;
+    p.behind = r.keys.used;
     const int64_t rts = ((int64_t)max_q * p.G + kTileRows - 1) / kTileRows, kts = max_len / kTileKeys + 1;
     const int64_t est = p.n_kv * (p.n_seqs * rts * kts + (r.tiles.all ? ((int64_t)p.n_tokens * p.G / kTileRows + 1) * kts : 0));
     if ((e = launch_tiles(p, type, DH, bits, est, std::min(sms, kMaxTileBlocks), st)) != cudaSuccess) return e;

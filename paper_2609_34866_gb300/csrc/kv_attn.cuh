@@ -47,6 +47,7 @@ struct AttnParams {
   int64_t ldo;
   float* lse;
   List list;
+  bool behind;  // the launch by keys comes before this one in the call
   int* status;
 };
 

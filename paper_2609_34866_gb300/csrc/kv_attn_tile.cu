@@ -272,7 +272,13 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
   __syncthreads();
   tc::fence_after_sync();
   const uint32_t tmem = __shfl_sync(0xffffffffu, bars->tmem_base, 0);
-  stream_order();
+  // Behind the launch by keys there is nothing to wait for yet: that one let this one in only when all before it was
+  // complete, and neither reads what the other writes. The joining kernel waits for this one's end, which waits below.
+  // (64 sequences behind 8192 shared keys: 75 us in all one after the other, 67 like this.)
+  if (p.behind)
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  else
+    stream_order();
   make_plan<R, KT, THREADS / 32>(p, gridDim.x, cum_t, cum_i, head);
   const int64_t all = (int64_t)head[kTotal] * p.n_kv;
   const int64_t x0 = (int64_t)blockIdx.x * head[kPer], x1 = min(all, x0 + head[kPer]);
@@ -734,6 +740,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
     __syncwarp();
     tc::tmem_dealloc(tmem, 512);
   }
+  if (p.behind) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 template <class T, int DH, int BITS>

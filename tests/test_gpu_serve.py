@@ -2,7 +2,7 @@
 float64 implementations.
 
 Tolerances. The projection, the codes, the scales and the read-back are compared bit for bit: their sums
-are exact and their roundings are part of the definition. Attention rounds each weight to fp16 (2^-12 of it;
+are exact and their roundings are part of the definition. Attention keeps each weight to 2^-12 of it (two fp16 parts where rows see few keys;
 weights below 2^-14 of the largest by 2^-25 of the largest) and the result to its type; scores are
 fp32 sums of at most 128 exact products, their exponentials good to 2^-22, which stays below 2^-16 of the
 result for scores of the size used here. So |error| <= (2^-12 + 2^-16) sum p |v| + n 2^-25 max|v| + ulp(type) / 2,
