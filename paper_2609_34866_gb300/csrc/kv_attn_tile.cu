@@ -50,7 +50,7 @@ struct Layout {
 
 struct Bars {
   uint64_t rk_full[KST], rk_empty[KST], rv_full[VST], rv_empty[VST], k_full[2], k_empty[2], sc_full[SCB], sc_empty[SCB], v_full[2], v_empty[2];
-  uint64_t item_full[IST], item_empty[IST], q_full[2], q_empty, rows_empty[2], s_full[2], s_empty[2], p_full[2], pv_done, o_full, o_empty, drain[2];
+  uint64_t item_full[IST], item_empty[IST], q_full[2], q_empty, rows_empty[2], s_full[2], s_empty[2], p_full[2], pv_done[2], o_full, o_empty, drain[2];
   uint32_t tmem_base;
   int abort;
 };
@@ -236,6 +236,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
       tc::mbar_init(&bars->q_full[s], 4);
       tc::mbar_init(&bars->rows_empty[s], 8);
       tc::mbar_init(&bars->p_full[s], 8);
+      tc::mbar_init(&bars->pv_done[s], 1);
       tc::mbar_init(&bars->v_full[s], 4);
       tc::mbar_init(&bars->v_empty[s], 1);
       tc::mbar_init(&bars->s_full[s], 1);
@@ -258,7 +259,6 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
       tc::mbar_init(&bars->sc_empty[s], 8);
     }
     tc::mbar_init(&bars->q_empty, 1);
-    tc::mbar_init(&bars->pv_done, 1);
     tc::mbar_init(&bars->o_full, 1);
     tc::mbar_init(&bars->o_empty, 8);
     bars->abort = 0;
@@ -404,7 +404,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
               for (int k = 0; k < KT / 16; ++k)
                 tc::umma_f16_ts(tmem + L::O_COL, tmem + L::LO_COL + k * 8, tc::sdesc_advance(vd, k * 16 * 128), IDESC, 1u);
             }
-            tc::umma_commit(&bars->pv_done);
+            tc::umma_commit(&bars->pv_done[j & 1]);
             tc::umma_commit(&bars->s_empty[j & 1]);
             tc::umma_commit(&bars->v_empty[j & 1]);
             if (s + 1 == it.s1) tc::umma_commit(&bars->o_full);
@@ -468,7 +468,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
         const uint32_t ts = tw + L::S_COL + (j & 1) * KT;
         // P V of the tile before is done: O may be rescaled and P written
         auto before_p = [&]() -> bool {
-          if (j > 0 && !tc::mbar_wait(&bars->pv_done, (j - 1) & 1, abort, p.status)) return false;
+          if (j > 0 && !tc::mbar_wait(&bars->pv_done[(j - 1) & 1], ((j - 1) >> 1) & 1, abort, p.status)) return false;
           tc::fence_after_sync();
           __syncwarp();
           return true;
