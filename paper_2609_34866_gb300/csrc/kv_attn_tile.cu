@@ -8,9 +8,9 @@
 // Both products are M128 N128 with their A operand in tensor memory:
 //   S = Q K^T   A = Q (fp16, written to tensor memory row by row), B = K as converted (K-major)
 //   O += P V    A = P (fp16 weights, written by the softmax), B = V as converted (MN-major: the same layout)
-// In key tiles that a mask cuts, P is its fp16 value and what that leaves over, in two products: rows that see few
-// keys (the first of a sequence, narrow windows) have them in such tiles, and one rounding of a weight would
-// show. In the others a weight is rounded once (2^-11 of it at most, over 128 keys and more).
+// P is its fp16 value and what that leaves over (2^-22 of a weight in all), in two products, as in the kernel by
+// keys: rounded once, a weight would be 2^-11 off, and what a token gets would hang on which of the two kernels its
+// batch brings it to.
 //   warp 0        bulk copies of codes and scales, rings of KST and VST tiles
 //   warp 1        tensor memory owner; issues S, a tile ahead of P V;   warp 2  issues P V
 //   warp 3        finds the block's items, ahead of all, and leaves them in a ring (each warp for itself: 1 to 2 us an item)
@@ -45,7 +45,8 @@ struct Layout {
   static constexpr int BAR_OFF = ROW_OFF + 2 * 3 * R * 4;
   static constexpr int ITEM_OFF = BAR_OFF + 512;
   static constexpr int USED = ITEM_OFF + IST * 64;
-  static constexpr uint32_t S_COL = 0, O_COL = 256, Q_COL = 384, LO_COL = 448;  // two S of 128 (then P in their place)
+  // Two S of 128 columns. P takes their place, 64 keys at a time: 32 columns of fp16 pairs, 32 of what they leave over.
+  static constexpr uint32_t S_COL = 0, O_COL = 256, Q_COL = 384;
 };
 
 struct Bars {
@@ -145,26 +146,40 @@ __device__ __forceinline__ void scale_rows(uint32_t taddr, const float (&f)[2]) 
   tc::tmem_st_wait();
 }
 
-// Weights of keys that no mask hides, as fp16 pairs, and the row sums of 2^y; `big` has the largest weight of either
-// half of the pairs. As long as none passes 2^15 the reference may stay, and neither the maximum nor the V scales'
-// logarithms are needed.
+// A pair of weights as fp16, and what that leaves over.
+__device__ __forceinline__ void two_parts(float2 w, uint32_t& h, uint32_t& r) {
+  h = tc::pack_half2(w.x, w.y);
+  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
+  r = tc::pack_half2(w.x - f.x, w.y - f.y);
+}
+
+// Weights of keys that no mask hides, in the scores' place: v[4n + 2c] becomes the pair in fp16, v[4n + 2c + 1] what
+// that leaves over; l gets the row sums of 2^y, `big` the largest weight of either half of the pairs. As long as none
+// passes 2^15 the reference may stay, and neither the maximum nor the V scales' logarithms are needed.
 template <class T>
-__device__ __forceinline__ void plain_weights(const uint32_t (&v)[32], const float* sc, const float (&ref)[2], const float (&fac)[2], float2 (&l)[2],
-                                              uint32_t (&hi2)[16], uint32_t& big) {
+__device__ __forceinline__ void plain_weights(uint32_t (&v)[32], const float* sc, const float (&ref)[2], const float (&fac)[2], float2 (&l)[2], uint32_t& big) {
   big = 0;
 #pragma unroll
   for (int n = 0; n < 8; ++n) {
     const float2 ks = *reinterpret_cast<const float2*>(sc + 8 * n), vs = *reinterpret_cast<const float2*>(sc + KT + 8 * n);
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-      const float2 y = score<T>(v + 4 * n + 2 * c, ks, fac[c], ref[c]);
+      uint32_t* e = v + 4 * n + 2 * c;
+      const float2 y = score<T>(e, ks, fac[c], ref[c]);
       const float2 ex = make_float2(tc::fast_exp2(y.x), tc::fast_exp2(y.y));
       l[c] = tc::add2(l[c], ex);
-      const float2 w = tc::mul2(ex, vs);
-      hi2[2 * n + c] = tc::pack_half2(w.x, w.y);
-      big = __vmaxu2(big, hi2[2 * n + c]);
+      two_parts(tc::mul2(ex, vs), e[0], e[1]);
+      big = __vmaxu2(big, e[0]);
     }
   }
+}
+
+// Stores 64 keys' weights as plain_weights and masked_weights leave them.
+__device__ __forceinline__ void store_weights(uint32_t taddr, const uint32_t (&v)[32]) {
+  uint32_t w[32];
+#pragma unroll
+  for (int k = 0; k < 16; ++k) w[k] = v[2 * k], w[16 + k] = v[2 * k + 1];
+  tc::tmem_st_16x128b_x16(taddr, w);
 }
 
 __device__ __forceinline__ uint32_t pair_as(float a, float b, half_t) { return tc::pack_half2(a, b); }
@@ -208,10 +223,7 @@ __device__ __forceinline__ void masked_weights(uint32_t (&v)[32], const float* s
       const Sees see(k0 + 8 * n, lo[c], hi[c]);
       const float2 ex = make_float2(see.x ? tc::fast_exp2(y.x) : 0.f, see.y ? tc::fast_exp2(y.y) : 0.f);
       l[c] = tc::add2(l[c], ex);
-      const float2 w = make_float2(see.x ? ex.x * vs.x : 0.f, see.y ? ex.y * vs.y : 0.f);
-      const uint32_t h = tc::pack_half2(w.x, w.y);
-      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
-      e[0] = h, e[1] = tc::pack_half2(w.x - f.x, w.y - f.y);
+      two_parts(make_float2(see.x ? ex.x * vs.x : 0.f, see.y ? ex.y * vs.y : 0.f), e[0], e[1]);
     }
   }
 }
@@ -393,17 +405,12 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
           if (ok && tc::elect_one()) {
             tc::fence_after_sync();
             const uint64_t vd = tc::sdesc_mnmajor_sw128(tc::smem_u32(smem + L::V_OFF + (j & 1) * L::TILE), L::CHUNK, 1024);
-            const int key0 = (it.t0 + s) * KT;
-            const bool masked = key0 < it.lo || key0 + KT > it.hi;
 #pragma unroll
-            for (int k = 0; k < KT / 16; ++k)
-              tc::umma_f16_ts(tmem + L::O_COL, tmem + L::S_COL + (j & 1) * KT + k * 8, tc::sdesc_advance(vd, k * 16 * 128), IDESC,
-                              s > it.s0 || k > 0 ? 1u : 0u);
-            if (masked) {
+            for (int part = 0; part < 2; ++part)
 #pragma unroll
               for (int k = 0; k < KT / 16; ++k)
-                tc::umma_f16_ts(tmem + L::O_COL, tmem + L::LO_COL + k * 8, tc::sdesc_advance(vd, k * 16 * 128), IDESC, 1u);
-            }
+                tc::umma_f16_ts(tmem + L::O_COL, tmem + L::S_COL + (j & 1) * KT + (k >> 2) * 64 + part * 32 + (k & 3) * 8, tc::sdesc_advance(vd, k * 16 * 128),
+                                IDESC, s > it.s0 || part > 0 || k > 0 ? 1u : 0u);
             tc::umma_commit(&bars->pv_done[j & 1]);
             tc::umma_commit(&bars->s_empty[j & 1]);
             tc::umma_commit(&bars->v_empty[j & 1]);
@@ -466,8 +473,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
         const int key0 = (it.t0 + s) * KT;
         const bool masked = key0 < it.lo || key0 + KT > it.hi;
         const uint32_t ts = tw + L::S_COL + (j & 1) * KT;
-        // P V of the tile before is done: O may be rescaled and P written
-        auto before_p = [&]() -> bool {
+        // P V of the tile before is done: O may be rescaled
+        auto before_o = [&]() -> bool {
           if (j > 0 && !tc::mbar_wait(&bars->pv_done[(j - 1) & 1], ((j - 1) >> 1) & 1, abort, p.status)) return false;
           tc::fence_after_sync();
           __syncwarp();
@@ -478,17 +485,19 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
         if (!masked && !__any_sync(0xffffffffu, m[0] == -INFINITY || m[1] == -INFINITY)) {
 #pragma unroll 1
           for (int b = 0; b < 2; ++b) {
-            uint32_t v[32], h[16], big;
+            uint32_t v[32], big;
             __syncwarp();
             tc::tmem_ld_16x256b_x8(ts + 64 * b, v);
             tc::tmem_ld_wait();
             float2 sum[2] = {l[0], l[1]};
-            plain_weights<T>(v, sc + 64 * b, m, fac, sum, h, big);
+            plain_weights<T>(v, sc + 64 * b, m, fac, sum, big);
             if (__any_sync(0xffffffffu, either_at_least(big, 0x7800u))) {
               // The maximum has to move, by a whole power of two: what is there of this tile's weights, of O and of the
               // sums goes down by it, and the 64 weights are taken again.
               float top[2] = {-INFINITY, -INFINITY}, f[2];
               const int lo_[2] = {0, 0}, hi_[2] = {INT32_MAX, INT32_MAX};
+              tc::tmem_ld_16x256b_x8(ts + 64 * b, v);
+              tc::tmem_ld_wait();
               masked_top<T>(v, sc + 64 * b, fac, lo_, hi_, 0, top);
 #pragma unroll
               for (int c = 0; c < 2; ++c) {
@@ -499,24 +508,25 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
                 m[c] += up;
                 l[c].x *= f[c], l[c].y *= f[c];
               }
-              if (!(ok = before_p())) break;
+              if (!(ok = before_o())) break;
               if (s > it.s0) scale_rows<DH>(tw + L::O_COL, f);
-              if (b > 0) {
+#pragma unroll 1
+              for (int part = 0; part < 2 * b; ++part) {
                 uint32_t e[16];
-                tc::tmem_ld_16x128b_x8(ts, e);
+                tc::tmem_ld_16x128b_x8(ts + 32 * part, e);
                 tc::tmem_ld_wait();
 #pragma unroll
                 for (int k = 0; k < 16; ++k) {
                   const float2 w = __half22float2(*reinterpret_cast<const __half2*>(&e[k]));
                   e[k] = tc::pack_half2(w.x * f[k & 1], w.y * f[k & 1]);
                 }
-                tc::tmem_st_16x128b_x8(ts, e);
+                tc::tmem_st_16x128b_x8(ts + 32 * part, e);
               }
               sum[0] = l[0], sum[1] = l[1];
-              plain_weights<T>(v, sc + 64 * b, m, fac, sum, h, big);
+              plain_weights<T>(v, sc + 64 * b, m, fac, sum, big);
             }
             l[0] = sum[0], l[1] = sum[1];
-            tc::tmem_st_16x128b_x8(ts + 32 * b, h);
+            store_weights(ts + 64 * b, v);
           }
           if (!ok) break;
         } else {  // a mask, or the item's first tile: the rows' maxima first
@@ -530,7 +540,6 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
             tc::tmem_ld_wait();
             masked_top<T>(v, sc + 64 * b, fac, lo_, hi_, key0 + 64 * b + 2 * q4, top);
           }
-          if (!(ok = before_p())) break;
           const bool grow = (m[0] == -INFINITY && top[0] > -INFINITY) || top[0] > m[0] + 8.f || (m[1] == -INFINITY && top[1] > -INFINITY) ||
                             top[1] > m[1] + 8.f;
           if (__any_sync(0xffffffffu, grow)) {
@@ -545,6 +554,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
               m[c] = t;
               l[c].x *= f[c], l[c].y *= f[c];
             }
+            if (!(ok = before_o())) break;
             if (s > it.s0) scale_rows<DH>(tw + L::O_COL, f);
           }
           const float ref[2] = {m[0] == -INFINITY ? 0.f : m[0], m[1] == -INFINITY ? 0.f : m[1]};
@@ -555,11 +565,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
             tc::tmem_ld_16x256b_x8(ts + 64 * b, v);
             tc::tmem_ld_wait();
             masked_weights<T>(v, sc + 64 * b, ref, fac, lo_, hi_, key0 + 64 * b + 2 * q4, l);
-            uint32_t h[16], r[16];
-#pragma unroll
-            for (int k = 0; k < 16; ++k) h[k] = v[2 * k], r[k] = v[2 * k + 1];
-            tc::tmem_st_16x128b_x8(ts + 32 * b, h);
-            if (masked) tc::tmem_st_16x128b_x8(tw + L::LO_COL + 32 * b, r);
+            store_weights(ts + 64 * b, v);
           }
         }
         tc::tmem_st_wait();

@@ -1,0 +1,98 @@
+"""The serving operators over their whole ranges: calls whose blocks go round their loops more than once, values at
+the edges of what the kernels hold, and inputs that have to be reported. Everything against plain float64
+implementations (serve_ref.py); the projection, codes, scales and read-back bit for bit."""
+import math
+
+import pytest
+import torch
+
+import serve_ref as R
+from test_gpu_serve import HALF_ULP, _filled, _gen, _linear, _pages
+
+pytestmark = pytest.mark.gpu
+
+import paper_2609_34866_gb300 as J  # noqa: E402
+
+
+@pytest.fixture(autouse=True)
+def _status():
+    J.jab_get_device_status()
+    yield
+    torch.cuda.synchronize()
+
+
+def _attention(cache, q, q_lens, lens, pages, shared=0, window=0, max_q=None, max_len=None, scale=0.0):
+    """(out, lse) of a call."""
+    n, hq, _ = q.shape
+    max_q, max_len = max_q or max(q_lens), max_len or max(lens)
+    start = torch.tensor([0] + list(torch.tensor(q_lens).cumsum(0)), dtype=torch.int32, device="cuda")
+    out, lse = torch.full_like(q, 77.0), torch.full((n, hq), 77.0, device="cuda")
+    ws = torch.full((J.jab_kv_attention_workspace_size(cache, len(lens), n, hq, max_q, max_len, shared),), 0xFF, dtype=torch.uint8,
+                    device="cuda")
+    J.jab_kv_attention(cache, q, start, pages, torch.tensor(lens, dtype=torch.int32, device="cuda"), out, ws, max_q, max_len,
+                       shared_len=shared, window=window, softmax_scale=scale, lse=lse)
+    return out, lse
+
+
+def _exact(cache, kd, vd, q, q_lens, lens, pages, window=0, scale=0.0):
+    """Per (token, head) in float64: o, log-sum-exp, sum p |v|, the longest row, and the largest p_j max|v_j|."""
+    n, hq, dh = q.shape
+    page, hkv, at = cache.page_tokens, cache.n_kv_heads, 0
+    f64 = dict(dtype=torch.float64, device="cuda")
+    o, mag = torch.zeros((n, hq, dh), **f64), torch.zeros((n, hq, dh), **f64)
+    lse, top, keys = torch.full((n, hq), -math.inf, **f64), torch.zeros((n, hq, 1), **f64), torch.zeros((n, hq, 1), **f64)
+    for b, (nq, length) in enumerate(zip(q_lens, lens)):
+        j = torch.arange(length, device="cuda")
+        ids = pages[b].long()[j // page]
+        k, v = kd[ids, j % page], vd[ids, j % page]
+        pos = torch.arange(length - nq, length, device="cuda")[:, None]
+        seen = (j <= pos) & ((j > pos - window) if window else torch.ones_like(j <= pos))
+        rows = slice(at, at + nq)
+        for h in range(hq):
+            kh, vh = k[:, h // (hq // hkv)], v[:, h // (hq // hkv)]
+            s = (q[rows, h].double() @ kh.t() * (scale or 1 / math.sqrt(dh))).masked_fill(~seen, -math.inf)
+            ls = torch.logsumexp(s, -1)
+            p = torch.where(seen, torch.exp(s - torch.where(ls > -math.inf, ls, 0.0)[:, None]), 0.0)
+            o[rows, h], mag[rows, h], lse[rows, h] = p @ vh, p @ vh.abs(), ls
+            if length:
+                top[rows, h, 0] = (p * vh.abs().amax(-1)).amax(-1)
+            keys[rows, h, 0] = seen.sum(-1).double()
+        at += nq
+    return o, lse, mag, keys, top
+
+
+def _held(out, want, o, rel, floor):
+    tol = rel + floor + HALF_ULP[out.dtype] * o.abs() + 1e-30
+    err = (out.double() - want).abs()
+    assert bool((err <= tol).all()), (err / tol).max().item()
+
+
+def _lse_held(lse, want):
+    fin = torch.isfinite(want)
+    assert bool((lse[~fin].double() == want[~fin]).all())
+    assert bool(((lse.double() - want).abs()[fin] <= 2.0 ** -16 + 2.0 ** -21 * want.abs()[fin]).all()), (lse.double() - want).abs()[fin].max().item()
+
+
+# ------------------------------------------------------------------ attention: bits of the weights
+# A weight is an fp16 number and what that leaves over: within 2^-22 of it, or 2^-25 where that is more (twice that
+# after the reference has moved). The largest of a row, p_a v_a, is at least 2^-1 as held, so that the second is at
+# most 2^-23 p_a v_a of the result a key. Scores up to 10 in magnitude are within 2^-16 (eight truncated fp32 sums and
+# their exponential), and two truncated products for 16 keys lose 2^-26 of the result a key.
+@pytest.mark.parametrize("q_lens,lens,shared,window", [
+    ([300, 77], [1000, 900], 0, 0),
+    ([40], [513], 0, 0),
+    ([260, 33], [1700, 500], 0, 400),
+    ([1] * 40, [520 + 7 * i for i in range(40)], 512, 0),
+])
+@pytest.mark.parametrize("dh,hq,hkv,bits,dt", [(128, 8, 2, 8, torch.float16), (64, 4, 4, 4, torch.float16), (128, 6, 2, 4, torch.bfloat16)])
+def test_weights_keep_their_bits_in_every_tile(q_lens, lens, shared, window, dh, hq, hkv, bits, dt):
+    g = _gen(sum(lens) + dh + bits)
+    page = 64
+    cache, kd, vd = _filled(g, hkv, dh, bits, page, sum(-(-max(n, shared) // page) for n in lens) + 3)
+    q = (torch.randn((sum(q_lens), hq, dh), generator=g, device="cuda") * 2).to(dt)
+    pages = _pages(g, [max(n, shared) for n in lens], page, cache.n_pages, shared)
+    out, lse = _attention(cache, q, q_lens, lens, pages, shared, window)
+    assert J.jab_get_device_status() == 0
+    o, ls, mag, keys, top = _exact(cache, kd, vd, q, q_lens, lens, pages, window)
+    _held(out, o, o, (2.0 ** -22 + 2.0 ** -16 + keys * 2.0 ** -26) * mag, keys * 2.0 ** -23 * top)
+    _lse_held(lse, ls)
