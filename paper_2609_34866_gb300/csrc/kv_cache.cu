@@ -125,8 +125,9 @@ __device__ __forceinline__ float largest(float a, float b, float c) {
 // the next token's angles and the slot and position of the one after are under way while a row is worked on. Long inputs
 // are bound by instructions as much as by bytes: with a grid-stride loop over rows, its 64-bit divisions and a division of
 // every element, 8 x 2048 tokens of 48 heads of 128 (370 MB) took 108 us, with a token a block and no row ahead 90, like this 67 (5.5 TB/s).
+constexpr int kWriteThreads = 384;  // of a block, at most
 template <class T, int DH, int BITS>
-__global__ void __launch_bounds__(384, sizeof(T) == 2 ? 2 : 1) kv_write_kernel(const __grid_constant__ WriteParams p) {
+__global__ void __launch_bounds__(kWriteThreads, sizeof(T) == 2 ? 2 : 1) kv_write_kernel(const __grid_constant__ WriteParams p) {
   constexpr int LANES = DH / 16;
   stream_order();
   const int t = threadIdx.x % LANES, head0 = threadIdx.x / LANES, heads = blockDim.x / LANES;
@@ -291,12 +292,12 @@ __global__ void __launch_bounds__(256) kv_read_kernel(const __grid_constant__ Re
 
 template <class T, int DH, int BITS>
 cudaError_t write_as(const WriteParams& p, int sms, cudaStream_t st) {
-  // A block has a token's heads, or as many of them as 384 threads take. With four tokens for every SM and more, a
-  // third of that where it leaves no thread idle: it loads a token's angles once for its rows in turn (2048 tokens of 48
+  // A block has a token's heads, or as many of them as kWriteThreads threads take. With four tokens for every SM and more, a
+  // third of the heads where that leaves no thread idle: it loads a token's angles once for its rows in turn (2048 tokens of 48
   // heads of 128: 19 us for writing and reading, 22 without; but 64 tokens 4.9 instead of 4.5).
   constexpr int PER_SM = sizeof(T) == 2 ? 768 : 512;
-  const int want = p.n_heads * (DH / 16), limit = p.n_tokens >= 4 * (int64_t)sms && want % 96 == 0 ? want / 3 : 384;
-  const int threads = (std::min(want, limit) + 31) / 32 * 32;
+  const int want = p.n_heads * (DH / 16), share = p.n_tokens >= 4 * (int64_t)sms && want % 96 == 0 ? want / 3 : want;
+  const int threads = (std::min(share, kWriteThreads) + 31) / 32 * 32;
   const int64_t blocks = std::min<int64_t>(p.n_tokens, (int64_t)sms * std::min(32, std::max(1, PER_SM / threads)));
   return launch_after(kv_write_kernel<T, DH, BITS>, (unsigned)blocks, threads, 0, st, p);
 }

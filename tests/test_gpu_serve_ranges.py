@@ -96,3 +96,41 @@ def test_weights_keep_their_bits_in_every_tile(q_lens, lens, shared, window, dh,
     o, ls, mag, keys, top = _exact(cache, kd, vd, q, q_lens, lens, pages, window)
     _held(out, o, o, (2.0 ** -22 + 2.0 ** -16 + keys * 2.0 ** -26) * mag, keys * 2.0 ** -23 * top)
     _lse_held(lse, ls)
+
+
+# ------------------------------------------------------------------ cache
+def _write_check(n, hq, hkv, dh, bits, page, dt, rope):
+    g = _gen(n + hq + dh + bits)
+    n_pages = -(-n // page) + 2
+    qkv = torch.randn((n, (hq + 2 * hkv) * dh), generator=g, device="cuda").to(dt)
+    slots = torch.randperm(n_pages * page, generator=g, device="cuda")[:n].clone()
+    slots[::7] = -1
+    qkv[::7] = math.nan  # padding: not read
+    cache = J.KvCache(hkv, dh, bits, page, n_pages)
+    cos = sin = pos = None
+    if rope:
+        cos, sin = (torch.empty((777, dh // 2), device="cuda") for _ in range(2))
+        J.jab_rope_table(cos, sin, 10000.0)
+        pos = torch.randint(0, 777, (n,), generator=g, device="cuda").int()
+    q_out = torch.full((n, hq * dh), 9.0, dtype=dt, device="cuda") if hq else None
+    J.jab_kv_write(cache, qkv, hq, slots, q_out=q_out, positions=pos, rope=(cos, sin) if rope else None)
+    assert J.jab_get_device_status() == 0
+    live = slots >= 0
+    x = qkv.float().view(n, hq + 2 * hkv, dh)[live]
+    turned = R.rotate(x[:, : hq + hkv], cos[pos[live].long()], sin[pos[live].long()]) if rope else x[:, : hq + hkv]
+    if hq:
+        assert torch.equal(q_out[live], turned[:, :hq].reshape(-1, hq * dh).to(dt)) and bool((q_out[~live] == 9).all())
+    pg, at = slots[live] // page, slots[live] % page
+    for rows, codes, scales in ((turned[:, hq:], cache.k_codes, cache.k_scales), (x[:, hq + hkv:], cache.v_codes, cache.v_scales)):
+        c, s = R.quantize_rows(rows, bits)
+        assert torch.equal(scales[pg, :, at], s) and torch.equal(codes[pg, :, at], R.pack(c, bits))
+
+
+@pytest.mark.parametrize("hq,hkv,dh", [(64, 64, 128), (52, 52, 128), (104, 104, 64), (160, 16, 128)])
+@pytest.mark.parametrize("few", [True, False])
+def test_write_of_wide_blocks(hq, hkv, dh, few):
+    """More heads than a block's threads: few tokens, and four for every SM and more."""
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    for n in (4 * sms - 1,) if few else (4 * sms, 700):
+        for dt, bits in ((torch.float16, 8), (torch.bfloat16, 4), (torch.float32, 8)):
+            _write_check(n, hq, hkv, dh, bits, 32, dt, True)
