@@ -206,12 +206,12 @@ __device__ __forceinline__ float load_q(const T* row, int q, bool live, uint32_t
 template <int NS, int NT, int MT, bool MASKED>
 __device__ __forceinline__ void softmax_step(float (&s)[NS][NT][4], const float2 (&sc)[NS][2], const float (&fac)[NT][2], int key, const int (&lo)[NT][2],
                                              const int (&hi)[NT][2], float (&m)[NT][2], float (&l)[NT][2], float (&o)[NT][MT][4], uint32_t (&pb)[NS][NT][4]) {
-  float lv[NS][2];  // exponents of the V scales (2^lv <= scale < 2^(lv + 1)); a row of zeros counts as one of 2^-100
+  float lv[NS][2];  // exponents of the V scales (2^lv <= scale < 2^(lv + 1))
 #pragma unroll
   for (int n = 0; n < NS; ++n)
 #pragma unroll
     for (int i = 0; i < 2; ++i)
-      lv[n][i] = fmaxf(__uint_as_float((__float_as_uint(sc[n][i].y) >> 23) | 0x4b000000u) - 8388735.f, -100.f);
+      lv[n][i] = fmaxf(__uint_as_float((__float_as_uint(sc[n][i].y) >> 23) | 0x4b000000u) - 8388735.f, kLeastLog2);
 #pragma unroll
   for (int j = 0; j < NT; ++j) {
     bool see[NS][4];

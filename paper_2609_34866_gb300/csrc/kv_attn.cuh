@@ -282,6 +282,11 @@ __device__ __forceinline__ int64_t slot_of(const AttnParams& p, int worker, int 
   return p.shared > 0 ? (int64_t)worker + item : 2 * (int64_t)worker + (first ? 0 : 1);
 }
 
+// log2 of the least V scale that the running maxima know: one below it (a row of zeros) counts as this. Such a key's
+// weight is small whatever its score is, its 2^(s - m) is not: like this, that is at most 2^98 when the maximum follows
+// from 2^8 on, and the sums of 2^29 of them are finite.
+constexpr float kLeastLog2 = -90.f;
+
 // 2^(a - b) with 2^(-inf - -inf) = 0.
 __device__ __forceinline__ float shift2(float a, float b) { return a == -INFINITY ? 0.f : exp2f(a - b); }
 

@@ -155,7 +155,9 @@ __device__ __forceinline__ void two_parts(float2 w, uint32_t& h, uint32_t& r) {
 
 // Weights of keys that no mask hides, in the scores' place: v[4n + 2c] becomes the pair in fp16, v[4n + 2c + 1] what
 // that leaves over; l gets the row sums of 2^y, `big` the largest weight of either half of the pairs. As long as none
-// passes 2^15 the reference may stay, and neither the maximum nor the V scales' logarithms are needed.
+// passes 2^15 and no sum 2^112 the reference may stay, and neither the maximum nor the V scales' logarithms are
+// needed. (The sums: a key whose values are zero has no weight, however far its score is ahead. Once the reference has
+// moved its 2^y is at most 2^90, and a sum has room for 2^22 more of them.)
 template <class T>
 __device__ __forceinline__ void plain_weights(uint32_t (&v)[32], const float* sc, const float (&ref)[2], const float (&fac)[2], float2 (&l)[2], uint32_t& big) {
   big = 0;
@@ -173,6 +175,8 @@ __device__ __forceinline__ void plain_weights(uint32_t (&v)[32], const float* sc
     }
   }
 }
+
+__device__ __forceinline__ bool sums_fit(const float2 (&l)[2]) { return fmaxf(fmaxf(l[0].x, l[0].y), fmaxf(l[1].x, l[1].y)) < 5.192297e33f; }
 
 // Stores 64 keys' weights as plain_weights and masked_weights leave them.
 __device__ __forceinline__ void store_weights(uint32_t taddr, const uint32_t (&v)[32]) {
@@ -491,7 +495,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
             tc::tmem_ld_wait();
             float2 sum[2] = {l[0], l[1]};
             plain_weights<T>(v, sc + 64 * b, m, fac, sum, big);
-            if (__any_sync(0xffffffffu, either_at_least(big, 0x7800u))) {
+            if (__any_sync(0xffffffffu, either_at_least(big, 0x7800u) || !sums_fit(sum))) {
               // The maximum has to move, by a whole power of two: what is there of this tile's weights, of O and of the
               // sums goes down by it, and the 64 weights are taken again.
               float top[2] = {-INFINITY, -INFINITY}, f[2];
@@ -727,7 +731,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
           const float vs = scales[KT + tid];
           sc[tid] = scales[tid] * p.scale_log2;
           sc[KT + tid] = vs;
-          sc[2 * KT + tid] = vs > 0.f ? __log2f(vs) : vs == 0.f ? -100.f : vs;  // (a row of zeros counts as one of 2^-100)
+          sc[2 * KT + tid] = vs > 0.f ? fmaxf(__log2f(vs), kLeastLog2) : vs == 0.f ? kLeastLog2 : vs;
           convert_tile<DH, BITS>(raw, smem + L::K_OFF + (j & 1) * L::TILE, tid);
           done(&bars->k_full[j & 1]);
           if (lane == 0) {

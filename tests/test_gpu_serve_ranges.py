@@ -61,6 +61,26 @@ def _exact(cache, kd, vd, q, q_lens, lens, pages, window=0, scale=0.0):
     return o, lse, mag, keys, top
 
 
+def _one_ahead(dh, bits, page, length):
+    """A cache whose key 0 is 1 everywhere, all others 0; values 1, of key 0 every other one 0."""
+    n_pages = -(-length // page)
+    cache = J.KvCache(1, dh, bits, page, n_pages)
+    zero, top = (128, 127) if bits == 8 else (8, 7)
+    full = zero + top
+    cache.k_codes.fill_(zero if bits == 8 else zero * 17)
+    cache.v_codes.fill_(full if bits == 8 else full * 17)
+    cache.k_scales.fill_(1.0 / top)
+    cache.v_scales.fill_(1.0 / top)
+    cache.k_codes[0, 0, 0] = full if bits == 8 else full * 17
+    if bits == 8:
+        cache.v_codes[0, 0, 0, 1::2] = zero
+    else:
+        cache.v_codes[0, 0, 0] = full + 16 * zero
+    kd = R.unpack(cache.k_codes, bits) * cache.k_scales.double()[..., None]
+    vd = R.unpack(cache.v_codes, bits) * cache.v_scales.double()[..., None]
+    return cache, kd.transpose(1, 2), vd.transpose(1, 2), torch.arange(n_pages, dtype=torch.int32, device="cuda").view(1, -1)
+
+
 def _held(out, want, o, rel, floor):
     tol = rel + floor + HALF_ULP[out.dtype] * o.abs() + 1e-30
     err = (out.double() - want).abs()
@@ -95,6 +115,44 @@ def test_weights_keep_their_bits_in_every_tile(q_lens, lens, shared, window, dh,
     assert J.jab_get_device_status() == 0
     o, ls, mag, keys, top = _exact(cache, kd, vd, q, q_lens, lens, pages, window)
     _held(out, o, o, (2.0 ** -22 + 2.0 ** -16 + keys * 2.0 ** -26) * mag, keys * 2.0 ** -23 * top)
+    _lse_held(lse, ls)
+
+
+# ------------------------------------------------------------------ attention: values of zero, NaN
+# (Many sequences, here of the same pages, so that a share of the work has several key tiles of a row in turn.)
+@pytest.mark.parametrize("nq,B", [(1, 2048), (40, 400)])
+@pytest.mark.parametrize("ahead", [60.0, 83.0, 88.0, 300.0])
+def test_keys_far_ahead_whose_values_are_zero(nq, B, ahead):
+    """Their scores alone decide the log-sum-exp; their weights are 0 whatever the scores are."""
+    dh, page, length = 64, 64, 700
+    cache, kd, vd, pages = _one_ahead(dh, 8, page, length)
+    cache.k_codes[0, 0, 0], cache.v_codes[0, 0, 0] = 128, 255
+    cache.k_codes[4], cache.v_codes[4] = 255, 128  # keys 256 to 319, in a tile that no mask cuts
+    cache.v_scales[4] = 0.0
+    kd[0, 0], kd[4], vd[0, 0], vd[4] = 0, 1, 1, 0
+    q = torch.ones((nq, 2, dh), device="cuda").to(torch.float16)
+    out, lse = _attention(cache, q.repeat(B, 1, 1), [nq] * B, [length] * B, pages.repeat(B, 1), scale=ahead / dh)
+    assert J.jab_get_device_status() == 0
+    o, ls, mag, keys, top = _exact(cache, kd, vd, q, [nq], [length], pages, scale=ahead / dh)
+    _held(out.view(B, nq, 2, dh), o, o, 2.0 ** -10 * mag, 2.0 ** -60)
+    _lse_held(lse.view(B, nq, 2), ls.expand(B, nq, 2))
+
+
+@pytest.mark.parametrize("nq", [1, 40])
+@pytest.mark.parametrize("size", [1e-25, 1e-40])
+def test_values_near_the_end_of_fp32(nq, size):
+    g = _gen(21)
+    dh, page, length = 64, 64, 700
+    cache, kd, vd = _filled(g, 1, dh, 8, page, 11)
+    pages = torch.arange(11, dtype=torch.int32, device="cuda").view(1, -1)
+    vd *= (size / cache.v_scales.double()).transpose(1, 2)[..., None]
+    cache.v_scales.fill_(size)
+    q = torch.randn((nq, 2, dh), generator=g, device="cuda").to(torch.bfloat16)
+    out, lse = _attention(cache, q, [nq], [length], pages)
+    assert J.jab_get_device_status() == 0
+    o, ls, mag, keys, top = _exact(cache, kd, vd, q, [nq], [length], pages)
+    tol = 2.0 ** -11 * mag + 2.0 ** -8 * o.abs() + 1e-37
+    assert bool(((out.double() - o).abs() <= tol).all())
     _lse_held(lse, ls)
 
 
