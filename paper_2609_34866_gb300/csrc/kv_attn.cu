@@ -6,8 +6,8 @@
 //
 // The codes are exact in fp16 and the scales stay outside of the products: the one on K multiplies the
 // score, the one on V the weight, so a byte of the cache costs one or two integer instructions and one
-// subtraction on its way to the matrix instructions. m_i is a running maximum of s_ij + log2 v_j, not of
-// s_ij: the weights that are rounded to fp16 are then at most 2^8 whatever the scales of V are.
+// subtraction on its way to the matrix instructions. m_i is a running maximum of s_ij + log2 v_j - 6, not of
+// s_ij: the weights that are rounded to fp16 are then at most 2^15 whatever the scales of V are.
 //
 // Rows of a tile are (token, query head) pairs that share a KV head, R = 8 NT of them. Keys go 16 at a time, two such
 // groups together:
@@ -206,12 +206,12 @@ __device__ __forceinline__ float load_q(const T* row, int q, bool live, uint32_t
 template <int NS, int NT, int MT, bool MASKED>
 __device__ __forceinline__ void softmax_step(float (&s)[NS][NT][4], const float2 (&sc)[NS][2], const float (&fac)[NT][2], int key, const int (&lo)[NT][2],
                                              const int (&hi)[NT][2], float (&m)[NT][2], float (&l)[NT][2], float (&o)[NT][MT][4], uint32_t (&pb)[NS][NT][4]) {
-  float lv[NS][2];  // exponents of the V scales (2^lv <= scale < 2^(lv + 1))
+  float lv[NS][2];  // exponents of the V scales (2^e <= scale < 2^(e + 1)), less the headroom
 #pragma unroll
   for (int n = 0; n < NS; ++n)
 #pragma unroll
     for (int i = 0; i < 2; ++i)
-      lv[n][i] = fmaxf(__uint_as_float((__float_as_uint(sc[n][i].y) >> 23) | 0x4b000000u) - 8388735.f, kLeastLog2);
+      lv[n][i] = fmaxf(__uint_as_float((__float_as_uint(sc[n][i].y) >> 23) | 0x4b000000u) - (8388735.f + kHeadroom), kLeastLog2 - kHeadroom);
 #pragma unroll
   for (int j = 0; j < NT; ++j) {
     bool see[NS][4];

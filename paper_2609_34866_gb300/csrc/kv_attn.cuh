@@ -283,9 +283,15 @@ __device__ __forceinline__ int64_t slot_of(const AttnParams& p, int worker, int 
 }
 
 // log2 of the least V scale that the running maxima know: one below it (a row of zeros) counts as this. Such a key's
-// weight is small whatever its score is, its 2^(s - m) is not: like this, that is at most 2^98 when the maximum follows
-// from 2^8 on, and the sums of 2^29 of them are finite.
+// weight is small whatever its score is, its 2^(s - m) is not: like this, that is at most 2^104 when the maximum follows
+// from 2^8 on, and the sums of 2^23 of them are finite.
 constexpr float kLeastLog2 = -90.f;
+
+// The maxima are held 2^6 lower than they are, in both kernels: a row's largest weight is then 2^6 and more as it goes
+// into the products (2^15 at most, where the maximum follows from 2^8 on), and what fp16 cannot hold of a small one,
+// 2^-25, is 2^-31 of that. (Held at 1, a flat tail of weights 2^-26 of one key's was lost from the outputs, though not
+// from the sums that they are divided by: 2^-10 of the result for 65536 keys.)
+constexpr float kHeadroom = 6.f;
 
 // 2^(a - b) with 2^(-inf - -inf) = 0.
 __device__ __forceinline__ float shift2(float a, float b) { return a == -INFINITY ? 0.f : exp2f(a - b); }

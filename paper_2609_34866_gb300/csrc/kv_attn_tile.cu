@@ -40,7 +40,7 @@ struct Layout {
   static constexpr int RAW = KT * DH * BITS / 8;       // K or V as codes
   static constexpr int K_STAGE = RAW + 2 * KT * 4;     // K and the scales of both
   static constexpr int K_OFF = 0, V_OFF = 2 * TILE, RK_OFF = 4 * TILE, RV_OFF = RK_OFF + KST * K_STAGE;
-  static constexpr int SC_OFF = RV_OFF + VST * RAW;                         // per tile: K scale * log2 e * c, V scale, its log2
+  static constexpr int SC_OFF = RV_OFF + VST * RAW;                         // per tile: K scale * log2 e * c, V scale, its log2 less the headroom
   static constexpr int ROW_OFF = SC_OFF + SCB * 3 * KT * 4;       // per item: lo, hi, power of two of Q
   static constexpr int BAR_OFF = ROW_OFF + 2 * 3 * R * 4;
   static constexpr int ITEM_OFF = BAR_OFF + 512;
@@ -157,7 +157,7 @@ __device__ __forceinline__ void two_parts(float2 w, uint32_t& h, uint32_t& r) {
 // that leaves over; l gets the row sums of 2^y, `big` the largest weight of either half of the pairs. As long as none
 // passes 2^15 and no sum 2^112 the reference may stay, and neither the maximum nor the V scales' logarithms are
 // needed. (The sums: a key whose values are zero has no weight, however far its score is ahead. Once the reference has
-// moved its 2^y is at most 2^90, and a sum has room for 2^22 more of them.)
+// moved its 2^y is at most 2^96, and a sum has room for 2^16 more of them.)
 template <class T>
 __device__ __forceinline__ void plain_weights(uint32_t (&v)[32], const float* sc, const float (&ref)[2], const float (&fac)[2], float2 (&l)[2], uint32_t& big) {
   big = 0;
@@ -198,7 +198,7 @@ struct Sees {
   __device__ __forceinline__ Sees(int k, int lo, int hi) : x(k >= lo && k < hi), y(k + 1 >= lo && k + 1 < hi) {}
 };
 
-// The rows' largest score + log2 of the key's V scale, with masks. (A hidden key's scales may be anything.)
+// The rows' largest score + log2 of the key's V scale (less the headroom), with masks. (A hidden key's scales may be anything.)
 template <class T>
 __device__ __forceinline__ void masked_top(const uint32_t (&v)[32], const float* sc, const float (&fac)[2], const int (&lo)[2], const int (&hi)[2], int k0,
                                            float (&top)[2]) {
@@ -507,7 +507,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
               for (int c = 0; c < 2; ++c) {
                 top[c] = fmaxf(top[c], __shfl_xor_sync(0xffffffffu, top[c], 1));
                 top[c] = fmaxf(top[c], __shfl_xor_sync(0xffffffffu, top[c], 2));
-                const float up = ceilf(fmaxf(top[c] - m[c], 0.f));
+                const float up = floorf(fmaxf(top[c] - m[c], 0.f));
                 f[c] = exp2f(-up);
                 m[c] += up;
                 l[c].x *= f[c], l[c].y *= f[c];
@@ -731,7 +731,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
           const float vs = scales[KT + tid];
           sc[tid] = scales[tid] * p.scale_log2;
           sc[KT + tid] = vs;
-          sc[2 * KT + tid] = vs > 0.f ? fmaxf(__log2f(vs), kLeastLog2) : vs == 0.f ? kLeastLog2 : vs;
+          sc[2 * KT + tid] = (vs > 0.f ? fmaxf(__log2f(vs), kLeastLog2) : vs == 0.f ? kLeastLog2 : vs) - kHeadroom;
           convert_tile<DH, BITS>(raw, smem + L::K_OFF + (j & 1) * L::TILE, tid);
           done(&bars->k_full[j & 1]);
           if (lane == 0) {

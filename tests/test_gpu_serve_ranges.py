@@ -118,6 +118,24 @@ def test_weights_keep_their_bits_in_every_tile(q_lens, lens, shared, window, dh,
     _lse_held(lse, ls)
 
 
+# ------------------------------------------------------------------ attention: small weights
+# Weights 2^-26 of the largest are held within 2^-31 of it (2^-30 by tiles, twice that after a move), where a share of
+# the work has all of a sequence's keys: many sequences, here of the same pages.
+@pytest.mark.parametrize("nq,B,bits,dh", [(1, 2048, 8, 128), (1, 2048, 4, 64), (40, 600, 8, 128), (40, 600, 4, 64)])
+@pytest.mark.parametrize("dt", [torch.float16, torch.bfloat16])
+def test_a_long_flat_tail_behind_one_key(nq, B, bits, dh, dt):
+    length = 4096
+    cache, kd, vd, pages = _one_ahead(dh, bits, 64, length)
+    q = torch.full((nq, 2, dh), 1.0, device="cuda").to(dt)
+    scale = 26 * math.log(2) / dh
+    out, lse = _attention(cache, q.repeat(B, 1, 1), [nq] * B, [length] * B, pages.repeat(B, 1), scale=scale)
+    assert J.jab_get_device_status() == 0
+    o, ls, mag, keys, top = _exact(cache, kd, vd, q, [nq], [length], pages, scale=scale)
+    assert 0.98 * 2.0 ** -14 < o[0, 0, 1].item() < 2.0 ** -14
+    _held(out.view(B, nq, 2, dh), o, o, 2.0 ** -11 * mag * (vd[0, 0, 0] > 0), keys * 2.0 ** -29 * top)
+    _lse_held(lse.view(B, nq, 2), ls.expand(B, nq, 2))
+
+
 # ------------------------------------------------------------------ attention: values of zero, NaN
 # (Many sequences, here of the same pages, so that a share of the work has several key tiles of a row in turn.)
 @pytest.mark.parametrize("nq,B", [(1, 2048), (40, 400)])
