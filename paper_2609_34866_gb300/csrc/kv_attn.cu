@@ -158,7 +158,7 @@ __device__ __forceinline__ void take(const uint8_t* p, uint32_t* w) {
 }
 
 // Q's dimensions that go with a lane's codes of K, as the B operand of K's steps; returns the power of two that the row
-// was divided by (bf16: it is brought into fp16's range; exact down to 2^-24 of its largest). A lane has DH / 4 of them, in
+// was divided by (bf16: it is brought into fp16's range; exact down to 2^-31 of its largest). A lane has DH / 4 of them, in
 // runs of what it reads at once.
 template <class T, int DH, int BITS>
 __device__ __forceinline__ float load_q(const T* row, int q, bool live, uint32_t (&b)[DH / 8]) {

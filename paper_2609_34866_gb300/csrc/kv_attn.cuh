@@ -303,12 +303,14 @@ __device__ __forceinline__ void store_out<half_t>(half_t* p, float v) { *p = __f
 template <>
 __device__ __forceinline__ void store_out<bf16_t>(bf16_t* p, float v) { *p = __float2bfloat16_rn(v); }
 
-// Power of two that brings a bf16 row whose largest magnitude has the bits `big` to [8, 16), and its inverse: fp16
-// then holds the row's elements exactly down to 2^-24 of the largest. Both are normal numbers.
+// Power of two that brings a bf16 row whose largest magnitude has the bits `big` to [2^14, 2^15), the last octave but
+// one of fp16, and its inverse. The row's elements from 2^-31 of the largest on are then exact in fp16 (their last of
+// eight bits is at 2^-24 or above), the others within 2^-39 of it. Both powers are normal numbers; the largest bf16
+// exponent comes to the last octave.
 __device__ __forceinline__ void row_power(uint32_t big, float& by, float& back) {
-  const int e = min(max((int)(big >> 23), 4), 253);
-  by = __uint_as_float((uint32_t)(257 - e) << 23);   // 2^(130 - e)
-  back = __uint_as_float((uint32_t)(e - 3) << 23);   // 2^(e - 130)
+  const int e = min(max((int)(big >> 23), 15), 253);
+  by = __uint_as_float((uint32_t)(268 - e) << 23);    // 2^(141 - e)
+  back = __uint_as_float((uint32_t)(e - 14) << 23);   // 2^(e - 141)
 }
 
 // Tile kernel (kv_attn_tile.cu): 128 rows x 128 keys on the tensor cores.

@@ -136,6 +136,24 @@ def test_a_long_flat_tail_behind_one_key(nq, B, bits, dh, dt):
     _lse_held(lse.view(B, nq, 2), ls.expand(B, nq, 2))
 
 
+def test_bf16_query_elements_far_below_the_largest():
+    """Elements 2^-22 of a row's largest are used with all of their bits: the largest meets codes of 0."""
+    dh, page, length = 128, 16, 48
+    g = _gen(11)
+    cache, kd, vd = _filled(g, 1, dh, 8, page, 3)
+    cache.k_codes[..., 0] = 128
+    kd[..., 0] = 0
+    q = torch.randn((1, 4, dh), generator=g, device="cuda").to(torch.bfloat16)
+    q[..., 0] = 2.0 ** 22
+    pages = torch.arange(3, dtype=torch.int32, device="cuda").view(1, 3)
+    for qq, nq in ((q, 1), (q.expand(40, 4, dh).contiguous(), 40)):
+        out, lse = _attention(cache, qq, [nq], [length], pages, scale=0.3)
+        assert J.jab_get_device_status() == 0
+        o, ls, mag, keys, top = _exact(cache, kd, vd, qq, [nq], [length], pages, scale=0.3)
+        _held(out, o, o, (2.0 ** -22 + 2.0 ** -15 + keys * 2.0 ** -26) * mag, keys * 2.0 ** -23 * top)
+        _lse_held(lse, ls)
+
+
 # ------------------------------------------------------------------ attention: values of zero, NaN
 # (Many sequences, here of the same pages, so that a share of the work has several key tiles of a row in turn.)
 @pytest.mark.parametrize("nq,B", [(1, 2048), (40, 400)])
