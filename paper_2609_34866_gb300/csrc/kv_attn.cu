@@ -210,8 +210,10 @@ __device__ __forceinline__ void softmax_step(float (&s)[NS][NT][4], const float2
 #pragma unroll
   for (int n = 0; n < NS; ++n)
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-      lv[n][i] = fmaxf(__uint_as_float((__float_as_uint(sc[n][i].y) >> 23) | 0x4b000000u) - (8388735.f + kHeadroom), kLeastLog2 - kHeadroom);
+    for (int i = 0; i < 2; ++i) {
+      const float e = __uint_as_float((__float_as_uint(sc[n][i].y) >> 23) | 0x4b000000u) - (8388735.f + kHeadroom);
+      lv[n][i] = e < 128.f - kHeadroom ? fmaxf(e, kLeastLog2 - kHeadroom) : -kHeadroom;
+    }
 #pragma unroll
   for (int j = 0; j < NT; ++j) {
     bool see[NS][4];

@@ -285,6 +285,7 @@ __device__ __forceinline__ int64_t slot_of(const AttnParams& p, int worker, int 
 // log2 of the least V scale that the running maxima know: one below it (a row of zeros) counts as this. Such a key's
 // weight is small whatever its score is, its 2^(s - m) is not: like this, that is at most 2^104 when the maximum follows
 // from 2^8 on, and the sums of 2^23 of them are finite.
+// A scale of NaN (or infinity) counts as 1: the row's output is NaN, its log-sum-exp stays right.
 constexpr float kLeastLog2 = -90.f;
 
 // The maxima are held 2^6 lower than they are, in both kernels: a row's largest weight is then 2^6 and more as it goes

@@ -731,7 +731,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
           const float vs = scales[KT + tid];
           sc[tid] = scales[tid] * p.scale_log2;
           sc[KT + tid] = vs;
-          sc[2 * KT + tid] = (vs > 0.f ? fmaxf(__log2f(vs), kLeastLog2) : vs == 0.f ? kLeastLog2 : vs) - kHeadroom;
+          sc[2 * KT + tid] = (vs < INFINITY ? fmaxf(__log2f(vs), kLeastLog2) : 0.f) - kHeadroom;
           convert_tile<DH, BITS>(raw, smem + L::K_OFF + (j & 1) * L::TILE, tid);
           done(&bars->k_full[j & 1]);
           if (lane == 0) {

@@ -192,6 +192,21 @@ def test_values_near_the_end_of_fp32(nq, size):
     _lse_held(lse, ls)
 
 
+@pytest.mark.parametrize("nq", [1, 40])
+@pytest.mark.parametrize("key", [5, 265, 650])
+def test_a_value_that_is_nan_leaves_the_log_sum_exp(nq, key):
+    g = _gen(key)
+    dh, page, length = 64, 64, 700
+    cache, kd, vd = _filled(g, 1, dh, 8, page, 11)
+    pages = torch.arange(11, dtype=torch.int32, device="cuda").view(1, -1)
+    q = torch.randn((nq, 2, dh), generator=g, device="cuda").to(torch.float16)
+    cache.v_scales[key // page, 0, key % page] = math.nan
+    out, lse = _attention(cache, q, [nq], [length], pages)
+    o, ls, *_ = _exact(cache, kd, vd, q, [nq], [length], pages)
+    assert bool(torch.isnan(out).all())
+    _lse_held(lse, ls)
+
+
 # ------------------------------------------------------------------ cache
 def _write_check(n, hq, hkv, dh, bits, page, dt, rope):
     g = _gen(n + hq + dh + bits)
