@@ -413,7 +413,8 @@ jab_status jab_kv_read(const jab_kv_cache* cache, int32_t n_seqs, const int32_t*
  * key j when j <= p and, with window > 0, j > p - window, where p = seq_lens[b] - n + i. A row
  * that sees nothing has output 0 and log-sum-exp -inf.
  *   Q_dev        type (JAB_FP16 or JAB_BF16) [n_tokens, n_q_heads * head_dim], pitch ldq
- *   q_start_dev  int32 [n_seqs + 1], increasing from 0 to n_tokens
+ *   q_start_dev  int32 [n_seqs + 1], increasing from 0 to n_tokens; rows that no sequence has are reported
+ *                (JAB_ERR_INVALID_ARG) and left as they are
  *   pages_dev    int32 [n_seqs, max_pages], seq_lens_dev int32 [n_seqs]
  *   max_q_len, max_seq_len   the longest of the sequences, or more: they set how the work is cut up, not
  *                what is computed

@@ -227,6 +227,8 @@ __device__ void make_plan(const AttnParams& p, int workers, int* cum_t, int* cum
   }
   __syncthreads();
   if (blockIdx.x != 0) return;
+  // rows that no sequence owns would stay as they are
+  if (tid == 0 && (__ldg(p.q_start) != 0 || __ldg(p.q_start + p.n_seqs) != p.n_tokens)) report(p.status, JAB_ERR_INVALID_ARG);
   // for the joining kernel: the scalars, and every item
   for (int i = tid; i < kPlanHead; i += 32 * WARPS) p.list.plan[i] = head[i];
   for (int e = tid; e < E; e += 32 * WARPS) {

@@ -207,6 +207,22 @@ def test_a_value_that_is_nan_leaves_the_log_sum_exp(nq, key):
     _lse_held(lse, ls)
 
 
+# ------------------------------------------------------------------ attention: inputs that are reported
+def test_rows_that_no_sequence_owns_are_reported():
+    cache, _, _ = _filled(_gen(1), 1, 64, 8, 16, 4)
+    pages = torch.arange(4, dtype=torch.int32, device="cuda").view(2, 2)
+    for hq, max_q in ((1, 2), (64, 40)):  # by keys, and by tiles
+        n = 2 * max_q
+        q = torch.randn((n, hq, 64), device="cuda").to(torch.float16)
+        ws = torch.empty(J.jab_kv_attention_workspace_size(cache, 2, n, hq, max_q, 32), dtype=torch.uint8, device="cuda")
+        lens = torch.tensor([32, 32], dtype=torch.int32, device="cuda")
+        for start, status in (((0, max_q, n), 0), ((1, max_q, n), 1), ((0, max_q, n - 1), 1), ((0, 0, 0), 1), ((n, n, n), 1)):
+            out = torch.full_like(q, 5.0)
+            J.jab_kv_attention(cache, q, torch.tensor(start, dtype=torch.int32, device="cuda"), pages, lens, out, ws, max_q, 32)
+            assert J.jab_get_device_status() == status, start
+            assert bool((out[: start[0]] == 5).all()) and bool((out[start[2]:] == 5).all())
+
+
 # ------------------------------------------------------------------ cache
 def _write_check(n, hq, hkv, dh, bits, page, dt, rope):
     g = _gen(n + hq + dh + bits)
