@@ -423,7 +423,9 @@ jab_status jab_kv_read(const jab_kv_cache* cache, int32_t n_seqs, const int32_t*
  *   softmax_scale  <= 0 selects 1/sqrt(head_dim)
  *   O_dev        out type [n_tokens, n_q_heads * head_dim], pitch ldo
  *   lse_dev      out fp32 [n_tokens, n_q_heads] or NULL: natural log-sum-exp of the scaled scores
- * n_q_heads a multiple of n_kv_heads; n_seqs up to 2048; ws 256-byte aligned. */
+ * n_q_heads a multiple of n_kv_heads; n_seqs up to 2048; ws 256-byte aligned. A call of 2^30 and more pairs of a row tile
+ * (128 rows, 8 to 32 where all sequences are short) and a key tile (128, 16 or 32 keys) that see each other raises
+ * JAB_ERR_INVALID_ARG on the device and computes nothing. */
 size_t jab_kv_attention_workspace_size(const jab_kv_cache* cache, int32_t n_seqs, int64_t n_tokens,
                                        int32_t n_q_heads, int32_t max_q_len, int32_t max_seq_len,
                                        int32_t shared_len);

@@ -562,7 +562,7 @@ __global__ void __launch_bounds__(32 * MW, BATCH == 4 ? 6 : 2)
     it_c = __ldcg(common.items);
     items_c = __ldcg(common.plan + kItems), per_c = __ldcg(common.plan + kPer), total_c = __ldcg(common.plan + kTotal);
   }
-  if (i >= items) return;
+  if (i >= items || (p.shared > 0 && items_c == 0)) return;  // (a list too long to be run is empty)
   // (the shared keys' own items are taken with the sequences')
   if (own.all && i < ((int64_t)p.n_tokens * p.G + own.rows - 1) / own.rows) return;
   const int rt = it.y >> 8, rows = min((it.y & 255) - r0, MW);

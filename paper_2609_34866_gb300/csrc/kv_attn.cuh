@@ -146,8 +146,12 @@ __device__ __forceinline__ int position_of(const AttnParams& p, int token) {
   return en.len - en.nq + token - en.tok0;
 }
 
+// Key tiles and items of a KV head that a list may have. Counts stop there (and are 32-bit numbers for that: q_start and
+// lengths of any kind could bring them past 2^31, with shares of the work that begin before the list or behind it).
+constexpr int kMostTiles = 1 << 30, kMostItems = 1 << 23;
+
 // The plan, by all WARPS * 32 threads of a block: cum_t[e], cum_i[e] = key tiles and items of a KV head before entry
-// e, head[] = the scalars.
+// e, head[] = the scalars. A list that is too long is reported and counts as empty.
 template <int R, int KT, int WARPS>
 __device__ void make_plan(const AttnParams& p, int workers, int* cum_t, int* cum_i, int* head) {
   __shared__ int w_v[4][WARPS];
@@ -193,12 +197,12 @@ __device__ void make_plan(const AttnParams& p, int workers, int* cum_t, int* cum
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const int ut = __shfl_up_sync(0xffffffffu, t, o), ui = __shfl_up_sync(0xffffffffu, i, o);
-        if (lane >= o) t += ut, i += ui;
+        if (lane >= o) t = min(t + ut, kMostTiles), i = min(i + ui, kMostItems);
       }
       if (lane == 31) w_v[0][warp] = t, w_v[1][warp] = i;
       __syncthreads();
       at = t - st, ai = i - si;
-      for (int w = 0; w < warp; ++w) at += w_v[0][w], ai += w_v[1][w];
+      for (int w = 0; w < warp; ++w) at = min(at + w_v[0][w], kMostTiles), ai = min(ai + w_v[1][w], kMostItems);
     }
     for (int e = e0; e < e1; ++e) {
       const Entry en = entry_of(p, e);
@@ -207,23 +211,27 @@ __device__ void make_plan(const AttnParams& p, int workers, int* cum_t, int* cum
       int sum = 0, t0, n;
       if (en.all) {
         key_tiles<R, KT>(p, en, 0, head, t0, n);
-        sum = n * nrt;
-      } else {
+        sum = (int)min((int64_t)n * nrt, (int64_t)kMostTiles);
+      } else if (nrt < kMostItems) {
         for (int rt = 0; rt < nrt; ++rt) {
           key_tiles<R, KT>(p, en, rt, head, t0, n);
-          sum += n;
+          sum = min(sum + n, kMostTiles);
         }
       }
-      at += sum, ai += nrt;
+      at = min(at + sum, kMostTiles), ai = min(ai + nrt, kMostItems);
     }
     if (pass == 0) st = at, si = ai;
   }
   if (tid == 0) {
     int t = 0, i = 0;
-    for (int w = 0; w < WARPS; ++w) t += w_v[0][w], i += w_v[1][w];
+    for (int w = 0; w < WARPS; ++w) t = min(t + w_v[0][w], kMostTiles), i = min(i + w_v[1][w], kMostItems);
+    int64_t per = ((int64_t)t * p.n_kv + workers - 1) / workers;
+    if (t >= kMostTiles || i >= kMostItems || per > INT32_MAX) {
+      t = i = per = 0;
+      if (blockIdx.x == 0) report(p.status, JAB_ERR_INVALID_ARG);
+    }
     cum_t[E] = t, cum_i[E] = i;
-    head[kTotal] = t, head[kItems] = i;
-    head[kPer] = (int)min(((int64_t)t * p.n_kv + workers - 1) / workers, (int64_t)INT32_MAX);
+    head[kTotal] = t, head[kItems] = i, head[kPer] = (int)per;
   }
   __syncthreads();
   if (blockIdx.x != 0) return;
@@ -231,6 +239,7 @@ __device__ void make_plan(const AttnParams& p, int workers, int* cum_t, int* cum
   if (tid == 0 && (__ldg(p.q_start) != 0 || __ldg(p.q_start + p.n_seqs) != p.n_tokens)) report(p.status, JAB_ERR_INVALID_ARG);
   // for the joining kernel: the scalars, and every item
   for (int i = tid; i < kPlanHead; i += 32 * WARPS) p.list.plan[i] = head[i];
+  if (head[kItems] == 0) return;
   for (int e = tid; e < E; e += 32 * WARPS) {
     const Entry en = entry_of(p, e);
     int at = cum_t[e], i = cum_i[e], t0, n;

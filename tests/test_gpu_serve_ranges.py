@@ -223,6 +223,23 @@ def test_rows_that_no_sequence_owns_are_reported():
             assert bool((out[: start[0]] == 5).all()) and bool((out[start[2]:] == 5).all())
 
 
+def test_a_list_of_work_too_long_to_count_is_reported():
+    """2048 sequences that all claim the same rows, behind tables for 2^20 keys: 2^31 pairs of a row tile and a key
+    tile. Nothing is computed."""
+    page, B, n = 4096, 2048, 8192
+    cache, _, _ = _filled(_gen(1), 1, 64, 8, page, 1)
+    pages = torch.zeros((B, 256), dtype=torch.int32, device="cuda")
+    lens = torch.full((B,), 256 * page, dtype=torch.int32, device="cuda")
+    start = (torch.arange(B + 1, dtype=torch.int32, device="cuda") % 2) * n
+    q = torch.randn((n, 4, 64), device="cuda").to(torch.float16)
+    for shared in (0, page):
+        out = torch.full_like(q, 5.0)
+        ws = torch.empty(J.jab_kv_attention_workspace_size(cache, B, n, 4, n, 256 * page, shared), dtype=torch.uint8, device="cuda")
+        J.jab_kv_attention(cache, q, start, pages, lens, out, ws, n, 256 * page, shared_len=shared)
+        assert J.jab_get_device_status() == 1
+        assert bool((out == 5).all())
+
+
 # ------------------------------------------------------------------ cache
 def _write_check(n, hq, hkv, dh, bits, page, dt, rope):
     g = _gen(n + hq + dh + bits)
