@@ -28,6 +28,7 @@
 #include <type_traits>
 
 #include "kv_attn.cuh"
+#include "per_device.h"
 #include "tc.cuh"
 
 namespace jab {
@@ -725,23 +726,21 @@ template <class T, int DH, int BITS, int NT>
 cudaError_t launch_keys(const AttnParams& p, int64_t est_tiles, int sms, cudaStream_t st) {
   auto kern = kv_attn_kernel<T, DH, BITS, NT>;
   const size_t most = kKeysSmem<DH, BITS, NT> + (size_t)2 * (2048 + 2) * 4;
-  static bool attr_set = false;
-  if (!attr_set) {
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
-    if (e != cudaSuccess) return e;
-    attr_set = true;
-  }
+  static SetUp ready;
+  static Found resident;  // blocks an SM, by the number of entries
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  e = ready.once(dev, [&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most); });
+  if (e != cudaSuccess) return e;
   const int E = p.n_seqs + (p.list.all ? 1 : 0);
   const size_t smem = kKeysSmem<DH, BITS, NT> + (size_t)2 * (E + 1) * 4;
-  static size_t asked = 0;
-  static int occ = 0;
-  if (occ == 0 || asked != smem) {
+  const int occ = resident.get(dev, E, [&] {
     int n = 0;
-    const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kern, 32 * W, smem);
-    if (e != cudaSuccess) return e;
-    occ = std::max(n, 1);
-    asked = smem;
-  }
+    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kern, 32 * W, smem);
+    return e == cudaSuccess ? std::max(n, 1) : 0;
+  });
+  if (e != cudaSuccess) return e;
   const int64_t grid = std::max<int64_t>(1, std::min<int64_t>({(int64_t)sms * occ, kMaxBlocks, (est_tiles + W - 1) / W}));
   return launch_after(kern, (unsigned)grid, 32 * W, smem, st, p);
 }

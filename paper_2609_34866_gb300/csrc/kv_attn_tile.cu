@@ -25,6 +25,7 @@
 #include <type_traits>
 
 #include "kv_attn.cuh"
+#include "per_device.h"
 #include "tc.cuh"
 
 namespace jab {
@@ -760,12 +761,12 @@ cudaError_t launch_as(const AttnParams& p, int64_t est_tiles, int sms, cudaStrea
   constexpr int most = L::USED + 1024 + 2 * 2050 * 4;
   static_assert(most <= 226 * 1024 + 512, "shared memory budget");
   const int smem = L::USED + 1024 + 2 * (p.n_seqs + 2) * 4;
-  static bool attr_set = false;
-  if (!attr_set) {
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
-    if (e != cudaSuccess) return e;
-    attr_set = true;
-  }
+  static SetUp ready;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  e = ready.once(dev, [&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, most); });
+  if (e != cudaSuccess) return e;
   const int64_t grid = std::max<int64_t>(1, std::min<int64_t>(sms, est_tiles));
   return launch_after(kern, (unsigned)grid, THREADS, (size_t)smem, st, p);
 }

@@ -23,6 +23,7 @@
 #include <algorithm>
 
 #include "kernels.h"
+#include "per_device.h"
 #include "quotient.cuh"
 #include "serve.h"
 #include "tc.cuh"
@@ -537,10 +538,10 @@ Scratch plan_scratch(int64_t M, int N, int K) {
 // (its launch, the meeting of its blocks, the sums' way), a stage of 128 a quarter of one: 64 tokens x 6144 x 4096 take
 // 14.5 us in two ranges and 16.5 in one, x 2304 x 768 9.3 in three and 7.3 in one.
 template <class C, class Kernel>
-int ranges_of(Kernel kern, const LinParams& p, int sms, int (&fit)[kMaxRanges + 1]) {
+int ranges_of(Kernel kern, const LinParams& p, int sms, int dev, Found& fit) {
   const int64_t tiles = (int64_t)p.tiles_n * p.tiles_m;
   for (int s = (int)std::min<int64_t>({kMaxRanges, sms / tiles, p.stages / kExactStages}); s > 1; --s) {
-    if (fit[s] == 0) {  // clusters of that many blocks that are resident at once
+    const int clusters = fit.get(dev, s, [&] {  // of that many blocks, resident at once
       cudaLaunchConfig_t cfg = {};
       cudaLaunchAttribute at[1];
       at[0].id = cudaLaunchAttributeClusterDimension;
@@ -553,9 +554,9 @@ int ranges_of(Kernel kern, const LinParams& p, int sms, int (&fit)[kMaxRanges + 
       cfg.numAttrs = 1;
       int n = 0;
       if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess) cudaGetLastError();
-      fit[s] = std::max(n, 1);
-    }
-    if (tiles <= fit[s]) return s;
+      return std::max(n, 1);
+    });
+    if (tiles <= clusters) return s;
   }
   return 1;
 }
@@ -569,14 +570,14 @@ template <class T, int NTOK>
 cudaError_t launch_as(const CUtensorMap& tw, const CUtensorMap& tx, LinParams p, int sms, cudaStream_t st) {
   using C = Cfg<NTOK>;
   auto kern = qlinear_kernel<T, NTOK>;
-  static bool attr_set = false;
-  static int fit[kMaxRanges + 1] = {};
-  if (!attr_set) {
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
-    if (e != cudaSuccess) return e;
-    attr_set = true;
-  }
-  p.ranges = C::SPLIT ? ranges_of<C>(kern, p, sms, fit) : 1;
+  static SetUp ready;
+  static Found fit;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  e = ready.once(dev, [&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM); });
+  if (e != cudaSuccess) return e;
+  p.ranges = C::SPLIT ? ranges_of<C>(kern, p, sms, dev, fit) : 1;
   const int64_t tiles = (int64_t)p.tiles_n * p.tiles_m;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute at[2];
@@ -591,7 +592,7 @@ cudaError_t launch_as(const CUtensorMap& tw, const CUtensorMap& tx, LinParams p,
   cfg.stream = st;
   cfg.attrs = at;
   cfg.numAttrs = p.ranges > 1 ? 2 : 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, tw, tx, p);
+  e = cudaLaunchKernelEx(&cfg, kern, tw, tx, p);
   if (e != cudaSuccess) cudaGetLastError();
   return e;
 }
