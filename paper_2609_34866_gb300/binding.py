@@ -430,7 +430,8 @@ def _shaped(t: torch.Tensor, shape, dtype, name: str) -> int:
 class KvCache:
     """A paged cache of quantised keys and values (jab_kv_cache): caller-owned tensors k_codes, v_codes
     (uint8 [n_pages, n_kv_heads, page_tokens, head_dim * bits / 8]) and k_scales, v_scales (float32
-    [n_pages, n_kv_heads, page_tokens]), allocated here unless given."""
+    [n_pages, n_kv_heads, page_tokens]), allocated here unless given. The calls go by the addresses that these tensors
+    have now, so they are held for as long as the cache and cannot be exchanged (their contents can: copy_)."""
 
     def __init__(self, n_kv_heads: int, head_dim: int, bits: int, page_tokens: int, n_pages: int, device=None,
                  k_codes=None, v_codes=None, k_scales=None, v_scales=None):
@@ -447,14 +448,17 @@ class KvCache:
 
         self.n_kv_heads, self.head_dim, self.bits = int(n_kv_heads), int(head_dim), int(bits)
         self.page_tokens, self.n_pages = int(page_tokens), int(n_pages)
-        self.k_codes = have(k_codes, codes, torch.uint8, "k_codes")
-        self.v_codes = have(v_codes, codes, torch.uint8, "v_codes")
-        self.k_scales = have(k_scales, lead, torch.float32, "k_scales")
-        self.v_scales = have(v_scales, lead, torch.float32, "v_scales")
+        self._held = (have(k_codes, codes, torch.uint8, "k_codes"), have(v_codes, codes, torch.uint8, "v_codes"),
+                      have(k_scales, lead, torch.float32, "k_scales"), have(v_scales, lead, torch.float32, "v_scales"))
         self.desc = _KvCacheDesc(self.n_kv_heads, self.head_dim, self.bits, self.page_tokens, self.n_pages,
                                  self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.k_scales.data_ptr(),
                                  self.v_scales.data_ptr())
         self.ref = ctypes.byref(self.desc)
+
+    k_codes = property(lambda self: self._held[0])
+    v_codes = property(lambda self: self._held[1])
+    k_scales = property(lambda self: self._held[2])
+    v_scales = property(lambda self: self._held[3])
 
 
 def jab_quantized_linear_workspace_size(M: int, N: int, K: int) -> int:

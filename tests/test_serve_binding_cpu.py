@@ -1,0 +1,24 @@
+"""The binding's side of the serving calls, without a GPU."""
+import pytest
+import torch
+
+from paper_2609_34866_gb300 import binding
+
+
+def _any_device(monkeypatch):
+    monkeypatch.setattr(binding, "_ptr", lambda t, dtype=None, name="tensor": None if t is None else t.data_ptr())
+
+
+def test_tensors_of_a_cache_cannot_be_exchanged(monkeypatch):
+    """The calls go by addresses that were taken once: another tensor in their place would leave them behind."""
+    _any_device(monkeypatch)
+    cache = binding.KvCache(2, 64, 8, 16, 3, device="cpu")
+    want = {"k_codes": cache.desc.k_codes, "v_codes": cache.desc.v_codes, "k_scales": cache.desc.k_scales, "v_scales": cache.desc.v_scales}
+    for name, address in want.items():
+        t = getattr(cache, name)
+        assert t.data_ptr() == address
+        with pytest.raises(AttributeError):
+            setattr(cache, name, torch.zeros_like(t))
+        assert getattr(cache, name) is t
+    given = torch.ones((3, 2, 16, 64), dtype=torch.uint8)
+    assert binding.KvCache(2, 64, 8, 16, 3, device="cpu", v_codes=given).v_codes is given
