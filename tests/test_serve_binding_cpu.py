@@ -22,3 +22,17 @@ def test_tensors_of_a_cache_cannot_be_exchanged(monkeypatch):
         assert getattr(cache, name) is t
     given = torch.ones((3, 2, 16, 64), dtype=torch.uint8)
     assert binding.KvCache(2, 64, 8, 16, 3, device="cpu", v_codes=given).v_codes is given
+
+
+def test_current_stream_without_torch_internals(monkeypatch):
+    """The handle of the current stream, from torch's short way if this torch has it, else from its public one."""
+    class Stream:
+        cuda_stream = 1234
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda: Stream())
+    monkeypatch.setattr(binding, "_raw_stream", lambda device: 1000 + device)
+    assert binding._stream(None) == 1003
+    monkeypatch.setattr(binding, "_raw_stream", None)
+    assert binding._stream(None) == 1234
+    assert binding._stream(Stream()) == 1234 and binding._stream(77) == 77
