@@ -276,3 +276,48 @@ def test_write_of_wide_blocks(hq, hkv, dh, few):
     for n in (4 * sms - 1,) if few else (4 * sms, 700):
         for dt, bits in ((torch.float16, 8), (torch.bfloat16, 4), (torch.float32, 8)):
             _write_check(n, hq, hkv, dh, bits, 32, dt, True)
+
+
+@pytest.mark.parametrize("hq,hkv,dh,bits,page", [(32, 8, 128, 8, 64), (12, 12, 64, 4, 16), (0, 3, 64, 8, 48), (71, 1, 128, 4, 32)])
+@pytest.mark.parametrize("dt", [torch.float16, torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rope", [False, True])
+def test_write_of_many_tokens(hq, hkv, dh, bits, page, dt, rope):
+    """A block takes many tokens one after the other, and several rounds of heads."""
+    _write_check(6007, hq, hkv, dh, bits, page, dt, rope)
+
+
+@pytest.mark.parametrize("hkv,dh,bits,page", [(8, 128, 8, 64), (3, 64, 4, 48), (40, 128, 4, 16)])
+@pytest.mark.parametrize("dt", [torch.float16, torch.bfloat16, torch.float32])
+def test_read_of_many_tokens(hkv, dh, bits, page, dt):
+    """Several tokens a block, blocks that cross from one sequence to the next."""
+    g = _gen(hkv + dh)
+    B, T = 9, 1111
+    counts = torch.tensor([1111, 0, 1, 1000, 1111, 513, 7, 1110, 999], dtype=torch.int32, device="cuda")
+    starts = torch.tensor([0, 3, 900, 111, 17, 0, 1000, 1, 64], dtype=torch.int32, device="cuda")
+    width = -(-2300 // page)
+    cache, kd, vd = _filled(g, hkv, dh, bits, page, 200)
+    pages = torch.randint(0, 200, (B, width), generator=g, device="cuda").int()
+    k, v = (torch.full((B, T, hkv, dh), 3.0, dtype=dt, device="cuda") for _ in range(2))
+    J.jab_kv_read(cache, pages, counts, k, v, starts=starts)
+    assert J.jab_get_device_status() == 0
+    for b in range(B):
+        j = torch.arange(int(counts[b]), device="cuda") + starts[b]
+        ids = pages[b].long()[j // page]
+        for got, codes, scales in ((k, cache.k_codes, cache.k_scales), (v, cache.v_codes, cache.v_scales)):
+            want = (R.unpack(codes[ids, :, j % page], bits).float() * scales[ids, :, j % page][..., None]).to(dt)
+            assert torch.equal(got[b, : j.numel()], want) and bool((got[b, j.numel():] == 0).all())
+
+
+# ------------------------------------------------------------------ projection
+@pytest.mark.parametrize("M,N,K", [(1500, 3500, 64), (1500, 3501, 336), (2100, 2600, 1200), (1411, 6144, 2064), (64, 21000, 1104), (9, 40001, 144)])
+@pytest.mark.parametrize("xt,yt", [(torch.bfloat16, torch.bfloat16), (torch.float16, torch.float32), (torch.bfloat16, torch.float16)])
+def test_linear_of_several_tiles_a_block(M, N, K, xt, yt):
+    """More than two tiles for every SM: the accumulators and the rings go on from one tile to the next."""
+    g = _gen(M + N + K)
+    x = torch.randn((M, K), generator=g, device="cuda")
+    x[:, :: max(1, K // 5)] *= 20
+    x = x.to(xt)
+    codes = torch.randint(-127, 128, (N, K), generator=g, device="cuda").to(torch.int8)
+    ws = torch.rand((N,), generator=g, device="cuda") * 0.01 + 1e-4
+    assert torch.equal(_linear(x, codes, ws, yt), R.linear(x, codes, ws, yt))
+    assert J.jab_get_device_status() == 0
