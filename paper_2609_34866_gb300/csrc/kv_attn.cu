@@ -660,16 +660,20 @@ __global__ void __launch_bounds__(32 * MW, BATCH == 4 ? 6 : 2)
 
 // ------------------------------------------------------------------ host side
 constexpr int kMaxBlocks = 608, kMaxTileBlocks = 512;  // (workers of the by-keys kernel: W times as many)
-constexpr int kFewRows = 32;  // rows of a sequence up to which all of the work goes by 16 keys
+constexpr int kFewRows = 32;   // rows of a sequence up to which all of the work goes by 16 keys
+constexpr int kFewBeside = 16;  // the same where longer ones are in the batch
 
 int n_tiles_of_rows(int64_t rows) { return rows <= 8 ? 1 : rows <= 16 ? 2 : 4; }
 
 // Which kernel takes what. Sequences of up to kFewRows (token, head) rows go by 16-key tiles: the cache's bytes bound
-// them, not the products. Longer ones fill 128-row tiles; where lengths are mixed, those of up to 8 rows still go
+// them, not the products. Longer ones fill 128-row tiles; where lengths are mixed, those of up to kFewBeside rows still go
 // by keys, in a launch of their own. Measured, both ways (heads of 128, 8 bits, G = 4, up to 2048 keys): 64 sequences of 32
 // rows 116 us by keys and 165 by tiles, of 16 rows 61 and 163, of 36 rows 189 and 166, of 64 rows 200 and 170; 4 of 36
 // behind 8192 keys 58 and 44. (With heads of 64 and G = 1 the bound would lie higher: 64 sequences of 40 rows 170 and
-// 224, but 4 of 40 behind 8192 keys 54 and 47.)
+// 224, but 4 of 40 behind 8192 keys 54 and 47.) Beside a chunk of 512 tokens, with bounds of 8, 16 and 32 (G = 4, up to 2048
+// keys): 64 sequences of 4 rows 101, 104 and 149 us, of 16 rows 192, 110 and 156, of 32 rows 195, 197 and 166; with up to
+// 8192 keys 4 rows 131, 139 and 244, 16 rows 276, 147 and 254; single tokens at G = 16 100, 84 and 98. (Rows of one tile wait for
+// the longest of them: a bound of 16 makes all of them 16.)
 struct Route {
   List keys, tiles;
   int nt;  // 8-row blocks of the by-keys kernel
@@ -686,8 +690,8 @@ Route route(int dh, int n_kv, int n_seqs, int64_t n_tokens, int G, int max_q, bo
   r.tiles.used = tiles_own || tiles_all;
   r.keys.all = keys_all;
   r.tiles.all = tiles_all;
-  r.nt = !tiles_own ? n_tiles_of_rows(keys_all ? std::max(rows, all_rows) : rows) : keys_all ? 4 : 1;
-  const int split = !tiles_own ? INT32_MAX : uniform ? 0 : 8;  // rows up to which a sequence goes by keys
+  r.nt = !tiles_own ? n_tiles_of_rows(keys_all ? std::max(rows, all_rows) : rows) : keys_all ? 4 : n_tiles_of_rows(kFewBeside);
+  const int split = !tiles_own ? INT32_MAX : uniform ? 0 : kFewBeside;  // rows up to which a sequence goes by keys
   r.keys.min_rows = 1, r.keys.max_rows = keys_own ? split : 0;
   r.tiles.min_rows = tiles_own ? split + 1 : INT32_MAX, r.tiles.max_rows = INT32_MAX;
   size_t at = 0;

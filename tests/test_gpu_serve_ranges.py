@@ -118,6 +118,21 @@ def test_weights_keep_their_bits_in_every_tile(q_lens, lens, shared, window, dh,
     _lse_held(lse, ls)
 
 
+@pytest.mark.parametrize("q_lens,lens", [([130, 4, 1, 3, 2, 5, 4], [700, 1500, 40, 3, 900, 77, 65]), ([600, 1, 1, 2], [600, 1000, 17, 2])])
+@pytest.mark.parametrize("dh,hq,hkv,bits,dt", [(128, 8, 2, 8, torch.float16), (64, 16, 1, 4, torch.float16), (128, 6, 2, 4, torch.bfloat16)])
+def test_short_runs_beside_a_chunk(q_lens, lens, dh, hq, hkv, bits, dt):
+    """Sequences of 1 to 80 rows in one batch with a chunk: the two kernels share the work between them."""
+    g = _gen(sum(lens) + dh + bits)
+    cache, kd, vd = _filled(g, hkv, dh, bits, 64, sum(-(-n // 64) for n in lens) + 3)
+    q = (torch.randn((sum(q_lens), hq, dh), generator=g, device="cuda") * 2).to(dt)
+    pages = _pages(g, lens, 64, cache.n_pages)
+    out, lse = _attention(cache, q, q_lens, lens, pages)
+    assert J.jab_get_device_status() == 0
+    o, ls, mag, keys, top = _exact(cache, kd, vd, q, q_lens, lens, pages)
+    _held(out, o, o, (2.0 ** -22 + 2.0 ** -16 + keys * 2.0 ** -26) * mag, keys * 2.0 ** -23 * top)
+    _lse_held(lse, ls)
+
+
 # ------------------------------------------------------------------ attention: small weights
 # Weights 2^-26 of the largest are held within 2^-31 of it (2^-30 by tiles, twice that after a move), where a share of
 # the work has all of a sequence's keys: many sequences, here of the same pages.
