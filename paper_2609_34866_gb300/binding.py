@@ -433,6 +433,15 @@ def _shaped(t: torch.Tensor, shape, dtype, name: str) -> int:
     return _ptr(t, dtype, name)
 
 
+def _held(i: int, name: str) -> property:
+    """A tensor that a KvCache holds: it may be changed in place (cache.k_scales *= 2), not exchanged."""
+    def put(self, t):
+        if t is not self._tensors[i]:
+            raise AttributeError(f"{name} cannot be exchanged: the calls go by its address; copy_ into it")
+
+    return property(lambda self: self._tensors[i], put)
+
+
 class KvCache:
     """A paged cache of quantised keys and values (jab_kv_cache): caller-owned tensors k_codes, v_codes
     (uint8 [n_pages, n_kv_heads, page_tokens, head_dim * bits / 8]) and k_scales, v_scales (float32
@@ -454,17 +463,15 @@ class KvCache:
 
         self.n_kv_heads, self.head_dim, self.bits = int(n_kv_heads), int(head_dim), int(bits)
         self.page_tokens, self.n_pages = int(page_tokens), int(n_pages)
-        self._held = (have(k_codes, codes, torch.uint8, "k_codes"), have(v_codes, codes, torch.uint8, "v_codes"),
-                      have(k_scales, lead, torch.float32, "k_scales"), have(v_scales, lead, torch.float32, "v_scales"))
+        self._tensors = (have(k_codes, codes, torch.uint8, "k_codes"), have(v_codes, codes, torch.uint8, "v_codes"),
+                         have(k_scales, lead, torch.float32, "k_scales"), have(v_scales, lead, torch.float32, "v_scales"))
         self.desc = _KvCacheDesc(self.n_kv_heads, self.head_dim, self.bits, self.page_tokens, self.n_pages,
                                  self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.k_scales.data_ptr(),
                                  self.v_scales.data_ptr())
         self.ref = ctypes.byref(self.desc)
 
-    k_codes = property(lambda self: self._held[0])
-    v_codes = property(lambda self: self._held[1])
-    k_scales = property(lambda self: self._held[2])
-    v_scales = property(lambda self: self._held[3])
+    k_codes, v_codes = _held(0, "k_codes"), _held(1, "v_codes")
+    k_scales, v_scales = _held(2, "k_scales"), _held(3, "v_scales")
 
 
 def jab_quantized_linear_workspace_size(M: int, N: int, K: int) -> int:

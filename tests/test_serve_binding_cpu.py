@@ -20,6 +20,8 @@ def test_tensors_of_a_cache_cannot_be_exchanged(monkeypatch):
         with pytest.raises(AttributeError):
             setattr(cache, name, torch.zeros_like(t))
         assert getattr(cache, name) is t
+    cache.k_scales += 2.0  # in place: the same tensor
+    assert cache.k_scales.data_ptr() == want["k_scales"] and bool((cache.k_scales == 2).all())
     given = torch.ones((3, 2, 16, 64), dtype=torch.uint8)
     assert binding.KvCache(2, 64, 8, 16, 3, device="cpu", v_codes=given).v_codes is given
 
