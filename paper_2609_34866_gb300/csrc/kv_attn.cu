@@ -795,6 +795,12 @@ size_t kv_attention_scratch(int n_kv, int dh, int n_seqs, int64_t n_tokens, int 
   return kv::route(dh, n_kv, n_seqs, n_tokens, n_q_heads / n_kv, max_q, shared > 0).total;
 }
 
+int kv_attention_kernels(const KvAttnArgs& a) {
+  const int n_kv = a.cache.n_kv_heads;
+  const kv::Route r = kv::route(a.cache.head_dim, n_kv, a.n_seqs, a.n_tokens, a.n_q_heads / n_kv, a.max_q, a.shared > 0);
+  return (r.keys.used ? 1 : 0) + (r.tiles.used ? 1 : 0) + 1;
+}
+
 cudaError_t launch_kv_attention(const KvAttnArgs& a, int sms, cudaStream_t st) {
   const jab_kv_cache& c = a.cache;
   kv::AttnParams p{};

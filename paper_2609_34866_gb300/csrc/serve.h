@@ -54,6 +54,7 @@ struct KvAttnArgs {
   int* status;
 };
 size_t kv_attention_scratch(int n_kv, int dh, int n_seqs, int64_t n_tokens, int n_q_heads, int max_q, int shared);
+int kv_attention_kernels(const KvAttnArgs& a);  // how many launch_kv_attention launches
 cudaError_t launch_kv_attention(const KvAttnArgs& a, int sms, cudaStream_t st);
 
 // qlinear.cu

@@ -208,7 +208,7 @@ jab_status jab_kv_attention(const jab_kv_cache* cache, int32_t n_seqs, int64_t n
   a.scale = softmax_scale > 0.f ? softmax_scale : (float)(1.0 / sqrt((double)cache->head_dim));
   a.out = O_dev, a.ldo = ldo, a.lse = lse_dev;
   a.ws = ws, a.status = status;
-  JAB_LAUNCH("kv_attention", 2, launch_kv_attention(a, sms, st));
+  JAB_LAUNCH("kv_attention", kv_attention_kernels(a), launch_kv_attention(a, sms, st));
   return JAB_OK;
 }
 

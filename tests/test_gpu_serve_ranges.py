@@ -255,6 +255,22 @@ def test_a_list_of_work_too_long_to_count_is_reported():
         assert bool((out == 5).all())
 
 
+def test_launches_are_counted():
+    """One kernel for the work and one that joins; one more where a chunk and short runs share a call."""
+    cache, _, _ = _filled(_gen(1), 1, 64, 8, 16, 40)
+    pages = torch.arange(40, dtype=torch.int32, device="cuda").view(2, 20)
+    q = torch.randn((101, 1, 64), generator=_gen(2), device="cuda").to(torch.float16)
+    for q_lens, launches in (([1, 1], 2), ([50, 50], 2), ([100, 1], 3)):
+        J.jab_timing_reset()
+        J.jab_timing_enable(True)
+        try:
+            _attention(cache, q[: sum(q_lens)], q_lens, [300, 300], pages)
+        finally:
+            J.jab_timing_enable(False)
+        assert J.jab_timing_read()["kv_attention"][1:] == (1, launches)
+    J.jab_timing_reset()
+
+
 # ------------------------------------------------------------------ cache
 def _write_check(n, hq, hkv, dh, bits, page, dt, rope):
     g = _gen(n + hq + dh + bits)
