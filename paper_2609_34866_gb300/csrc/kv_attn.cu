@@ -359,8 +359,9 @@ __global__ void __launch_bounds__(32 * W) kv_attn_kernel(const __grid_constant__
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
       const int r = 8 * j + g, rr = rt * R + r, i = p.by_g.quot(rr), token = en.tok0 + i;
-      const T* row = static_cast<const T*>(p.q) + (int64_t)token * p.ldq + (int64_t)(h * p.G + rr - i * p.G) * DH;
-      const float back = load_q<T, DH, BITS>(row, q4, r < it.rows, qf[j]) * p.scale_log2;
+      const int64_t q_at = (int64_t)token * p.ldq + (int64_t)(h * p.G + rr - i * p.G) * DH;
+      const bool used = r < it.rows && in_bounds(q_at + DH - 1, rows_extent(p, p.ldq, DH), p.status);
+      const float back = load_q<T, DH, BITS>(static_cast<const T*>(p.q) + q_at, q4, used, qf[j]) * p.scale_log2;
       int row_lo = 0, row_hi = 0;
       if (r < it.rows) seen_by_row(p, en, en.all ? position_of(p, token) : en.len - en.nq + i, row_lo, row_hi);
 #pragma unroll
@@ -483,7 +484,8 @@ __global__ void __launch_bounds__(32 * W) kv_attn_kernel(const __grid_constant__
         if (r >= it.rows) continue;
         if (whole) {
           const float inv = l[j][c] == 0.f ? 0.f : 1.f / l[j][c];
-          T* out = static_cast<T*>(p.out) + token * p.ldo + (int64_t)qh * DH + g * (DH / 8);
+          const int64_t at = token * p.ldo + (int64_t)qh * DH + g * (DH / 8), lse_at = token * ((int64_t)p.n_kv * p.G) + qh;
+          T* out = static_cast<T*>(p.out) + at;
 #pragma unroll
           for (int d = 0; d < MT; d += 4) {
             __align__(16) T v[8];
@@ -492,11 +494,11 @@ __global__ void __launch_bounds__(32 * W) kv_attn_kernel(const __grid_constant__
               store_out(v + 2 * k, o[j][d + k][c] * inv);
               store_out(v + 2 * k + 1, o[j][d + k][c + 2] * inv);
             }
-            *reinterpret_cast<uint4*>(out + 2 * d) = *reinterpret_cast<const uint4*>(v);
+            if (out_fits(p, at + 2 * d + 7, DH)) *reinterpret_cast<uint4*>(out + 2 * d) = *reinterpret_cast<const uint4*>(v);
           }
-          if (g == 0 && p.lse != nullptr)
-            p.lse[token * ((int64_t)p.n_kv * p.G) + qh] = l[j][c] == 0.f ? -INFINITY : (m[j][c] + log2f(l[j][c])) * kLn2;
-        } else if (slot < p.list.n_slots) {
+          if (g == 0 && p.lse != nullptr && lse_fits(p, lse_at))
+            p.lse[lse_at] = l[j][c] == 0.f ? -INFINITY : (m[j][c] + log2f(l[j][c])) * kLn2;
+        } else if (slot < p.list.n_slots && part_fits(p, (slot * R + r + 1) * DH - 1, R, DH)) {
           float* part = p.list.part_o + (slot * R + r) * DH + g * (DH / 8);
 #pragma unroll
           for (int d = 0; d < MT; d += 2)
@@ -647,7 +649,9 @@ __global__ void __launch_bounds__(32 * MW, BATCH == 4 ? 6 : 2)
   }
   if (!live) return;
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  T* out = static_cast<T*>(p.out) + (int64_t)token * p.ldo + (int64_t)qh * DH + lane * N;
+  const int64_t at = (int64_t)token * p.ldo + (int64_t)qh * DH + lane * N, lse_at = (int64_t)token * (p.n_kv * p.G) + qh;
+  if (!out_fits(p, at + N - 1, DH) || !lse_fits(p, lse_at)) return;
+  T* out = static_cast<T*>(p.out) + at;
   __align__(8) T v[N];
 #pragma unroll
   for (int d = 0; d < N; ++d) store_out(v + d, o[d] * inv);
@@ -655,7 +659,7 @@ __global__ void __launch_bounds__(32 * MW, BATCH == 4 ? 6 : 2)
     *reinterpret_cast<uint2*>(out) = *reinterpret_cast<const uint2*>(v);
   else
     *reinterpret_cast<uint32_t*>(out) = *reinterpret_cast<const uint32_t*>(v);
-  if (lane == 0 && p.lse != nullptr) p.lse[(int64_t)token * (p.n_kv * p.G) + qh] = l == 0.f ? -INFINITY : (mx + log2f(l)) * kLn2;
+  if (lane == 0 && p.lse != nullptr) p.lse[lse_at] = l == 0.f ? -INFINITY : (mx + log2f(l)) * kLn2;
 }
 
 // ------------------------------------------------------------------ host side

@@ -51,6 +51,16 @@ struct AttnParams {
   int* status;
 };
 
+// Elements of Q, O and the log-sum-exps, and of a list's parts, for the checked build.
+__device__ __forceinline__ int64_t rows_extent(const AttnParams& p, int64_t pitch, int dh) {
+  return (int64_t)(p.n_tokens - 1) * pitch + (int64_t)p.n_kv * p.G * dh;
+}
+__device__ __forceinline__ bool out_fits(const AttnParams& p, int64_t last, int dh) { return in_bounds(last, rows_extent(p, p.ldo, dh), p.status); }
+__device__ __forceinline__ bool lse_fits(const AttnParams& p, int64_t at) { return in_bounds(at, (int64_t)p.n_tokens * p.n_kv * p.G, p.status); }
+__device__ __forceinline__ bool part_fits(const AttnParams& p, int64_t last, int rows, int dh) {
+  return in_bounds(last, (int64_t)p.list.n_slots * rows * dh, p.status);
+}
+
 struct Entry {
   int tok0, nq, len, kbeg;
   bool all;

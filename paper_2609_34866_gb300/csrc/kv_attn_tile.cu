@@ -598,12 +598,14 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
         t += __shfl_xor_sync(0xffffffffu, t, 2);
         const int r = r0 + g + 8 * c, rr = it.rt * R + r, q = p.by_g.quot(rr), qh = it.h * p.G + rr - q * p.G;
         const int64_t token = it.tok0 + q;
+        const int64_t lse_at = token * ((int64_t)p.n_kv * p.G) + qh;
         live[c] = r < it.rows && (whole || fits);
         inv[c] = t == 0.f ? 0.f : 1.f / t;  // (of a whole item; a part stays as it is)
         out[c] = whole ? token * p.ldo + (int64_t)qh * DH : (slot * R + r) * DH;
+        if (live[c]) live[c] = whole ? out_fits(p, out[c] + DH - 1, DH) && lse_fits(p, lse_at) : part_fits(p, out[c] + DH - 1, R, DH);
         if (live[c] && q4 == 0) {
           if (!whole) p.list.part_ml[slot * R + r] = make_float2(m[c], t);
-          else if (p.lse != nullptr) p.lse[token * ((int64_t)p.n_kv * p.G) + qh] = t == 0.f ? -INFINITY : (m[c] + log2f(t)) * kLn2;
+          else if (p.lse != nullptr) p.lse[lse_at] = t == 0.f ? -INFINITY : (m[c] + log2f(t)) * kLn2;
         }
       }
 #pragma unroll 1
@@ -681,11 +683,13 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
             const Entry en{it.tok0, it.nq, it.len, it.kbeg, it.all != 0};
             seen_by_row(p, en, it.all ? position_of(p, token) : it.len - it.nq + q, lo, hi);
           }
-          const uint4* row = reinterpret_cast<const uint4*>(static_cast<const T*>(p.q) + (int64_t)token * p.ldq + (int64_t)(it.h * p.G + rr - q * p.G) * DH);
+          const int64_t q_at = (int64_t)token * p.ldq + (int64_t)(it.h * p.G + rr - q * p.G) * DH;
+          const uint4* row = reinterpret_cast<const uint4*>(static_cast<const T*>(p.q) + q_at);
+          const bool used = live && in_bounds(q_at + DH - 1, rows_extent(p, p.ldq, DH), p.status);
           float by = 1.f, back = 1.f;
           if constexpr (std::is_same<T, bf16_t>::value) {
             uint32_t big = 0;
-            if (live) {
+            if (used) {
 #pragma unroll
               for (int c = 0; c < DH / 8; ++c) {
                 const uint4 u = __ldg(row + c);
@@ -700,7 +704,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
 #pragma unroll
             for (int c = 0; c < 8; ++c) {
               uint4 u = make_uint4(0u, 0u, 0u, 0u);
-              if (live) u = __ldg(row + 8 * b + c);
+              if (used) u = __ldg(row + 8 * b + c);
               uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
               for (int e = 0; e < 4; ++e) {

@@ -188,9 +188,12 @@ __global__ void __launch_bounds__(kWriteThreads, sizeof(T) == 2 ? 2 : 1) kv_writ
 #pragma unroll
       for (int i = 0; i < 8; ++i) big = largest(big, a[i], b[i]);
       if (is_q) {
-        T* out = static_cast<T*>(p.q_out) + (now * p.n_q + row) * DH + 8 * t;
-        store(out, a);
-        store(out + DH / 2, b);
+        const int64_t at = (now * p.n_q + row) * DH + 8 * t;
+        T* out = static_cast<T*>(p.q_out) + at;
+        if (in_bounds(at + DH / 2 + 7, p.n_tokens * p.n_q * DH, p.status)) {
+          store(out, a);
+          store(out + DH / 2, b);
+        }
         // finite, but not in Q's type (or neither): from halfway past the largest fp16 (65504) on
         if (std::is_same<T, half_t>::value && !(big < 65520.f)) report(p.status, JAB_ERR_RANGE);
       }
@@ -212,6 +215,7 @@ __global__ void __launch_bounds__(kWriteThreads, sizeof(T) == 2 ? 2 : 1) kv_writ
     const int h = row - p.n_q - (is_k ? 0 : p.n_kv);
     const int64_t pg = p.page_shift >= 0 ? to >> p.page_shift : to / p.page;
     const int64_t r = (pg * p.n_kv + h) * p.page + (to - pg * p.page);
+    if (!in_bounds(r, p.n_slots * p.n_kv, p.status)) continue;
     uint8_t* codes = (is_k ? p.k_codes : p.v_codes) + r * (DH * BITS / 8) + t * BITS;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
@@ -284,8 +288,10 @@ __global__ void __launch_bounds__(256) kv_read_kernel(const __grid_constant__ Re
       }
     }
     const int64_t o = ((t0 + token) * p.n_kv + h) * DH + t * N;
-    store(static_cast<T*>(p.k) + o, k);
-    store(static_cast<T*>(p.v) + o, v);
+    if (in_bounds(o + N - 1, p.tokens * p.n_kv * DH, p.status)) {
+      store(static_cast<T*>(p.k) + o, k);
+      store(static_cast<T*>(p.v) + o, v);
+    }
     for (u += 256; u >= units; u -= units) ++token, ++j;
   }
 }

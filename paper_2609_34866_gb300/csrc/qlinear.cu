@@ -126,6 +126,7 @@ __global__ void __launch_bounds__(256) quantize_tokens_kernel(const __grid_const
       p.sx[m] = s;
       if (!(s >= 0.f)) report(p.status, JAB_ERR_NONFINITE);
     }
+    if (!in_bounds((m + 1) * p.Kp - 1, p.M * p.Kp, p.status)) continue;
     uint4* out = reinterpret_cast<uint4*>(p.xh + m * p.Kp);
 #pragma unroll
     for (int c = 0; c < KEEP; ++c)
@@ -356,6 +357,7 @@ __global__ void __launch_bounds__(Cfg<NTOK>::THREADS, 1)
     float* sx = token_scales + (warp - 4) * HALF;
     // two channels of a token in one store, where they lie together in a word
     const bool words = sizeof(T) == 2 && p.ldy % 2 == 0 && (reinterpret_cast<uintptr_t>(p.y) & 3) == 0;
+    auto inside = [&](int64_t last) { return in_bounds(last, (p.M - 1) * p.ldy + p.N, p.status); };
     int d = 0;
     bool ok = true;
     for (int unit = unit0; unit < total && ok; unit += step) {
@@ -414,7 +416,7 @@ __global__ void __launch_bounds__(Cfg<NTOK>::THREADS, 1)
           T* y = static_cast<T*>(p.y) + (t0 + c0) * p.ldy + n;
 #pragma unroll
           for (int j = 0; j < 8; ++j)
-            if (c0 + j < all) y[j * p.ldy] = out_as<T>(__fmul_rn(__fmul_rn((float)sum[j], p.sx[t0 + c0 + j]), wn));
+            if (c0 + j < all && inside((t0 + c0 + j) * p.ldy + n)) y[j * p.ldy] = out_as<T>(__fmul_rn(__fmul_rn((float)sum[j], p.sx[t0 + c0 + j]), wn));
         }
         break;
       }
@@ -429,13 +431,14 @@ __global__ void __launch_bounds__(Cfg<NTOK>::THREADS, 1)
           const float2 s = *reinterpret_cast<const float2*>(sx + c);
           const float u = __fmul_rn(__fmul_rn((float)acc[c], s.x), wn), v = __fmul_rn(__fmul_rn((float)acc[c + 1], s.y), wn);
           const float other = __shfl_xor_sync(0xffffffffu, odd ? u : v, 1);
-          if constexpr (sizeof(T) == 2) *reinterpret_cast<uint32_t*>(y) = odd ? pair_as(other, v, T()) : pair_as(u, other, T());
+          if constexpr (sizeof(T) == 2)
+            if (inside(y - static_cast<T*>(p.y) + 1)) *reinterpret_cast<uint32_t*>(y) = odd ? pair_as(other, v, T()) : pair_as(u, other, T());
           y += 2 * p.ldy;
         }
       } else if (n < p.N) {
 #pragma unroll
         for (int c = 0; c < HALF; ++c)
-          if (c < cols) y[c * p.ldy] = out_as<T>(__fmul_rn(__fmul_rn((float)acc[c], sx[c]), wn));
+          if (c < cols && inside((m0 + c) * p.ldy + n)) y[c * p.ldy] = out_as<T>(__fmul_rn(__fmul_rn((float)acc[c], sx[c]), wn));
       }
     }
   } else {  // ---------------- converters

@@ -61,3 +61,13 @@ def test_parity_cases_raise_no_check_in_the_checked_build():
                 "teacher_output_parity or loss_forward_parity or backward_parity or backward_kl or "
                 "weight_gradient_and_fisher or kl_forward or hutchinson or bit_identical"])
     assert r.returncode == 0, r.stdout[-3000:] + r.stderr[-3000:]
+
+
+def test_serving_cases_raise_no_check_in_the_checked_build():
+    """The projection, the cache and attention by either kernel and joined, on libjab_checked.so: the serving tests'
+    values, and device status 0 after each."""
+    r = _child([sys.executable, "-m", "pytest", "-x", "-q", "-m", "gpu", "-p", "no:cacheprovider",
+                os.path.join("tests", "test_gpu_serve.py"), os.path.join("tests", "test_gpu_serve_ranges.py"), "-k",
+                "linear_pitched or linear_largest or several_tiles or (write_and_read and rope) or wide_blocks or read_of_many or "
+                "long_and_split or shared_prefix or pitched_stream or (many_rows and dt0) or keep_their_bits"])
+    assert r.returncode == 0, r.stdout[-3000:] + r.stderr[-3000:]
