@@ -753,12 +753,15 @@ cudaError_t launch_keys(const AttnParams& p, int64_t est_tiles, int sms, cudaStr
   return launch_after(kern, (unsigned)grid, 32 * W, smem, st, p);
 }
 
+// Tiles that a launch has at most, by the caller's hints, which may be as large as their types hold.
+int64_t estimate(double tiles) { return (int64_t)std::min(tiles, 1e15); }
+
 template <class T, int DH>
 cudaError_t launch_all(AttnParams p, const Route& r, int bits, jab_dtype type, int max_q, int max_len, int sms, cudaStream_t st) {
   cudaError_t e;
   if (r.keys.used) {
     p.list = r.keys;
-    const int64_t est = (int64_t)p.n_kv * p.n_seqs * ((int64_t)max_len / 32 + 1) * std::max<int64_t>(1, (int64_t)max_q * p.G / (8 * r.nt));
+    const int64_t est = estimate((double)p.n_kv * p.n_seqs * (max_len / 32 + 1) * std::max<int64_t>(1, (int64_t)max_q * p.G / (8 * r.nt)));
     if (bits == 8)
       e = r.nt == 1 ? launch_keys<T, DH, 8, 1>(p, est, sms, st) : r.nt == 2 ? launch_keys<T, DH, 8, 2>(p, est, sms, st) : launch_keys<T, DH, 8, 4>(p, est, sms, st);
     else
@@ -769,7 +772,7 @@ cudaError_t launch_all(AttnParams p, const Route& r, int bits, jab_dtype type, i
     p.list = r.tiles;
     p.behind = r.keys.used;
     const int64_t rts = ((int64_t)max_q * p.G + kTileRows - 1) / kTileRows, kts = max_len / kTileKeys + 1;
-    const int64_t est = p.n_kv * (p.n_seqs * rts * kts + (r.tiles.all ? ((int64_t)p.n_tokens * p.G / kTileRows + 1) * kts : 0));
+    const int64_t est = estimate(p.n_kv * ((double)p.n_seqs * rts * kts + (r.tiles.all ? ((double)p.n_tokens * p.G / kTileRows + 1) * kts : 0)));
     if ((e = launch_tiles(p, type, DH, bits, est, std::min(sms, kMaxTileBlocks), st)) != cudaSuccess) return e;
   }
   auto joined = [](const List& l, int rows) {

@@ -255,6 +255,37 @@ def test_a_list_of_work_too_long_to_count_is_reported():
         assert bool((out == 5).all())
 
 
+@pytest.mark.parametrize("max_q,max_len", [(1 << 20, 1 << 20), (2 ** 31 - 1, 2 ** 31 - 1)])
+def test_hints_of_any_size_leave_the_work_to_all_blocks(max_q, max_len):
+    """The longest of the sequences "or more": the same values, and no call of one block (a hundred times as long)."""
+    g = _gen(31)
+    B, page, dh = 64, 64, 128
+    lens = [1024 + 16 * i for i in range(B)]
+    cache, kd, vd = _filled(g, 8, dh, 8, page, sum(-(-n // page) for n in lens))
+    pages = _pages(g, lens, page, cache.n_pages)
+    q = torch.randn((B, 32, dh), generator=g, device="cuda").to(torch.float16)
+    start, length = torch.arange(B + 1, dtype=torch.int32, device="cuda"), torch.tensor(lens, dtype=torch.int32, device="cuda")
+    times, outs = [], []
+    for hints in ((max_q, max_len), (1, max(lens))):
+        out = torch.empty_like(q)
+        ws = torch.empty(J.jab_kv_attention_workspace_size(cache, B, B, 32, *hints), dtype=torch.uint8, device="cuda")
+        best = math.inf
+        for _ in range(5):
+            a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            a.record()
+            J.jab_kv_attention(cache, q, start, pages, length, out, ws, *hints)
+            b.record()
+            b.synchronize()
+            best = min(best, a.elapsed_time(b))
+        times.append(best)
+        outs.append(out)
+    assert J.jab_get_device_status() == 0
+    o, ls, mag, keys, top = _exact(cache, kd, vd, q, [1] * B, lens, pages)
+    for out in outs:
+        _held(out, o, o, (2.0 ** -22 + 2.0 ** -16 + keys * 2.0 ** -26) * mag, keys * 2.0 ** -23 * top)
+    assert times[0] < 10 * times[1], times
+
+
 def test_launches_are_counted():
     """One kernel for the work and one that joins; one more where a chunk and short runs share a call."""
     cache, _, _ = _filled(_gen(1), 1, 64, 8, 16, 40)
