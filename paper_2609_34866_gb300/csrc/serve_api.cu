@@ -64,7 +64,8 @@ jab_status check_attention(const jab_kv_cache* c, int32_t n_seqs, int64_t n_toke
   const jab_status s = check_cache_shape(c);
   if (s != JAB_OK) return s;
   if (n_seqs < 1 || n_tokens < 0 || n_q_heads < 1 || max_q_len < 1 || max_seq_len < 0 || shared_len < 0) return JAB_ERR_INVALID_ARG;
-  if (n_q_heads % c->n_kv_heads != 0 || n_seqs > 2048 || n_tokens * n_q_heads >= (int64_t)1 << 30) return JAB_ERR_UNSUPPORTED;
+  if (n_q_heads % c->n_kv_heads != 0 || n_seqs > 2048 || n_tokens >= (int64_t)1 << 30 || n_tokens * n_q_heads >= (int64_t)1 << 30)
+    return JAB_ERR_UNSUPPORTED;
   if (shared_len % c->page_tokens != 0) return JAB_ERR_UNSUPPORTED;
   return JAB_OK;
 }

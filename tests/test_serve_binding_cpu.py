@@ -1,4 +1,6 @@
 """The binding's side of the serving calls, without a GPU."""
+import ctypes
+
 import pytest
 import torch
 
@@ -38,3 +40,16 @@ def test_current_stream_without_torch_internals(monkeypatch):
     monkeypatch.setattr(binding, "_raw_stream", None)
     assert binding._stream(None) == 1234
     assert binding._stream(Stream()) == 1234 and binding._stream(77) == 77
+
+
+def test_numbers_of_tokens_past_64_bits_are_refused():
+    """n_tokens * n_q_heads is bounded whatever the product does in 64 bits."""
+    from paper_2609_34866_gb300 import build
+    build.build()
+    L = binding.lib()
+    cache = binding._KvCacheDesc(2, 64, 8, 16, 4, 1 << 20, 1 << 20, 1 << 20, 1 << 20)
+    fake = ctypes.c_void_p(1 << 20)  # never dereferenced
+    for n in (1 << 30, 1 << 60, 1 << 62, (1 << 62) + 1, (1 << 63) - 1):
+        assert L.jab_kv_attention_workspace_size(ctypes.byref(cache), 2, n, 4, 1, 64, 0) == 0
+        assert L.jab_kv_attention(ctypes.byref(cache), 2, n, 4, fake, 0, 256, fake, fake, 4, fake, 1, 64, 0, 0, 0.0, fake, 256, None, fake,
+                                  (1 << 64) - 1, None) == 2  # JAB_ERR_UNSUPPORTED
