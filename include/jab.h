@@ -367,8 +367,8 @@ typedef struct {
 } jab_kv_cache;
 
 /* Y[m, n] = s_m w_n sum_k qx[m, k] codes[n, k]: the rows of X are quantised to 8 bits (one scale s_m per
- * token), the sum is exact (whole numbers), and the two products by the scales are rounded to fp32 before
- * the result is rounded to y_type.
+ * token), the sum is exact (whole numbers). Rounded to fp32 it is multiplied by s_m, then by w_n, each
+ * product rounded to fp32, before the result is rounded to y_type.
  *   X_dev         x_type (JAB_FP16 or JAB_BF16) [M, K], pitch ldx
  *   codes_dev     int8 [N, K] (jab_quantize with group_size = d_model, any bit width), 16-byte aligned
  *   w_scales_dev  fp32 [N]
@@ -411,7 +411,11 @@ jab_status jab_kv_read(const jab_kv_cache* cache, int32_t n_seqs, const int32_t*
 /* Attention of new tokens over the cache. Sequence b has the query rows q_start[b] .. q_start[b + 1] - 1
  * of Q, the last ones of its seq_lens[b] cached tokens (they are in the cache already): query i of n sees
  * key j when j <= p and, with window > 0, j > p - window, where p = seq_lens[b] - n + i. A row
- * that sees nothing has output 0 and log-sum-exp -inf.
+ * that sees nothing has output 0 and log-sum-exp -inf. Scores, weights, sums and outputs are fp32 until the
+ * result is rounded to type, but for what the tensor cores take: elements of a bf16 row of Q are within
+ * 2^-39 of the row's largest (exact from 2^-31 of it on), a weight (times V's scale) within 2^-22 of itself or
+ * 2^-29 of the row's largest, whichever is more. A V scale of NaN makes outputs NaN; the log-sum-exp does
+ * not hang on it.
  *   Q_dev        type (JAB_FP16 or JAB_BF16) [n_tokens, n_q_heads * head_dim], pitch ldq
  *   q_start_dev  int32 [n_seqs + 1], increasing from 0 to n_tokens; rows that no sequence has are reported
  *                (JAB_ERR_INVALID_ARG) and left as they are

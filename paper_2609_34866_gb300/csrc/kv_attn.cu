@@ -256,7 +256,7 @@ __device__ __forceinline__ void softmax_step(float (&s)[NS][NT][4], const float2
         wt[c] = see[n][c] ? ex * sc[n][c >> 1].y : 0.f;
       }
       // A weight enters the products as its fp16 value and what that leaves over (2^-22 of it in all): rounded
-      // once, a row with few keys would be 2^-12 off. The products are not what bounds this kernel.
+      // once, a row with few keys would be 2^-11 off. The products are not what bounds this kernel.
 #pragma unroll
       for (int c = 0; c < 4; c += 2) {
         const uint32_t h = tc::pack_half2(wt[c], wt[c + 1]);
@@ -544,8 +544,8 @@ struct Joined {
 // the item's record, then statistics and rows of BATCH parts at once. (One block per item over a chain of five trips took
 // 13 us for 64 sequences of up to 8192 keys.)
 // BATCH: parts of a row on their way at once; 16 for calls with few rows, which have many parts (4 sequences of 65536
-// keys: 69 us in all, 81 with 4), 4 where many blocks an SM are worth more (64 behind a shared prefix of 8192: 76, 77 with
-// 16).
+// keys: 73 us in all, 88 with 4), 4 where many blocks an SM are worth more (2 x 512 queries behind 5000 keys: 150, 159 with
+// 16; in between the difference is small and the other way: 64 behind a shared prefix of 8192 67.6, 65.2 with 16).
 template <class T, int DH, int BATCH>
 __global__ void __launch_bounds__(32 * MW, BATCH == 4 ? 6 : 2)
     kv_merge_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Joined j0, const __grid_constant__ Joined j1) {
@@ -671,10 +671,10 @@ int n_tiles_of_rows(int64_t rows) { return rows <= 8 ? 1 : rows <= 16 ? 2 : 4; }
 
 // Which kernel takes what. Sequences of up to kFewRows (token, head) rows go by 16-key tiles: the cache's bytes bound
 // them, not the products. Longer ones fill 128-row tiles; where lengths are mixed, those of up to kFewBeside rows still go
-// by keys, in a launch of their own. Measured, both ways (heads of 128, 8 bits, G = 4, up to 2048 keys): 64 sequences of 32
-// rows 116 us by keys and 165 by tiles, of 16 rows 61 and 163, of 36 rows 189 and 166, of 64 rows 200 and 170; 4 of 36
-// behind 8192 keys 58 and 44. (With heads of 64 and G = 1 the bound would lie higher: 64 sequences of 40 rows 170 and
-// 224, but 4 of 40 behind 8192 keys 54 and 47.) Beside a chunk of 512 tokens, with bounds of 8, 16 and 32 (G = 4, up to 2048
+// by keys, in a launch of their own. Measured, both ways (heads of 128, 8 bits, G = 4, 300 to 2048 keys): 64 sequences of 16
+// rows 53 us by keys and 135 by tiles, of 32 rows 96 and 138, of 36 rows 143 and 139, of 64 rows 157 and 143; 4 of 32
+// behind 8192 keys 54 and 49, of 36 69 and 49. (With heads of 64 and G = 1 the bound would lie higher: 64 sequences of 40 rows
+// 135 and 181, but 4 of 40 behind 8192 keys 64 and 53.) Beside a chunk of 512 tokens, with bounds of 8, 16 and 32 (G = 4, up to 2048
 // keys): 64 sequences of 4 rows 101, 104 and 149 us, of 16 rows 192, 110 and 156, of 32 rows 195, 197 and 166; with up to
 // 8192 keys 4 rows 131, 139 and 244, 16 rows 276, 147 and 254; single tokens at G = 16 100, 84 and 98. (Rows of one tile wait for
 // the longest of them: a bound of 16 makes all of them 16.)

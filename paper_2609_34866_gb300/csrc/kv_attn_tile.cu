@@ -17,10 +17,12 @@
 //   warps 4..11   softmax: 16 rows a warp, four threads a row (16x256b shape); at an item's end the output
 //   warps 12..15  converters of K, a tile ahead; of Q at an item's start, and of the keys' scales
 //   warps 16..19  converters of V
-// Bound: no unit, but the latency of the softmax: 2500 of the 3300 clocks that a 128 x 128 tile takes, with the issue slots
-// half used (2 x 512 queries behind 5000 keys, 32 heads of 128: 124 us and 28 to join, tensor pipe 21 % busy); 64 more scores
-// read ahead made it 158 in all. Where items are short, the first tile of each, which looks for the maximum first and
-// is taken in two parts, and its output are what counts (12 x 482 queries over their own keys: 226 us).
+// Bound: no unit, but the latency of the softmax: 2800 of the 3500 clocks that a 128 x 128 tile takes (with clock stamps),
+// the issue slots half used (2 x 512 queries, 4100 to 6000 keys, window 4096, 32 heads of 128: 122 us and 28 to join,
+// tensor pipe 32 % busy). With one part of a weight where no mask cuts, the call took as long: the second product runs
+// beside the next softmax. Where items are short, the first tile of each, which looks for the maximum first, its Q and its
+// output are what counts: 12 prompts of 482 tokens over their own keys take 272 us, one of 2048 207, where Q, O and the
+// products need 16 and 18.
 #include <algorithm>
 #include <type_traits>
 

@@ -14,8 +14,8 @@
 // serves one token and thousands. Many tiles: persistent blocks, two accumulators in turn, sums in registers. Few
 // tiles: one a cluster, whose blocks take K ranges of it and add their sums through shared memory.
 //
-// Bound: 8192 tokens x 6144 x 4096 take 293 us, 26 of them for the tokens' codes (0.7 of HBM's rate) and 265 for the
-// products, 1.56 PFLOP/s, 0.82 of the tensor cores' measured rate; without converters, drains and stores the products
+// Bound: 8192 tokens x 6144 x 4096 take 295 to 307 us, 26 of them for the tokens' codes (0.7 of HBM's rate) and 270 for the
+// products, 1.53 PFLOP/s, 0.80 of the tensor cores' measured rate; without converters, drains and stores the products
 // alone took 237 in all. One token (25 MB of codes) takes 12 us where the bytes take 3.7: the chain of launches, copy,
 // conversion and products of 16 stages.
 #include <cudaTypedefs.h>
@@ -152,13 +152,13 @@ template <int NTOK>
 struct Cfg {
   static constexpr int WST = NTOK == 128 ? 4 : 8;  // stages of weight codes
   static constexpr int W_STAGE = TM * LK, X_STAGE = NTOK * LK * 2;
-  // Rows of a box of weights: half as many requests for the copy engine at 128 bytes (64 tokens x 6144 x 4096: 14.7 us, at 64
-  // bytes 15.2), but the largest calls like the converters' reads of 64 better (8192 tokens: 293 us, at 128 bytes 305).
+  // Rows of a box of weights: half as many requests for the copy engine at 128 bytes (64 tokens x 6144 x 4096: 14.1 us, at 64
+  // bytes 14.6), but the largest calls like the converters' reads of 64 better (8192 tokens: 297 us, at 128 bytes 306).
   static constexpr int W_ROW = NTOK == 128 ? BK : LK;
   static constexpr int D_COLS = NTOK < 32 ? 32 : NTOK;
   static constexpr int GROUPS = NTOK == 128 ? 2 : 4, THREADS = 32 * (4 + 8 + 4 * GROUPS);
   static constexpr int EPI_REGS = NTOK == 128 ? 128 : 96, CONV_REGS = NTOK == 128 ? 88 : 64;
-  static constexpr bool SPLIT = NTOK < 128;  // whether clusters share a tile (128 tokens x 6144 x 4096: 17.9 us so, 19.3 without; the code costs the largest calls 5 %)
+  static constexpr bool SPLIT = NTOK < 128;  // whether clusters share a tile (128 tokens x 6144 x 4096: 18.2 us so, 18.3 without; the code costs 512 tokens and the largest calls 5 %)
   static constexpr int SMEM = WST * W_STAGE + LST * X_STAGE + 1024 + 512 + 8 * (NTOK / 2) * 4;
   static_assert(NTOK * TM * 4 <= WST * W_STAGE, "a tile's sums take the weights' place");
   static_assert(128 * 40 + 256 * EPI_REGS + 128 * GROUPS * CONV_REGS <= THREADS * (65536 / THREADS / 8 * 8), "registers");
@@ -539,7 +539,7 @@ Scratch plan_scratch(int64_t M, int N, int K) {
 
 // K ranges of a tile: as many as leave no cluster waiting for another to end, of 1024 and more each. A cluster costs 2 us
 // (its launch, the meeting of its blocks, the sums' way), a stage of 128 a quarter of one: 64 tokens x 6144 x 4096 take
-// 14.5 us in two ranges and 16.5 in one, x 2304 x 768 9.3 in three and 7.3 in one.
+// 14.1 us in two ranges and 15.6 in one, x 2304 x 768 9.3 in three and 6.8 in one.
 template <class C, class Kernel>
 int ranges_of(Kernel kern, const LinParams& p, int sms, int dev, Found& fit) {
   const int64_t tiles = (int64_t)p.tiles_n * p.tiles_m;
