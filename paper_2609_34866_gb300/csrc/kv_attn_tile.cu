@@ -517,6 +517,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_tile_kernel(const __grid_consta
               }
               if (!(ok = before_o())) break;
               if (s > it.s0) scale_rows<DH>(tw + L::O_COL, f);
+              tc::tmem_st_wait();  // the first 64 weights are read back (scale_rows has waited for them too: no tile here is an item's first)
 #pragma unroll 1
               for (int part = 0; part < 2 * b; ++part) {
                 uint32_t e[16];
