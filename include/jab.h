@@ -440,6 +440,138 @@ jab_status jab_kv_attention(const jab_kv_cache* cache, int32_t n_seqs, int64_t n
                             int32_t shared_len, int32_t window, float softmax_scale, void* O_dev,
                             int64_t ldo, float* lse_dev, void* ws, size_t ws_bytes, jab_stream_t stream);
 
+/* Weights, or any rows, in 8-bit floating point (e4m3: 4 significant bits, 448 at most) with an fp32 scale for every block
+ * of block_rows rows (1 or 128) x 128 columns; the last blocks of either may be shorter:
+ *     s = fl32(max|x| / 448),  code = e4m3(fl32(x / s)), rounded to nearest even, at most 448 in magnitude
+ * A block of zeros has s = 0 and codes 0. One with an infinity or a NaN has s = NaN and codes 0, and raises
+ * JAB_ERR_NONFINITE on the device.
+ *   X_dev       type [M, K], pitch ldx
+ *   codes_dev   out e4m3 bytes [M, K], 16-byte aligned
+ *   scales_dev  out fp32 [ceil(M / block_rows), ceil(K / 128)]
+ * K a multiple of 16 up to 131072; M >= 0 (0: nothing to do). */
+jab_status jab_fp8_quantize(int64_t M, int32_t K, const void* X_dev, jab_dtype type, int64_t ldx, int32_t block_rows,
+                            void* codes_dev, float* scales_dev, jab_stream_t stream);
+
+/* Y[m, n] = sum_b sx[m, b] w_scales[n / block_rows, b] sum_{k in block b} qx[m, k] codes[n, k], blocks of 128 of K: the rows
+ * of X are quantised as by jab_fp8_quantize with block_rows = 1. A block's sum is fp32, as the tensor cores add it up, its
+ * products with the two scales and the sum over the blocks are rounded to fp32, the result to y_type. (With block_rows =
+ * 128 the two scales are multiplied first: a product of theirs below 2^-126 loses bits.)
+ * The codes of jab_quantize of up to 5 bits at group_size = 128 are e4m3 numbers as they are: a fitted block is served with
+ * them and its scales, block_rows = 1.
+ *   X_dev         x_type (any of the three) [M, K], pitch ldx
+ *   codes_dev     e4m3 bytes [N, K], 16-byte aligned
+ *   w_scales_dev  fp32 [ceil(N / block_rows), ceil(K / 128)]; block_rows 1 or 128
+ *   Y_dev         out y_type [M, N], pitch ldy
+ * K a multiple of 16 up to 131072; M >= 0 (0: nothing to do), N >= 1. ws 256-byte aligned. Sums run in a fixed order:
+ * repeated calls give the same bits. */
+size_t jab_fp8_linear_workspace_size(int64_t M, int32_t N, int32_t K);
+jab_status jab_fp8_linear(int64_t M, int32_t N, int32_t K, const void* X_dev, jab_dtype x_type, int64_t ldx,
+                          const void* codes_dev, const float* w_scales_dev, int32_t block_rows, void* Y_dev,
+                          jab_dtype y_type, int64_t ldy, void* ws, size_t ws_bytes, jab_stream_t stream);
+
+/* Tables for the rotation by position p in contexts longer than those that a block was trained on. With f_j =
+ * theta^(-2j / rotary_dim):
+ *   JAB_ROPE_PLAIN     angles p f_j
+ *   JAB_ROPE_LINEAR    angles p f_j / factor
+ *   JAB_ROPE_BY_PARTS  with t_j = original_length f_j / (2 pi), the turns that a pair takes in the original context, and
+ *                      g_j = clip((t_j - low_turns) / (high_turns - low_turns), 0, 1): angles p (g_j f_j + (1 - g_j) f_j /
+ *                      factor). Fast pairs stay as they are, slow ones are stretched.
+ * Every cos and sin is multiplied by `attention` (1: plain; some blocks scale their scores that way). */
+typedef enum { JAB_ROPE_PLAIN = 0, JAB_ROPE_LINEAR = 1, JAB_ROPE_BY_PARTS = 2 } jab_rope_kind;
+typedef struct {
+  int32_t kind;             /* jab_rope_kind                                          */
+  float factor;             /* >= 1 (kind 0: not read)                                */
+  float original_length;    /* tokens, > 0 (kind 2)                                   */
+  float low_turns;          /* >= 0 (kind 2)                                          */
+  float high_turns;         /* > low_turns (kind 2)                                   */
+  float attention;          /* > 0                                                    */
+} jab_rope_scaling;
+
+/* cos and sin, fp32 [length, rotary_dim / 2] each, from angles in 64 bits. rotary_dim a multiple of 16 up to 128.
+ * scaling == NULL: plain. */
+jab_status jab_rope_table_scaled(int32_t length, int32_t rotary_dim, float theta, const jab_rope_scaling* scaling,
+                                 float* cos_dev, float* sin_dev, jab_stream_t stream);
+
+/* What is done to the heads of Q and K of a row before they are used: a norm for each head, then the rotation.
+ *   norm (norm != 0)    r = 1 / sqrt(mean x^2 + eps) of the head, rounded to fp32 (nearest but for one in 2^16 or fewer), then
+ *                       fl32(fl32(x r) w). eps within 1e-30 .. 1e30. A row whose squares leave fp32's range, or with an infinity or a
+ *                       NaN, has r = NaN and raises JAB_ERR_NONFINITE.
+ *   q_weight, k_weight  fp32 [head_dim] on the device, 16-byte aligned, or NULL: all 1
+ *   rotation            (positions_dev != NULL) elements [0, rotary_dim) of each head by the table rows of the token's position; the
+ *                       others stay. Pair j is (j, j + rotary_dim / 2), or (2j, 2j + 1) with interleaved != 0:
+ *                       (a cos - b sin, b cos + a sin), each product and sum rounded to fp32.
+ *   positions_dev       int32 [n_tokens], each in [0, rope_len)
+ *   cos_dev, sin_dev    fp32 [rope_len, rotary_dim / 2], 16-byte aligned; rotary_dim a multiple of 16 up to head_dim */
+typedef struct {
+  int32_t norm;
+  float eps;
+  const float *q_weight_dev, *k_weight_dev;
+  const int32_t* positions_dev;
+  const float *cos_dev, *sin_dev;
+  int32_t rope_len, rotary_dim, interleaved;
+} jab_norm_rope;
+
+/* jab_kv_write with that in place of its rotation: Q and K are normed and rotated, V is not; K and V are quantised and
+ * written to the tokens' slots, Q goes to Q_dev. Arguments, padding (slots below 0) and errors as for jab_kv_write. */
+jab_status jab_kv_write_norm_rope(const jab_kv_cache* cache, int64_t n_tokens, int32_t n_q_heads, const void* X_dev,
+                                  jab_dtype type, int64_t ldx, const int64_t* slots_dev, const jab_norm_rope* how,
+                                  void* Q_dev, jab_stream_t stream);
+
+/* The same for rows that go to no cache (prompts, training batches):
+ *   X_dev         type [n_tokens, at least (n_q_heads + n_k_heads) * head_dim], pitch ldx: heads of Q, then of K; what
+ *                 lies behind them (V) is not read
+ *   Q_dev, K_dev  out type [n_tokens, n_q_heads * head_dim] and [n_tokens, n_k_heads * head_dim], pitches ldq, ldk; they may be the
+ *                 places of Q and K in X themselves. NULL where there are no such heads
+ * A token whose position is out of range is reported (JAB_ERR_INVALID_ARG) and its outputs are left as they are.
+ * head_dim 64 or 128; n_q_heads + n_k_heads up to 4096. */
+jab_status jab_qk_norm_rope(int64_t n_tokens, int32_t n_q_heads, int32_t n_k_heads, int32_t head_dim, const void* X_dev,
+                            jab_dtype type, int64_t ldx, const jab_norm_rope* how, void* Q_dev, int64_t ldq, void* K_dev,
+                            int64_t ldk, jab_stream_t stream);
+
+/* Its gradient. With y = R n, n = (x r) w: g = R^T dy, u = g w, dx = r (u - x r mean(u x r)), dw = sum over tokens and heads
+ * of g x r (without a norm dx = g).
+ *   dQ_dev, dK_dev    type, gradients of the outputs, pitches lddq, lddk
+ *   dX_dev            out type, columns [0, (n_q_heads + n_k_heads) * head_dim) of rows of pitch lddx; the others are left as
+ *                     they are
+ *   dq_weight_dev, dk_weight_dev  out fp32 [head_dim], or NULL: not wanted (both NULL without a norm)
+ * X, dQ, dK and dX do not overlap. A token whose position is out of range is reported; its dX is left as it is and it adds
+ * nothing to the weights' gradients. Sums run in a fixed order: repeated calls give the same bits. ws 256-byte aligned. */
+size_t jab_qk_norm_rope_backward_workspace_size(int64_t n_tokens, int32_t n_q_heads, int32_t n_k_heads, int32_t head_dim);
+jab_status jab_qk_norm_rope_backward(int64_t n_tokens, int32_t n_q_heads, int32_t n_k_heads, int32_t head_dim,
+                                     const void* X_dev, jab_dtype type, int64_t ldx, const jab_norm_rope* how,
+                                     const void* dQ_dev, int64_t lddq, const void* dK_dev, int64_t lddk, void* dX_dev,
+                                     int64_t lddx, float* dq_weight_dev, float* dk_weight_dev, void* ws, size_t ws_bytes,
+                                     jab_stream_t stream);
+
+/* A server step's bookkeeping on the device: page tables, lengths and a stack of free pages, with no word to or from the
+ * host, so that a captured graph of a step can be replayed. Of the cache only page_tokens and n_pages count.
+ *
+ * jab_kv_release: the pages of sequences that have ended (ended[b] != 0) go back to the stack, sequence by sequence and each
+ * in its order, but for those of the first shared_len tokens (a multiple of page_tokens), which other sequences use too:
+ *   new_lens[b] = ended ? min(lens[b], shared_len) : lens[b],  new_free = n_free + pages given back
+ * jab_kv_plan: places for the next counts[b] tokens of every sequence, pages from the top of the stack where one begins:
+ *   new_lens[b] = lens[b] + counts[b],  q_start[b] = counts[0] + ... + counts[b - 1],
+ *   positions[q_start[b] + i] = lens[b] + i,  slots[...] = page * page_tokens + offset of that token
+ * Rows from q_start[n_seqs] on are padding: slot -1, position 0. (jab_kv_attention wants every row to belong to a sequence: give
+ * it one sequence more, of length 0, whose rows end at n_tokens.)
+ *   lens_dev, counts_dev, ended_dev  int32 [n_seqs]
+ *   pages_dev       int32 [n_seqs, max_pages]; jab_kv_plan writes the entries of the pages that it hands out
+ *   free_dev        int32 [free_capacity], the first n_free entries are free pages; jab_kv_release writes behind them
+ *   n_free_dev, new_free_dev  int32 [1]; new_lens_dev int32 [n_seqs]: they may be the same buffers as n_free_dev and lens_dev
+ *   q_start_dev     out int32 [n_seqs + 1]; slots_dev out int64 [n_tokens], positions_dev out int32 [n_tokens]
+ * A call that cannot be carried out as a whole changes no pages and no stack: a length or count below 0, a sequence past
+ * max_pages pages, more tokens than n_tokens, too few free pages, a stack that would outgrow free_capacity. It raises
+ * JAB_ERR_INVALID_ARG on the device, new_lens = lens, new_free = n_free, and all rows are padding (q_start all 0). A page
+ * number outside the cache raises it too; the token's slot is then -1. n_seqs up to 8192, max_pages * page_tokens < 2^30. */
+jab_status jab_kv_release(const jab_kv_cache* cache, int32_t n_seqs, const int32_t* lens_dev, const int32_t* ended_dev,
+                          const int32_t* pages_dev, int32_t max_pages, int32_t shared_len, int32_t* free_dev,
+                          int32_t free_capacity, const int32_t* n_free_dev, int32_t* new_lens_dev, int32_t* new_free_dev,
+                          jab_stream_t stream);
+jab_status jab_kv_plan(const jab_kv_cache* cache, int32_t n_seqs, int64_t n_tokens, const int32_t* lens_dev,
+                       const int32_t* counts_dev, int32_t* pages_dev, int32_t max_pages, const int32_t* free_dev,
+                       int32_t free_capacity, const int32_t* n_free_dev, int32_t* new_lens_dev, int32_t* new_free_dev,
+                       int32_t* q_start_dev, int64_t* slots_dev, int32_t* positions_dev, jab_stream_t stream);
+
 /* ---- Instrumentation (not part of the method): per-launch-site device time with CUDA events. ----
  * jab_timing_enable(1) makes every later entry-point call record a CUDA event pair on its stream
  * around each of its kernel launch sites. jab_timing_collect synchronises those events and folds

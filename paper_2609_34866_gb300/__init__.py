@@ -17,4 +17,7 @@ from .binding import (  # noqa: F401
     jab_set_deterministic, jab_selftest_bounds_check, jab_loss_backward_scales_kl,
     KvCache, jab_quantized_linear, jab_quantized_linear_workspace_size, jab_rope_table, jab_kv_write,
     jab_kv_read, jab_kv_attention, jab_kv_attention_workspace_size,
+    jab_fp8_quantize, jab_fp8_linear, jab_fp8_linear_workspace_size, jab_rope_table_scaled,
+    jab_kv_write_norm_rope, jab_qk_norm_rope, jab_qk_norm_rope_backward,
+    jab_qk_norm_rope_backward_workspace_size, jab_kv_release, jab_kv_plan,
 )

@@ -61,6 +61,22 @@ class _KvCacheDesc(ctypes.Structure):
                 ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p)]
 
 
+class _RopeScaling(ctypes.Structure):
+    """jab_rope_scaling"""
+
+    _fields_ = [("kind", ctypes.c_int32), ("factor", ctypes.c_float), ("original_length", ctypes.c_float),
+                ("low_turns", ctypes.c_float), ("high_turns", ctypes.c_float), ("attention", ctypes.c_float)]
+
+
+class _NormRope(ctypes.Structure):
+    """jab_norm_rope"""
+
+    _fields_ = [("norm", ctypes.c_int32), ("eps", ctypes.c_float), ("q_weight", ctypes.c_void_p),
+                ("k_weight", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("cos", ctypes.c_void_p),
+                ("sin", ctypes.c_void_p), ("rope_len", ctypes.c_int32), ("rotary_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32)]
+
+
 _P = ctypes.c_void_p
 _LIB = None
 
@@ -128,8 +144,24 @@ def lib() -> ctypes.CDLL:
     L.jab_kv_attention_workspace_size.restype = sz
     L.jab_kv_attention.argtypes = [KV, i32, i64, i32, _P, i32, i64, _P, _P, i32, _P, i32, i32, i32, i32, f32,
                                    _P, i64, _P, _P, sz, _P]
+    H = ctypes.POINTER(_NormRope)
+    L.jab_fp8_quantize.argtypes = [i64, i32, _P, i32, i64, i32, _P, _P, _P]
+    L.jab_fp8_linear_workspace_size.argtypes = [i64, i32, i32]
+    L.jab_fp8_linear_workspace_size.restype = sz
+    L.jab_fp8_linear.argtypes = [i64, i32, i32, _P, i32, i64, _P, _P, i32, _P, i32, i64, _P, sz, _P]
+    L.jab_rope_table_scaled.argtypes = [i32, i32, f32, ctypes.POINTER(_RopeScaling), _P, _P, _P]
+    L.jab_kv_write_norm_rope.argtypes = [KV, i64, i32, _P, i32, i64, _P, H, _P, _P]
+    L.jab_qk_norm_rope.argtypes = [i64, i32, i32, i32, _P, i32, i64, H, _P, i64, _P, i64, _P]
+    L.jab_qk_norm_rope_backward_workspace_size.argtypes = [i64, i32, i32, i32]
+    L.jab_qk_norm_rope_backward_workspace_size.restype = sz
+    L.jab_qk_norm_rope_backward.argtypes = [i64, i32, i32, i32, _P, i32, i64, H, _P, i64, _P, i64, _P, i64, _P, _P, _P,
+                                            sz, _P]
+    L.jab_kv_release.argtypes = [KV, i32, _P, _P, _P, i32, i32, _P, i32, _P, _P, _P, _P]
+    L.jab_kv_plan.argtypes = [KV, i32, i64, _P, _P, _P, i32, _P, i32, _P, _P, _P, _P, _P, _P, _P]
     for fn in ("jab_reference_forward", "jab_loss_forward", "jab_loss_forward_noalloc",
                "jab_quantized_linear", "jab_rope_table", "jab_kv_write", "jab_kv_read", "jab_kv_attention",
+               "jab_fp8_quantize", "jab_fp8_linear", "jab_rope_table_scaled", "jab_kv_write_norm_rope",
+               "jab_qk_norm_rope", "jab_qk_norm_rope_backward", "jab_kv_release", "jab_kv_plan",
                "jab_loss_backward_scales", "jab_loss_backward_weights", "jab_allocate_bits",
                "jab_prepare_x", "jab_loss_backward_scales_prepared", "jab_flip_rate",
                "jab_loss_backward_scales_kl",
@@ -563,6 +595,189 @@ def jab_kv_attention(cache: KvCache, q, q_start, pages, seq_lens, out, ws, max_q
         None if lse is None else _shaped(lse, (n, hq), torch.float32, "lse"), _ptr(ws, torch.uint8, "ws"), ws.numel(),
         _stream(stream))
     _check(st, "jab_kv_attention")
+
+
+_FP8 = torch.float8_e4m3fn
+
+
+def _fp8_scales(t: torch.Tensor, rows: int, K: int, block_rows: int, name: str) -> int:
+    if block_rows not in (1, 128):
+        raise ValueError("block_rows must be 1 or 128")
+    return _shaped(t, (-(-rows // block_rows), -(-K // 128)), torch.float32, name)
+
+
+def jab_fp8_quantize(x, codes, scales, block_rows: int = 128, stream=None):
+    """Rows x (fp16 / bf16 / fp32 [M, K], may have a pitch) as codes (float8_e4m3fn [M, K]) with a scale for every block of
+    block_rows (1 or 128) rows x 128 columns: scales fp32 [ceil(M / block_rows), ceil(K / 128)]."""
+    M, K = x.shape
+    xp, ldx = _rows(x, K, "x")
+    st = lib().jab_fp8_quantize(M, K, xp, _dtype(x, "x"), ldx, int(block_rows), _shaped(codes, (M, K), _FP8, "codes"),
+                                _fp8_scales(scales, M, K, block_rows, "scales"), _stream(stream))
+    _check(st, "jab_fp8_quantize")
+
+
+def jab_fp8_linear_workspace_size(M: int, N: int, K: int) -> int:
+    return int(lib().jab_fp8_linear_workspace_size(M, N, K))
+
+
+def jab_fp8_linear(x, codes, w_scales, y, ws, block_rows: int = 128, stream=None):
+    """y[m, n] = the product of x's rows, quantised to e4m3 with a scale for every 128 elements, with the weights that codes
+    (float8_e4m3fn [N, K]) and w_scales (fp32 [ceil(N / block_rows), ceil(K / 128)]) stand for. x and y fp16 / bf16 /
+    fp32 [M, K] and [M, N], rows may have a pitch; ws uint8, jab_fp8_linear_workspace_size bytes."""
+    (M, K), N = x.shape, codes.shape[0]
+    xp, ldx = _rows(x, K, "x")
+    yp, ldy = _rows(y, N, "y", M)
+    st = lib().jab_fp8_linear(M, N, K, xp, _dtype(x, "x"), ldx, _shaped(codes, (N, K), _FP8, "codes"),
+                              _fp8_scales(w_scales, N, K, block_rows, "w_scales"), int(block_rows), yp, _dtype(y, "y"), ldy,
+                              _ptr(ws, torch.uint8, "ws"), ws.numel(), _stream(stream))
+    _check(st, "jab_fp8_linear")
+
+
+_ROPE_KINDS = {"plain": 0, "linear": 1, "by_parts": 2}
+
+
+def jab_rope_table_scaled(cos, sin, theta: float, kind: str = "plain", factor: float = 1.0, original_length: float = 0.0,
+                          low_turns: float = 1.0, high_turns: float = 32.0, attention: float = 1.0, stream=None):
+    """cos and sin of the angles position * f_j into fp32 [length, rotary_dim / 2] each, times `attention`. f_j = theta^(-2j /
+    rotary_dim) ("plain"), divided by factor ("linear"), or that for pairs of low_turns and fewer in original_length
+    tokens, unchanged for those of high_turns and more and in between in between ("by_parts")."""
+    scaling = _RopeScaling(_ROPE_KINDS[kind], float(factor), float(original_length), float(low_turns), float(high_turns),
+                           float(attention))
+    st = lib().jab_rope_table_scaled(cos.shape[0], 2 * cos.shape[1], float(theta), ctypes.byref(scaling),
+                                     _ptr(cos, torch.float32, "cos"), _shaped(sin, cos.shape, torch.float32, "sin"),
+                                     _stream(stream))
+    _check(st, "jab_rope_table_scaled")
+
+
+def _norm_rope(n: int, dh: int, positions, rope, interleaved, norm_eps, q_weight, k_weight) -> _NormRope:
+    how = _NormRope()
+    if norm_eps is not None:
+        how.norm, how.eps = 1, float(norm_eps)
+        how.q_weight, how.k_weight = (None if w is None else _shaped(w, (dh,), torch.float32, name)
+                                      for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")))
+    elif q_weight is not None or k_weight is not None:
+        raise ValueError("weights of a norm need norm_eps")
+    if rope is not None:
+        if positions is None:
+            raise ValueError("rope needs positions")
+        length, half = rope[0].shape
+        how.cos, how.sin = (_shaped(t, (length, half), torch.float32, "rope") for t in rope)
+        how.positions = _shaped(positions, (n,), torch.int32, "positions")
+        how.rope_len, how.rotary_dim, how.interleaved = length, 2 * half, int(bool(interleaved))
+    return how
+
+
+def jab_kv_write_norm_rope(cache: KvCache, qkv, n_q_heads: int, slots, q_out=None, positions=None, rope=None,
+                           interleaved: bool = False, norm_eps: Optional[float] = None, q_weight=None, k_weight=None,
+                           stream=None):
+    """jab_kv_write with a norm for each head of Q and K (norm_eps; weights fp32 [head_dim], None: all 1) and then the
+    rotation of their first elements: as many as the table rope = (cos, sin), fp32 [length, rotary_dim / 2] each, has
+    angles for, in pairs (j, j + rotary_dim / 2) or, interleaved, (2j, 2j + 1)."""
+    n, dh = qkv.shape[0], cache.head_dim
+    xp, ldx = _rows(qkv, (n_q_heads + 2 * cache.n_kv_heads) * dh, "qkv")
+    how = _norm_rope(n, dh, positions, rope, interleaved, norm_eps, q_weight, k_weight)
+    if q_out is not None:
+        if q_out.numel() != n * n_q_heads * dh:
+            raise ValueError("q_out must be [n_tokens, n_q_heads * head_dim] in qkv's type")
+        q_out = _ptr(q_out, qkv.dtype, "q_out")
+    st = lib().jab_kv_write_norm_rope(cache.ref, n, int(n_q_heads), xp, _dtype(qkv, "qkv"), ldx,
+                                      _shaped(slots, (n,), torch.int64, "slots"), ctypes.byref(how), q_out, _stream(stream))
+    _check(st, "jab_kv_write_norm_rope")
+
+
+def _heads(t, n: int, heads: int, dh: int, like, name: str):
+    """(pointer, pitch) of rows of `heads` heads; no such heads: (None, 0)."""
+    if heads == 0:
+        return None, 0
+    if t.dtype != like.dtype:
+        raise ValueError(f"{name} must have x's type")
+    return _rows(t, heads * dh, name, n)
+
+
+def _wide_rows(t, width: int, name: str, rows: int):
+    """(pointer, pitch) of rows of `width` contiguous elements and more."""
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] < width or (t.shape[1] != 1 and t.stride(1) != 1) or not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor of {rows} rows of at least {width} contiguous elements")
+    return t.data_ptr(), t.stride(0) if rows > 1 else t.shape[1]
+
+
+def jab_qk_norm_rope(x, n_q_heads: int, n_k_heads: int, head_dim: int, q, k, positions=None, rope=None,
+                     interleaved: bool = False, norm_eps: Optional[float] = None, q_weight=None, k_weight=None, stream=None):
+    """The norm and rotation of jab_kv_write_norm_rope on the heads of Q and K at the front of the rows x (fp16 / bf16 /
+    fp32 [n_tokens, (n_q_heads + n_k_heads) * head_dim and more]), into q and k ([n_tokens, heads * head_dim], x's type, rows
+    may have a pitch; views of x itself will do)."""
+    n = x.shape[0]
+    xp, ldx = _wide_rows(x, (n_q_heads + n_k_heads) * head_dim, "x", n)
+    qp, ldq = _heads(q, n, n_q_heads, head_dim, x, "q")
+    kp, ldk = _heads(k, n, n_k_heads, head_dim, x, "k")
+    how = _norm_rope(n, head_dim, positions, rope, interleaved, norm_eps, q_weight, k_weight)
+    st = lib().jab_qk_norm_rope(n, int(n_q_heads), int(n_k_heads), int(head_dim), xp, _dtype(x, "x"), ldx, ctypes.byref(how),
+                                qp, ldq, kp, ldk, _stream(stream))
+    _check(st, "jab_qk_norm_rope")
+
+
+def jab_qk_norm_rope_backward_workspace_size(n_tokens: int, n_q_heads: int, n_k_heads: int, head_dim: int) -> int:
+    return int(lib().jab_qk_norm_rope_backward_workspace_size(n_tokens, n_q_heads, n_k_heads, head_dim))
+
+
+def jab_qk_norm_rope_backward(x, n_q_heads: int, n_k_heads: int, head_dim: int, dq, dk, dx, ws=None, positions=None, rope=None,
+                              interleaved: bool = False, norm_eps: Optional[float] = None, q_weight=None, k_weight=None,
+                              dq_weight=None, dk_weight=None, stream=None):
+    """The gradient of jab_qk_norm_rope: from x as it was and the gradients dq and dk of its outputs, dx (the columns of Q and
+    K) and, where they are given, dq_weight and dk_weight (fp32 [head_dim]). ws uint8 (with a weight's gradient only),
+    jab_qk_norm_rope_backward_workspace_size bytes."""
+    n = x.shape[0]
+    width = (n_q_heads + n_k_heads) * head_dim
+    xp, ldx = _wide_rows(x, width, "x", n)
+    dxp, lddx = _wide_rows(dx, width, "dx", n)
+    if dx.dtype != x.dtype:
+        raise ValueError("dx must have x's type")
+    qp, ldq = _heads(dq, n, n_q_heads, head_dim, x, "dq")
+    kp, ldk = _heads(dk, n, n_k_heads, head_dim, x, "dk")
+    how = _norm_rope(n, head_dim, positions, rope, interleaved, norm_eps, q_weight, k_weight)
+    dw = [None if w is None else _shaped(w, (head_dim,), torch.float32, "dq_weight and dk_weight") for w in (dq_weight, dk_weight)]
+    st = lib().jab_qk_norm_rope_backward(n, int(n_q_heads), int(n_k_heads), int(head_dim), xp, _dtype(x, "x"), ldx,
+                                         ctypes.byref(how), qp, ldq, kp, ldk, dxp, lddx, *dw, _ptr(ws, torch.uint8, "ws"),
+                                         0 if ws is None else ws.numel(), _stream(stream))
+    _check(st, "jab_qk_norm_rope_backward")
+
+
+def _counters(n_free, new_free, lens, new_lens, B: int):
+    """Pointers of (n_free, new_lens, new_free); what is not given is updated in place."""
+    return (_shaped(n_free, (1,), torch.int32, "n_free"),
+            _shaped(lens if new_lens is None else new_lens, (B,), torch.int32, "new_lens"),
+            _shaped(n_free if new_free is None else new_free, (1,), torch.int32, "new_free"))
+
+
+def jab_kv_release(cache: KvCache, seq_lens, ended, pages, free_pages, n_free, shared_len: int = 0, new_lens=None,
+                   new_free=None, stream=None):
+    """The pages of the sequences with ended[b] != 0 back onto the stack free_pages (int32 [capacity], n_free [1] of them
+    free), but for those of the first shared_len tokens. seq_lens, ended int32 [n_seqs], pages int32 [n_seqs,
+    max_pages]; the lengths and the stack's size afterwards go to new_lens and new_free, None: in place."""
+    B = seq_lens.shape[0]
+    nf, nl, nn = _counters(n_free, new_free, seq_lens, new_lens, B)
+    st = lib().jab_kv_release(cache.ref, B, _shaped(seq_lens, (B,), torch.int32, "seq_lens"),
+                              _shaped(ended, (B,), torch.int32, "ended"),
+                              _shaped(pages, (B, pages.shape[1]), torch.int32, "pages"), pages.shape[1], int(shared_len),
+                              _shaped(free_pages, (free_pages.numel(),), torch.int32, "free_pages"), free_pages.numel(), nf, nl,
+                              nn, _stream(stream))
+    _check(st, "jab_kv_release")
+
+
+def jab_kv_plan(cache: KvCache, seq_lens, counts, pages, free_pages, n_free, q_start, slots, positions, new_lens=None,
+                new_free=None, stream=None):
+    """Places for the next counts[b] tokens of every sequence: pages from the top of the stack where one begins (into
+    pages), q_start int32 [n_seqs + 1], and for every row slots (int64 [n_tokens], -1: padding behind the last sequence) and
+    positions (int32 [n_tokens]). Other arguments as for jab_kv_release."""
+    B, n = seq_lens.shape[0], slots.shape[0]
+    nf, nl, nn = _counters(n_free, new_free, seq_lens, new_lens, B)
+    st = lib().jab_kv_plan(cache.ref, B, n, _shaped(seq_lens, (B,), torch.int32, "seq_lens"),
+                           _shaped(counts, (B,), torch.int32, "counts"),
+                           _shaped(pages, (B, pages.shape[1]), torch.int32, "pages"), pages.shape[1],
+                           _shaped(free_pages, (free_pages.numel(),), torch.int32, "free_pages"), free_pages.numel(), nf, nl, nn,
+                           _shaped(q_start, (B + 1,), torch.int32, "q_start"), _shaped(slots, (n,), torch.int64, "slots"),
+                           _shaped(positions, (n,), torch.int32, "positions"), _stream(stream))
+    _check(st, "jab_kv_plan")
 
 
 def jab_selftest_wait_timeout(stream=None):

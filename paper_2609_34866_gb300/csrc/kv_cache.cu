@@ -11,36 +11,11 @@
 
 #include "common.cuh"
 #include "quotient.cuh"
+#include "rows.cuh"
 #include "serve.h"
 
 namespace jab {
 namespace {
-
-__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
-  const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
-  v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-}
-
-__device__ __forceinline__ uint32_t pack2(float a, float b, half_t) {
-  const __half2 h = __floats2half2_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-__device__ __forceinline__ uint32_t pack2(float a, float b, bf16_t) {
-  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-template <class T, int N>
-__device__ __forceinline__ void store(T* p, const float (&v)[N]) {
-#pragma unroll
-  for (int i = 0; i < N; i += 8)
-    *reinterpret_cast<uint4*>(p + i) = make_uint4(pack2(v[i], v[i + 1], T()), pack2(v[i + 2], v[i + 3], T()),
-                                                  pack2(v[i + 4], v[i + 5], T()), pack2(v[i + 6], v[i + 7], T()));
-}
-template <int N>
-__device__ __forceinline__ void store(float* p, const float (&v)[N]) {
-#pragma unroll
-  for (int i = 0; i < N; i += 4) *reinterpret_cast<float4*>(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-}
 
 struct WriteParams {
   const void* x;
@@ -54,6 +29,13 @@ struct WriteParams {
   uint8_t *k_codes, *v_codes;
   float *k_scales, *v_scales;
   int* status;
+  // kWriteNormed and kRows
+  int64_t ldq, ldk;      // kRows (Q of the others has no pitch)
+  void* k_out;           // kRows
+  const float *wq, *wk;  // of the norms, or null
+  float eps;             // 0: no norm
+  int rotary;            // elements that are turned
+  bool neighbours;       // pairs (2j, 2j + 1)
 };
 
 // Codes of 8 elements of a row with scale s (> 0), offset by 2^(BITS - 1): bytes, or halves of bytes.
@@ -85,40 +67,9 @@ __device__ __forceinline__ void codes8(const float (&x)[8], float s, uint32_t (&
   }
 }
 
-// Eight elements of a row as they lie in memory.
-template <class T>
-struct Raw8 {
-  uint4 w[sizeof(T) / 2];
-  __device__ __forceinline__ void load(const T* p) {
-#pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = __ldcs(reinterpret_cast<const uint4*>(p) + i);
-  }
-  __device__ __forceinline__ void numbers(float (&x)[8]) const {
-    if constexpr (sizeof(T) == 4) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-        x[4 * i] = __uint_as_float(w[i].x), x[4 * i + 1] = __uint_as_float(w[i].y), x[4 * i + 2] = __uint_as_float(w[i].z), x[4 * i + 3] = __uint_as_float(w[i].w);
-    } else {
-      const uint32_t u[4] = {w[0].x, w[0].y, w[0].z, w[0].w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if constexpr (std::is_same<T, half_t>::value) {
-          const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u[i]));
-          x[2 * i] = f.x, x[2 * i + 1] = f.y;
-        } else {
-          x[2 * i] = __uint_as_float(u[i] << 16), x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
-        }
-      }
-    }
-  }
-};
-
-// The largest magnitude of three, or NaN if one is NaN.
-__device__ __forceinline__ float largest(float a, float b, float c) {
-  float d;
-  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
+// What becomes of a row: the rotation of all of Q and K and the cache; a norm for each head, the rotation of a part of it and the
+// cache; the same and an output for K.
+enum Mode { kWrite, kWriteNormed, kRows };
 
 // Blocks go over the tokens and a token's heads, a row of DH elements by DH / 16 threads, each with elements [8t, 8t + 8)
 // of either half: the rotation's partners are in the same thread, all loads and stores of Q are 16 bytes. The next row,
@@ -126,30 +77,44 @@ __device__ __forceinline__ float largest(float a, float b, float c) {
 // are bound by instructions as much as by bytes: with a grid-stride loop over rows, its 64-bit divisions and a division of
 // every element, 8 x 2048 tokens of 48 heads of 128 (370 MB) took 108 us, with a token a block and no row ahead 90, like this 67 (5.5 TB/s).
 constexpr int kWriteThreads = 384;  // of a block, at most
-template <class T, int DH, int BITS>
+template <class T, int DH, int BITS, int MODE>
 __global__ void __launch_bounds__(kWriteThreads, sizeof(T) == 2 ? 2 : 1) kv_write_kernel(const __grid_constant__ WriteParams p) {
   constexpr int LANES = DH / 16;
+  constexpr bool NORMED = MODE != kWrite;
+  __shared__ float weights[NORMED ? 2 : 1][NORMED ? DH : 1];  // of the norms of Q and K
   stream_order();
   const int t = threadIdx.x % LANES, head0 = threadIdx.x / LANES, heads = blockDim.x / LANES;
+  // The thread's groups of 8: partners of a rotation by halves where it turns them, else neighbours.
+  const bool turns = !NORMED || 16 * t < p.rotary;
+  const int at0 = NORMED && (p.neighbours || !turns) ? 16 * t : 8 * t;
+  const int at1 = !NORMED ? at0 + DH / 2 : p.neighbours || !turns ? at0 + 8 : at0 + p.rotary / 2;
+  if constexpr (NORMED) {
+    for (int i = threadIdx.x; i < 2 * DH; i += blockDim.x) {
+      const float* w = i < DH ? p.wq : p.wk;
+      weights[i / DH][i % DH] = w != nullptr ? __ldg(w + i % DH) : 1.f;
+    }
+    __syncthreads();
+  }
   Raw8<T> lo, hi;
   float c[8], s[8];
   int64_t slot = -1, next_slot = -1;
   int pos = 0, next_pos = 0;
   auto place = [&](int64_t token) {
-    next_slot = __ldg(p.slots + token);
+    next_slot = MODE == kRows ? 0 : __ldg(p.slots + token);
     if (p.positions != nullptr) next_pos = __ldg(p.positions + token);
   };
   auto angles = [&] {
     slot = next_slot, pos = next_pos;
-    if (p.positions != nullptr && pos >= 0 && pos < p.rope_len) {
-      load8(p.cos_t + (int64_t)pos * (DH / 2) + 8 * t, c);
-      load8(p.sin_t + (int64_t)pos * (DH / 2) + 8 * t, s);
+    if (p.positions != nullptr && turns && pos >= 0 && pos < p.rope_len) {
+      const int64_t at = (int64_t)pos * (NORMED ? p.rotary / 2 : DH / 2) + 8 * t;
+      load8(p.cos_t + at, c);
+      load8(p.sin_t + at, s);
     }
   };
   auto fetch = [&](int64_t token, int head) {
     if (head < p.n_heads && (head >= p.n_q || p.q_out != nullptr)) {
-      const T* row = static_cast<const T*>(p.x) + token * p.ldx + (int64_t)head * DH + 8 * t;
-      lo.load(row), hi.load(row + DH / 2);
+      const T* row = static_cast<const T*>(p.x) + token * p.ldx + (int64_t)head * DH;
+      lo.load(row + at0), hi.load(row + at1);
     }
   };
   int64_t token = blockIdx.x;
@@ -165,10 +130,32 @@ __global__ void __launch_bounds__(kWriteThreads, sizeof(T) == 2 ? 2 : 1) kv_writ
     const int64_t now = token, to = slot;
     const int row = head;
     const bool is_q = row < p.n_q, is_k = row < p.n_q + p.n_kv, turn = p.positions != nullptr && is_k;
-    const bool placed = to >= 0 && to < p.n_slots, turnable = p.positions == nullptr || (pos >= 0 && pos < p.rope_len);
+    const bool placed = MODE == kRows || (to >= 0 && to < p.n_slots), turnable = p.positions == nullptr || (pos >= 0 && pos < p.rope_len);
     const bool live = placed && row < p.n_heads && (!turn || turnable) && !(is_q && p.q_out == nullptr);
     if (threadIdx.x == 0 && to >= 0 && (!placed || !turnable)) report(p.status, JAB_ERR_INVALID_ARG);
-    if (live && turn) {
+    if constexpr (NORMED) {
+      if (p.eps > 0.f) {
+        const float r = norm_factor<T, LANES>(a, b, p.eps);
+        if (live && is_k) {
+          const float* w = weights[is_q ? 0 : 1];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            a[i] = __fmul_rn(__fmul_rn(a[i], r), w[at0 + i]);
+            b[i] = __fmul_rn(__fmul_rn(b[i], r), w[at1 + i]);
+          }
+          if (!(r == r)) report(p.status, JAB_ERR_NONFINITE);
+        }
+      }
+    }
+    if (NORMED && live && turn && turns && p.neighbours) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float* v = i < 4 ? a + 2 * i : b + 2 * (i - 4);
+        const float x = v[0], y = v[1];
+        v[0] = __fsub_rn(__fmul_rn(x, c[i]), __fmul_rn(y, s[i]));
+        v[1] = __fadd_rn(__fmul_rn(y, c[i]), __fmul_rn(x, s[i]));
+      }
+    } else if (live && turn && turns) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {  // every product and every sum rounded: no contraction, which packed forms were seen to get
         const float x = a[i], y = b[i];
@@ -187,12 +174,14 @@ __global__ void __launch_bounds__(kWriteThreads, sizeof(T) == 2 ? 2 : 1) kv_writ
     if (live) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) big = largest(big, a[i], b[i]);
-      if (is_q) {
-        const int64_t at = (now * p.n_q + row) * DH + 8 * t;
-        T* out = static_cast<T*>(p.q_out) + at;
-        if (in_bounds(at + DH / 2 + 7, p.n_tokens * p.n_q * DH, p.status)) {
-          store(out, a);
-          store(out + DH / 2, b);
+      if (is_q || MODE == kRows) {
+        const int n = is_q ? p.n_q : p.n_kv;
+        const int64_t ld = MODE != kRows ? (int64_t)p.n_q * DH : is_q ? p.ldq : p.ldk;
+        const int64_t at = now * ld + (is_q ? row : row - p.n_q) * DH;
+        T* out = static_cast<T*>(is_q ? p.q_out : p.k_out) + at;
+        if (in_bounds(at + max(at0, at1) + 7, (p.n_tokens - 1) * ld + (int64_t)n * DH, p.status)) {
+          store(out + at0, a);
+          store(out + at1, b);
         }
         // finite, but not in Q's type (or neither): from halfway past the largest fp16 (65504) on
         if (std::is_same<T, half_t>::value && !(big < 65520.f)) report(p.status, JAB_ERR_RANGE);
@@ -200,7 +189,7 @@ __global__ void __launch_bounds__(kWriteThreads, sizeof(T) == 2 ? 2 : 1) kv_writ
     }
 #pragma unroll
     for (int o = LANES / 2; o > 0; o >>= 1) big = largest(big, __shfl_xor_sync(0xffffffffu, big, o), 0.f);
-    if (is_q || !live) continue;
+    if (MODE == kRows || is_q || !live) continue;
     const bool fine = big < INFINITY;
     if (!fine) report(p.status, JAB_ERR_NONFINITE);
     const float scale = fine ? __fdiv_rn(big, (float)((1 << (BITS - 1)) - 1)) : __uint_as_float(0x7fc00000u);
@@ -216,13 +205,14 @@ __global__ void __launch_bounds__(kWriteThreads, sizeof(T) == 2 ? 2 : 1) kv_writ
     const int64_t pg = p.page_shift >= 0 ? to >> p.page_shift : to / p.page;
     const int64_t r = (pg * p.n_kv + h) * p.page + (to - pg * p.page);
     if (!in_bounds(r, p.n_slots * p.n_kv, p.status)) continue;
-    uint8_t* codes = (is_k ? p.k_codes : p.v_codes) + r * (DH * BITS / 8) + t * BITS;
+    uint8_t* codes = (is_k ? p.k_codes : p.v_codes) + r * (DH * BITS / 8);
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
+      uint8_t* to8 = codes + (half ? at1 : at0) * BITS / 8;
       if constexpr (BITS == 8)
-        *reinterpret_cast<uint2*>(codes + half * (DH / 2)) = make_uint2(w[half][0], w[half][1]);
+        *reinterpret_cast<uint2*>(to8) = make_uint2(w[half][0], w[half][1]);
       else
-        *reinterpret_cast<uint32_t*>(codes + half * (DH / 4)) = w[half][0];
+        *reinterpret_cast<uint32_t*>(to8) = w[half][0];
     }
     if (t == 0) (is_k ? p.k_scales : p.v_scales)[r] = scale;
   }
@@ -296,7 +286,7 @@ __global__ void __launch_bounds__(256) kv_read_kernel(const __grid_constant__ Re
   }
 }
 
-template <class T, int DH, int BITS>
+template <class T, int DH, int BITS, int MODE>
 cudaError_t write_as(const WriteParams& p, int sms, cudaStream_t st) {
   // A block has a token's heads, or as many of them as kWriteThreads threads take. With four tokens for every SM and more, a
   // third of the heads where that leaves no thread idle: it loads a token's angles once for its rows in turn (2048 tokens of 48
@@ -305,12 +295,20 @@ cudaError_t write_as(const WriteParams& p, int sms, cudaStream_t st) {
   const int want = p.n_heads * (DH / 16), share = p.n_tokens >= 4 * (int64_t)sms && want % 96 == 0 ? want / 3 : want;
   const int threads = (std::min(share, kWriteThreads) + 31) / 32 * 32;
   const int64_t blocks = std::min<int64_t>(p.n_tokens, (int64_t)sms * std::min(32, std::max(1, PER_SM / threads)));
-  return launch_after(kv_write_kernel<T, DH, BITS>, (unsigned)blocks, threads, 0, st, p);
+  return launch_after(kv_write_kernel<T, DH, BITS, MODE>, (unsigned)blocks, threads, 0, st, p);
 }
-template <class T>
+template <class T, int MODE>
 cudaError_t write_type(const WriteParams& p, int dh, int bits, int sms, cudaStream_t st) {
-  if (dh == 128) return bits == 8 ? write_as<T, 128, 8>(p, sms, st) : write_as<T, 128, 4>(p, sms, st);
-  return bits == 8 ? write_as<T, 64, 8>(p, sms, st) : write_as<T, 64, 4>(p, sms, st);
+  if constexpr (MODE != kRows) {
+    if (bits == 4) return dh == 128 ? write_as<T, 128, 4, MODE>(p, sms, st) : write_as<T, 64, 4, MODE>(p, sms, st);
+  }
+  return dh == 128 ? write_as<T, 128, 8, MODE>(p, sms, st) : write_as<T, 64, 8, MODE>(p, sms, st);
+}
+template <int MODE>
+cudaError_t write_mode(const WriteParams& p, jab_dtype type, int dh, int bits, int sms, cudaStream_t st) {
+  return type == JAB_FP16 ? write_type<half_t, MODE>(p, dh, bits, sms, st)
+         : type == JAB_BF16 ? write_type<bf16_t, MODE>(p, dh, bits, sms, st)
+                            : write_type<float, MODE>(p, dh, bits, sms, st);
 }
 
 template <class T, int DH, int BITS>
@@ -325,6 +323,18 @@ template <class T>
 cudaError_t read_type(const ReadParams& p, int dh, int bits, int sms, cudaStream_t st) {
   if (dh == 128) return bits == 8 ? read_as<T, 128, 8>(p, sms, st) : read_as<T, 128, 4>(p, sms, st);
   return bits == 8 ? read_as<T, 64, 8>(p, sms, st) : read_as<T, 64, 4>(p, sms, st);
+}
+
+void set_how(WriteParams& p, const jab_norm_rope& how) {
+  p.eps = how.norm ? how.eps : 0.f;
+  p.wq = how.q_weight_dev;
+  p.wk = how.k_weight_dev;
+  p.positions = how.positions_dev;
+  p.cos_t = how.cos_dev;
+  p.sin_t = how.sin_dev;
+  p.rope_len = how.rope_len;
+  p.rotary = how.positions_dev != nullptr ? how.rotary_dim : 0;
+  p.neighbours = how.interleaved != 0;
 }
 
 }  // namespace
@@ -347,14 +357,31 @@ cudaError_t launch_kv_write(const KvWriteArgs& a, int sms, cudaStream_t st) {
   p.sin_t = a.sin_t;
   p.rope_len = a.rope_len;
   p.q_out = a.q_out;
+  if (a.how != nullptr) set_how(p, *a.how);
   p.k_codes = static_cast<uint8_t*>(c.k_codes);
   p.v_codes = static_cast<uint8_t*>(c.v_codes);
   p.k_scales = c.k_scales;
   p.v_scales = c.v_scales;
   p.status = a.status;
-  if (a.type == JAB_FP16) return write_type<half_t>(p, c.head_dim, c.bits, sms, st);
-  if (a.type == JAB_BF16) return write_type<bf16_t>(p, c.head_dim, c.bits, sms, st);
-  return write_type<float>(p, c.head_dim, c.bits, sms, st);
+  return a.how != nullptr ? write_mode<kWriteNormed>(p, a.type, c.head_dim, c.bits, sms, st)
+                          : write_mode<kWrite>(p, a.type, c.head_dim, c.bits, sms, st);
+}
+
+cudaError_t launch_norm_rope(const NormRopeArgs& a, int sms, cudaStream_t st) {
+  WriteParams p{};
+  p.x = a.x;
+  p.ldx = a.ldx;
+  p.n_q = a.n_q;
+  p.n_kv = a.n_k;
+  p.n_heads = p.n_q + p.n_kv;
+  p.n_tokens = a.n_tokens;
+  p.q_out = a.q;
+  p.k_out = a.k;
+  p.ldq = a.ldq;
+  p.ldk = a.ldk;
+  p.status = a.status;
+  set_how(p, a.how);
+  return write_mode<kRows>(p, a.type, a.head_dim, 8, sms, st);
 }
 
 cudaError_t launch_kv_read(const KvReadArgs& a, int sms, cudaStream_t st) {

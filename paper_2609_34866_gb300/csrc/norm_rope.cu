@@ -1,0 +1,260 @@
+// The gradient of the norm and rotation of the heads of Q and K (the forward is a mode of kv_cache.cu's writing kernel), and rotation
+// tables for stretched contexts.
+//
+//   y = R n, n = (x r) w, r = (mean x^2 + eps)^(-1/2):   g = R^T dy, u = g w,
+//   dx = r (u - x r mean(u x r)),  dw = sum over tokens and heads of g x r
+#include <math.h>
+
+#include <algorithm>
+
+#include "common.cuh"
+#include "rows.cuh"
+#include "serve.h"
+
+namespace jab {
+namespace {
+
+struct BackParams {
+  const void *x, *dq, *dk;
+  int64_t ldx, lddq, lddk, lddx, n_tokens;
+  void* dx;
+  int n_q, n_k;
+  const int32_t* positions;
+  const float *cos_t, *sin_t, *wq, *wk;
+  int rope_len, rotary;
+  bool neighbours;
+  float eps;    // 0: no norm
+  float* part;  // [blocks, 2, DH] of the weights' gradients, or null
+  int* status;
+};
+
+constexpr int kBackThreads = 256;
+constexpr int kMostParts = 608;  // blocks along the tokens times blocks along the heads, where the heads allow it
+
+// A thread stays with one head's two groups of 8 (as in the writing kernel) and goes over the tokens, so that its share of the
+// weights' gradient is 16 registers. The next token's rows are under way while one is worked on.
+template <class T, int DH>
+__global__ void __launch_bounds__(kBackThreads, 2) norm_rope_back_kernel(const __grid_constant__ BackParams p) {
+  constexpr int LANES = DH / 16, HEADS = kBackThreads / LANES;
+  __shared__ float sums[HEADS][DH];
+  stream_order();
+  const int t = threadIdx.x % LANES, slot = threadIdx.x / LANES, head = blockIdx.y * HEADS + slot;
+  const bool exists = head < p.n_q + p.n_k, is_q = head < p.n_q;
+  const bool turns = p.positions != nullptr && 16 * t < p.rotary, pairs = p.neighbours || 16 * t >= p.rotary;
+  const int at0 = pairs ? 16 * t : 8 * t, at1 = pairs ? at0 + 8 : at0 + p.rotary / 2;
+  float w[16], dw[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const float* from = is_q ? p.wq : p.wk;
+    w[i] = from != nullptr && exists ? __ldg(from + (i < 8 ? at0 + i : at1 + i - 8)) : 1.f;
+    dw[i] = 0.f;
+  }
+  const T* x = static_cast<const T*>(p.x) + (int64_t)head * DH;
+  const T* dy = is_q ? static_cast<const T*>(p.dq) + (int64_t)head * DH : static_cast<const T*>(p.dk) + (int64_t)(head - p.n_q) * DH;
+  const int64_t lddy = is_q ? p.lddq : p.lddk;
+  Raw8<T> x0 = {}, x1 = {}, g0 = {}, g1 = {};
+  int next = 0;
+  auto fetch = [&](int64_t token) {
+    if (token >= p.n_tokens) return;
+    if (p.positions != nullptr) next = __ldg(p.positions + token);
+    if (!exists) return;
+    x0.load(x + token * p.ldx + at0), x1.load(x + token * p.ldx + at1);
+    g0.load(dy + token * lddy + at0), g1.load(dy + token * lddy + at1);
+  };
+  fetch(blockIdx.x);
+  for (int64_t token = blockIdx.x; token < p.n_tokens; token += gridDim.x) {
+    float a[8], b[8], g[8], h[8];
+    x0.numbers(a), x1.numbers(b), g0.numbers(g), g1.numbers(h);
+    const int pos = next;
+    const bool fine = p.positions == nullptr || (pos >= 0 && pos < p.rope_len);
+    if (threadIdx.x == 0 && !fine) report(p.status, JAB_ERR_INVALID_ARG);
+    float c[8], s[8];
+    if (turns && fine) {
+      load8(p.cos_t + (int64_t)pos * (p.rotary / 2) + 8 * t, c);
+      load8(p.sin_t + (int64_t)pos * (p.rotary / 2) + 8 * t, s);
+    }
+    fetch(token + gridDim.x);
+    if (turns && fine) {
+      auto back = [](float& y, float& z, float cs, float sn) {
+        const float da = y * cs + z * sn, db = z * cs - y * sn;
+        y = da, z = db;
+      };
+      if (p.neighbours) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) back(g[2 * i], g[2 * i + 1], c[i], s[i]), back(h[2 * i], h[2 * i + 1], c[4 + i], s[4 + i]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) back(g[i], h[i], c[i], s[i]);
+      }
+    }
+    if (p.eps > 0.f) {
+      const float r = norm_factor<T, LANES>(a, b, p.eps);
+      float dot = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        a[i] *= r, b[i] *= r;
+        if (fine) dw[i] += g[i] * a[i], dw[8 + i] += h[i] * b[i];
+        g[i] *= w[i], h[i] *= w[8 + i];
+        dot += g[i] * a[i] + h[i] * b[i];
+      }
+#pragma unroll
+      for (int o = LANES / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+      dot *= 1.f / DH;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        g[i] = r * (g[i] - a[i] * dot);
+        h[i] = r * (h[i] - b[i] * dot);
+      }
+      if (exists && !(r == r)) report(p.status, JAB_ERR_NONFINITE);
+    }
+    if (exists && fine) {
+      const int64_t at = token * p.lddx + (int64_t)head * DH;
+      if (in_bounds(at + max(at0, at1) + 7, (p.n_tokens - 1) * p.lddx + (int64_t)(p.n_q + p.n_k) * DH, p.status)) {
+        store(static_cast<T*>(p.dx) + at + at0, g);
+        store(static_cast<T*>(p.dx) + at + at1, h);
+      }
+    }
+  }
+  if (p.part == nullptr) return;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) sums[slot][at0 + i] = exists ? dw[i] : 0.f, sums[slot][at1 + i] = exists ? dw[8 + i] : 0.f;
+  __syncthreads();
+  if (threadIdx.x < 2 * DH) {
+    const int d = threadIdx.x % DH, first = blockIdx.y * HEADS;
+    const int q_end = min(max(p.n_q - first, 0), HEADS);
+    const int h0 = threadIdx.x < DH ? 0 : q_end, h1 = threadIdx.x < DH ? q_end : HEADS;
+    float v = 0.f;
+    for (int i = h0; i < h1; ++i) v += sums[i][d];
+    p.part[((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 2 * DH + threadIdx.x] = v;
+  }
+}
+
+// The blocks' sums, in their order: 32 columns a block, eight runs of blocks each, added up as pairs.
+__global__ void __launch_bounds__(256) weight_sum_kernel(const float* part, int n, int dh, float* dwq, float* dwk) {
+  __shared__ float hi_s[8][32], lo_s[8][32];
+  stream_order();
+  const int lane = threadIdx.x & 31, run = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
+  float hi = 0.f, lo = 0.f;
+#pragma unroll 8
+  for (int i = run; i < n; i += 8) pair_add(hi, lo, part[(int64_t)i * 2 * dh + col], 0.f);
+  hi_s[run][lane] = hi, lo_s[run][lane] = lo;
+  __syncthreads();
+  if (run != 0) return;
+  for (int i = 1; i < 8; ++i) pair_add(hi, lo, hi_s[i][lane], lo_s[i][lane]);
+  float* out = col < dh ? dwq : dwk;
+  if (out != nullptr) out[col < dh ? col : col - dh] = fabsf(hi) < INFINITY ? hi + lo : hi;
+}
+
+// ------------------------------------------------------------------ tables
+struct TableParams {
+  double freq_pi[64];  // angle of a step over pi
+  double by;
+  float *cos_t, *sin_t;
+  int length, half;
+};
+
+// Angles are position x frequency in 64 bits, reduced by the pi forms without a long division; the rounding of the product
+// (2^-53 of up to 2^31 turns) is 2^-22 of a turn at the very worst and 2^-36 at 2^17 positions. A thread takes sixteen positions of its
+// pair and rotates from the first, as an fp64 sincos costs some sixty instructions at two a clock and SM.
+constexpr int kRun = 16;
+__global__ void __launch_bounds__(64) rope_table_kernel(const __grid_constant__ TableParams p) {
+  stream_order();
+  const int j = threadIdx.x;
+  if (j >= p.half) return;
+  const double f = p.freq_pi[j];
+  const int t0 = blockIdx.x * kRun, n = min(kRun, p.length - t0);
+  double sn, cs, sd, cd;
+  sincospi((double)t0 * f, &sn, &cs);
+  sincospi(f, &sd, &cd);
+  int64_t i = (int64_t)t0 * p.half + j;
+  for (int k = 0; k < n; ++k, i += p.half) {
+    p.cos_t[i] = (float)(cs * p.by);
+    p.sin_t[i] = (float)(sn * p.by);
+    const double c2 = cs * cd - sn * sd;
+    sn = sn * cd + cs * sd;
+    cs = c2;
+  }
+}
+
+template <class T, int DH>
+cudaError_t back_as(const BackParams& p, float* dwq, float* dwk, cudaStream_t st) {
+  constexpr int HEADS = kBackThreads / (DH / 16);
+  const int gy = (p.n_q + p.n_k + HEADS - 1) / HEADS;
+  const int gx = p.n_tokens > 0 ? (int)std::min<int64_t>(p.n_tokens, std::max(1, kMostParts / gy)) : 0;
+  if (gx > 0) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = dim3(gx, gy);
+    cfg.blockDim = dim3(kBackThreads);
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, norm_rope_back_kernel<T, DH>, p);
+    if (e != cudaSuccess) {
+      cudaGetLastError();
+      return e;
+    }
+  }
+  if (p.part == nullptr) return cudaSuccess;
+  return launch_after(weight_sum_kernel, 2 * DH / 32, 256, 0, st, (const float*)p.part, gx * gy, DH, dwq, dwk);
+}
+template <class T>
+cudaError_t back_type(const BackParams& p, int dh, float* dwq, float* dwk, cudaStream_t st) {
+  return dh == 128 ? back_as<T, 128>(p, dwq, dwk, st) : back_as<T, 64>(p, dwq, dwk, st);
+}
+
+bool wants_weights(const NormRopeBackArgs& a) { return a.dwq != nullptr || a.dwk != nullptr; }
+
+}  // namespace
+
+size_t norm_rope_scratch(int n_heads, int dh) {
+  const int per = kBackThreads / (dh / 16);
+  return (size_t)std::max(kMostParts, (n_heads + per - 1) / per) * 2 * dh * sizeof(float);
+}
+
+int norm_rope_back_kernels(const NormRopeBackArgs& a) { return (a.n_tokens > 0 ? 1 : 0) + (wants_weights(a) ? 1 : 0); }
+
+cudaError_t launch_norm_rope_back(const NormRopeBackArgs& a, int, cudaStream_t st) {
+  BackParams p{};
+  p.x = a.x, p.dq = a.dq, p.dk = a.dk;
+  p.ldx = a.ldx, p.lddq = a.lddq, p.lddk = a.lddk, p.lddx = a.lddx;
+  p.n_tokens = a.n_tokens;
+  p.dx = a.dx;
+  p.n_q = a.n_q, p.n_k = a.n_k;
+  p.positions = a.how.positions_dev;
+  p.cos_t = a.how.cos_dev, p.sin_t = a.how.sin_dev;
+  p.wq = a.how.q_weight_dev, p.wk = a.how.k_weight_dev;
+  p.rope_len = a.how.rope_len;
+  p.rotary = a.how.positions_dev != nullptr ? a.how.rotary_dim : 0;
+  p.neighbours = a.how.interleaved != 0;
+  p.eps = a.how.norm ? a.how.eps : 0.f;
+  p.part = wants_weights(a) ? static_cast<float*>(a.ws) : nullptr;
+  p.status = a.status;
+  return a.type == JAB_FP16   ? back_type<half_t>(p, a.head_dim, a.dwq, a.dwk, st)
+         : a.type == JAB_BF16 ? back_type<bf16_t>(p, a.head_dim, a.dwq, a.dwk, st)
+                              : back_type<float>(p, a.head_dim, a.dwq, a.dwk, st);
+}
+
+cudaError_t launch_rope_table(const RopeTableArgs& a, cudaStream_t st) {
+  TableParams p{};
+  p.cos_t = a.cos_t, p.sin_t = a.sin_t;
+  p.length = a.length;
+  p.half = a.rotary / 2;
+  p.by = a.scaling.attention;
+  const double pi = 3.14159265358979323846;
+  for (int j = 0; j < p.half; ++j) {
+    double f = pow((double)a.theta, -2.0 * j / a.rotary);
+    if (a.scaling.kind == JAB_ROPE_LINEAR) f /= a.scaling.factor;
+    if (a.scaling.kind == JAB_ROPE_BY_PARTS) {
+      const double turns = a.scaling.original_length * f / (2 * pi);
+      const double g = std::min(1.0, std::max(0.0, (turns - a.scaling.low_turns) / ((double)a.scaling.high_turns - a.scaling.low_turns)));
+      f = g * f + (1 - g) * f / a.scaling.factor;
+    }
+    p.freq_pi[j] = f / pi;
+  }
+  return launch_after(rope_table_kernel, (unsigned)((a.length + kRun - 1) / kRun), 64, 0, st, p);
+}
+
+}  // namespace jab
