@@ -23,45 +23,64 @@ struct QuantParams {
   float* scales;
   int64_t row_pitch, block_pitch;
   int* status;
+  // fp8_rows_kernel
+  int rows;          // of a block of threads at a time
+  FastDiv by_blocks;
 };
 
-// A half warp has a row's block, a lane 8 elements of it; four blocks of a half warp are under way together.
+// Scale of the 128 elements of which the lanes of a half warp have eight each.
+template <class T>
+__device__ __forceinline__ float half_warp_scale(const Raw8<T>& raw, const float (&v)[8]) {
+  if constexpr (sizeof(T) == 2) {  // (magnitudes of 16-bit numbers are in the order of their bits)
+    uint32_t top = max_abs_f16x2(max_abs_f16x2(max_abs_f16x2(max_abs_f16x2(0u, raw.w[0].x), raw.w[0].y), raw.w[0].z), raw.w[0].w);
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, o));
+    top = max(top & 0xffffu, top >> 16);
+    constexpr bool HALF = std::is_same<T, half_t>::value;
+    return fp8_scale(HALF ? __half2float(__ushort_as_half((unsigned short)top)) : __uint_as_float(top << 16));
+  } else {
+    float big = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; j += 2) big = largest(big, v[j], v[j + 1]);
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) big = largest(big, __shfl_xor_sync(0xffffffffu, big, o), 0.f);
+    return fp8_scale(big);
+  }
+}
+
+// A half warp has a row's block, a lane 8 elements of it; several blocks of a half warp are under way together. A block of threads
+// goes over some rows at a time, so that the place of a unit takes one small division (a 64-bit one each: 8192 x 4096 in 32 us).
 template <class T>
 __global__ void __launch_bounds__(256) fp8_rows_kernel(const __grid_constant__ QuantParams p) {
   constexpr int AHEAD = sizeof(T) == 2 ? 4 : 2;
   stream_order();
-  const int lane = threadIdx.x & 15;
-  const int64_t units = p.M * p.blocks, step = (int64_t)gridDim.x * 16;
-  for (int64_t u0 = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); u0 - (threadIdx.x >> 4) < units; u0 += step * AHEAD) {
-    Raw8<T> raw[AHEAD];
-    int64_t m[AHEAD];
-    int kb[AHEAD];
-    bool live[AHEAD];
+  const int lane = threadIdx.x & 15, group = threadIdx.x >> 4;
+  for (int64_t m0 = (int64_t)blockIdx.x * p.rows; m0 < p.M; m0 += (int64_t)gridDim.x * p.rows) {
+    const int units = (int)min((int64_t)p.rows, p.M - m0) * p.blocks;
+    for (int u0 = 0; u0 < units; u0 += 16 * AHEAD) {  // (whole warps go round together)
+      Raw8<T> raw[AHEAD];
+      int m[AHEAD], kb[AHEAD];
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) {
-      const int64_t u = u0 + i * step;
-      m[i] = u / p.blocks, kb[i] = (int)(u - m[i] * p.blocks);
-      live[i] = u < units && kb[i] * 128 + lane * 8 < p.K;
-      raw[i] = {};
-      if (live[i]) raw[i].load(static_cast<const T*>(p.x) + m[i] * p.ldx + kb[i] * 128 + lane * 8);
-    }
-#pragma unroll
-    for (int i = 0; i < AHEAD; ++i) {
-      float v[8];
-      raw[i].numbers(v);
-      float big = 0.f;
-#pragma unroll
-      for (int j = 0; j < 8; j += 2) big = largest(big, v[j], v[j + 1]);
-#pragma unroll
-      for (int o = 8; o > 0; o >>= 1) big = largest(big, __shfl_xor_sync(0xffffffffu, big, o), 0.f);
-      const float s = fp8_scale(big);
-      if (u0 + i * step >= units) continue;
-      if (lane == 0) {
-        p.scales[m[i] * p.row_pitch + kb[i] * p.block_pitch] = s;
-        if (!(s >= 0.f)) report(p.status, JAB_ERR_NONFINITE);
+      for (int i = 0; i < AHEAD; ++i) {
+        const int u = u0 + i * 16 + group;
+        p.by_blocks.divmod(u, m[i], kb[i]);
+        raw[i] = {};
+        if (u < units && kb[i] * 128 + lane * 8 < p.K) raw[i].load(static_cast<const T*>(p.x) + (m0 + m[i]) * p.ldx + kb[i] * 128 + lane * 8);
       }
-      const int64_t at = m[i] * p.K + kb[i] * 128 + lane * 8;
-      if (live[i] && in_bounds(at + 7, p.M * p.K, p.status)) *reinterpret_cast<uint2*>(p.codes + at) = fp8_codes(v, s);
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        float v[8];
+        raw[i].numbers(v);
+        const float s = half_warp_scale<T>(raw[i], v);
+        if (u0 + i * 16 + group >= units) continue;
+        if (lane == 0) {
+          p.scales[(m0 + m[i]) * p.row_pitch + kb[i] * p.block_pitch] = s;
+          if (!(s >= 0.f)) report(p.status, JAB_ERR_NONFINITE);
+        }
+        const int k = kb[i] * 128 + lane * 8;
+        const int64_t at = (m0 + m[i]) * p.K + k;
+        if (k < p.K && in_bounds(at + 7, p.M * p.K, p.status)) *reinterpret_cast<uint2*>(p.codes + at) = fp8_codes(v, s);
+      }
     }
   }
 }
@@ -111,10 +130,13 @@ __global__ void __launch_bounds__(256) fp8_blocks_kernel(const __grid_constant__
 }
 
 template <class T>
-cudaError_t quantize_as(const QuantParams& p, int block_rows, int sms, cudaStream_t st) {
+cudaError_t quantize_as(QuantParams p, int block_rows, int sms, cudaStream_t st) {
   if (block_rows == 1) {
+    // units of four half warps' turns where that leaves all SMs two blocks, else of one
     const int64_t units = p.M * p.blocks;
-    return launch_after(fp8_rows_kernel<T>, (unsigned)std::min<int64_t>((units + 15) / 16, (int64_t)sms * 8), 256, 0, st, p);
+    p.rows = std::max(1, (units >= (int64_t)sms * 128 ? 64 : 16) / p.blocks);
+    p.by_blocks = FastDiv(p.blocks);
+    return launch_after(fp8_rows_kernel<T>, (unsigned)std::min<int64_t>((p.M + p.rows - 1) / p.rows, (int64_t)sms * 8), 256, 0, st, p);
   }
   const int64_t blocks = (p.M + 127) / 128 * p.blocks;
   return launch_after(fp8_blocks_kernel<T>, (unsigned)blocks, 256, 0, st, p);

@@ -135,7 +135,7 @@ __global__ void __launch_bounds__(kWriteThreads, sizeof(T) == 2 ? 2 : 1) kv_writ
     if (threadIdx.x == 0 && to >= 0 && (!placed || !turnable)) report(p.status, JAB_ERR_INVALID_ARG);
     if constexpr (NORMED) {
       if (p.eps > 0.f) {
-        const float r = norm_factor<T, LANES>(a, b, p.eps);
+        const float r = norm_factor<LANES>(a, b, p.eps);
         if (live && is_k) {
           const float* w = weights[is_q ? 0 : 1];
 #pragma unroll

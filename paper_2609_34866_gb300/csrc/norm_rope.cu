@@ -88,7 +88,7 @@ __global__ void __launch_bounds__(kBackThreads, 2) norm_rope_back_kernel(const _
       }
     }
     if (p.eps > 0.f) {
-      const float r = norm_factor<T, LANES>(a, b, p.eps);
+      const float r = norm_factor<LANES>(a, b, p.eps);
       float dot = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {

@@ -66,22 +66,31 @@ __device__ __forceinline__ float largest(float a, float b, float c) {
   return d;
 }
 
-// 1 / sqrt(mean x^2 + eps) of a row of 16 LANES elements, of which the lanes of a group have a[8], b[8] each: the sum as a pair
-// (2^-46 of it is lost), the root's reciprocal corrected by its remainder, so that the result is the nearest fp32 but for one in
-// 2^16 or fewer: the codes of what it multiplies are the same from any implementation that rounds it right. NaN where the
-// sum leaves fp32. Called by whole warps.
-template <class T, int LANES>
+// 1 / sqrt(mean x^2 + eps) of a row of 16 LANES elements, of which the lanes of a group have a[8], b[8] each, so near that it is the
+// nearest fp32 but for one in 2^16 or fewer: the codes of what it multiplies are then the same from any implementation that
+// rounds it right. A thread's squares are added to a power of two of 16 times their largest and more: the sum s = fl(h + x^2) is
+// within a factor of two of h, so that h - s is exact and what s lost, x^2 + (h - s), is one fused operation; the losses
+// add up beside it (about 2^-38 of the sum is lost; adding pairs takes twice the operations). NaN where 32 times a square leaves fp32.
+// Called by whole warps.
+template <int LANES>
 __device__ __forceinline__ float norm_factor(const float (&a)[8], const float (&b)[8], float eps) {
-  float hi = 0.f, lo = 0.f;
+  float big = 0.f;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const float x = i < 8 ? a[i & 7] : b[i & 7], q = __fmul_rn(x, x);
-    pair_add(hi, lo, q, sizeof(T) == 4 ? __fmaf_rn(x, x, -q) : 0.f);  // (squares of 16-bit numbers are exact)
+  for (int i = 0; i < 8; ++i) big = largest(big, a[i], b[i]);
+  const float base = __uint_as_float(__float_as_uint(32.f * big * big) & 0x7f800000u);
+  float2 h = make_float2(base, base), l = make_float2(0.f, 0.f);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float2 x = make_float2(a[i], b[i]), s = tc::fma2(x, x, h);
+    l = tc::add2(l, tc::fma2(x, x, tc::sub2(h, s)));
+    h = s;
   }
+  float hi = h.x - base, lo = l.x;
+  pair_add(hi, lo, h.y - base, l.y);
 #pragma unroll
   for (int o = LANES / 2; o > 0; o >>= 1) {
-    const float h = __shfl_xor_sync(0xffffffffu, hi, o), l = __shfl_xor_sync(0xffffffffu, lo, o);
-    pair_add(hi, lo, h, l);
+    const float u = __shfl_xor_sync(0xffffffffu, hi, o), v = __shfl_xor_sync(0xffffffffu, lo, o);
+    pair_add(hi, lo, u, v);
   }
   constexpr float kMean = 1.f / (16 * LANES);
   float m, e;
