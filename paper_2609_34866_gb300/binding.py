@@ -446,7 +446,10 @@ def _rows(t: torch.Tensor, width: int, name: str, rows: Optional[int] = None):
     may have any stride, the others are flattened."""
     if not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor")
-    shape, strides, have = t.shape, t.stride(), 1
+    shape = t.shape
+    if len(shape) == 2 and shape[1] == width and (rows is None or shape[0] == rows) and t.is_contiguous():
+        return t.data_ptr(), width  # (the usual case, without the walk over the dimensions)
+    strides, have = t.stride(), 1
     for d in range(len(shape) - 1, 0, -1):
         if shape[d] != 1 and strides[d] != have:
             have = -1
@@ -462,6 +465,8 @@ def _rows(t: torch.Tensor, width: int, name: str, rows: Optional[int] = None):
 def _shaped(t: torch.Tensor, shape, dtype, name: str) -> int:
     if t.shape != shape:
         raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    if t.dtype is dtype and t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
     return _ptr(t, dtype, name)
 
 
@@ -650,21 +655,25 @@ def jab_rope_table_scaled(cos, sin, theta: float, kind: str = "plain", factor: f
 
 
 def _norm_rope(n: int, dh: int, positions, rope, interleaved, norm_eps, q_weight, k_weight) -> _NormRope:
-    how = _NormRope()
+    qw = kw = pos = cos = sin = None
+    length = half = 0
     if norm_eps is not None:
-        how.norm, how.eps = 1, float(norm_eps)
-        how.q_weight, how.k_weight = (None if w is None else _shaped(w, (dh,), torch.float32, name)
-                                      for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")))
+        shape = (dh,)
+        if q_weight is not None:
+            qw = _shaped(q_weight, shape, torch.float32, "q_weight")
+        if k_weight is not None:
+            kw = _shaped(k_weight, shape, torch.float32, "k_weight")
     elif q_weight is not None or k_weight is not None:
         raise ValueError("weights of a norm need norm_eps")
     if rope is not None:
         if positions is None:
             raise ValueError("rope needs positions")
-        length, half = rope[0].shape
-        how.cos, how.sin = (_shaped(t, (length, half), torch.float32, "rope") for t in rope)
-        how.positions = _shaped(positions, (n,), torch.int32, "positions")
-        how.rope_len, how.rotary_dim, how.interleaved = length, 2 * half, int(bool(interleaved))
-    return how
+        cos_t, sin_t = rope
+        shape = cos_t.shape
+        length, half = shape
+        cos, sin = _shaped(cos_t, shape, torch.float32, "rope"), _shaped(sin_t, shape, torch.float32, "rope")
+        pos = _shaped(positions, (n,), torch.int32, "positions")
+    return _NormRope(norm_eps is not None, norm_eps or 0.0, qw, kw, pos, cos, sin, length, 2 * half, bool(interleaved))
 
 
 def jab_kv_write_norm_rope(cache: KvCache, qkv, n_q_heads: int, slots, q_out=None, positions=None, rope=None,

@@ -28,58 +28,71 @@ struct QuantParams {
   FastDiv by_blocks;
 };
 
-// Scale of the 128 elements of which the lanes of a half warp have eight each.
-template <class T>
-__device__ __forceinline__ float half_warp_scale(const Raw8<T>& raw, const float (&v)[8]) {
+// Largest magnitude of what the thread's groups of eight hold; an infinity or a NaN counts as itself.
+template <class T, int N>
+__device__ __forceinline__ float largest_of(const Raw8<T> (&raw)[N]) {
   if constexpr (sizeof(T) == 2) {  // (magnitudes of 16-bit numbers are in the order of their bits)
-    uint32_t top = max_abs_f16x2(max_abs_f16x2(max_abs_f16x2(max_abs_f16x2(0u, raw.w[0].x), raw.w[0].y), raw.w[0].z), raw.w[0].w);
+    uint32_t top = 0;
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1) top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, o));
+    for (int i = 0; i < N; ++i)
+      top = max_abs_f16x2(max_abs_f16x2(max_abs_f16x2(max_abs_f16x2(top, raw[i].w[0].x), raw[i].w[0].y), raw[i].w[0].z), raw[i].w[0].w);
     top = max(top & 0xffffu, top >> 16);
-    constexpr bool HALF = std::is_same<T, half_t>::value;
-    return fp8_scale(HALF ? __half2float(__ushort_as_half((unsigned short)top)) : __uint_as_float(top << 16));
+    return std::is_same<T, half_t>::value ? __half2float(__ushort_as_half((unsigned short)top)) : __uint_as_float(top << 16);
   } else {
     float big = 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; j += 2) big = largest(big, v[j], v[j + 1]);
+    for (int i = 0; i < N; ++i) {
+      float v[8];
+      raw[i].numbers(v);
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1) big = largest(big, __shfl_xor_sync(0xffffffffu, big, o), 0.f);
-    return fp8_scale(big);
+      for (int j = 0; j < 8; j += 2) big = largest(big, v[j], v[j + 1]);
+    }
+    return big;
   }
 }
 
-// A half warp has a row's block, a lane 8 elements of it; several blocks of a half warp are under way together. A block of threads
-// goes over some rows at a time, so that the place of a unit takes one small division (a 64-bit one each: 8192 x 4096 in 32 us).
+// Eight lanes have a row's block, a lane 16 elements of it (with eight a lane the places, the scale and its reciprocal take
+// two thirds of the instructions: 8192 x 4096 of bf16 in 29 us); several blocks of theirs are under way together. A block of threads
+// goes over some rows at a time, so that the place of a unit takes one small division.
 template <class T>
 __global__ void __launch_bounds__(256) fp8_rows_kernel(const __grid_constant__ QuantParams p) {
-  constexpr int AHEAD = sizeof(T) == 2 ? 4 : 2;
+  constexpr int AHEAD = sizeof(T) == 2 ? 2 : 1, UNITS = 32;
   stream_order();
-  const int lane = threadIdx.x & 15, group = threadIdx.x >> 4;
+  const int lane = threadIdx.x & 7, group = threadIdx.x >> 3;
   for (int64_t m0 = (int64_t)blockIdx.x * p.rows; m0 < p.M; m0 += (int64_t)gridDim.x * p.rows) {
     const int units = (int)min((int64_t)p.rows, p.M - m0) * p.blocks;
-    for (int u0 = 0; u0 < units; u0 += 16 * AHEAD) {  // (whole warps go round together)
-      Raw8<T> raw[AHEAD];
+    for (int u0 = 0; u0 < units; u0 += UNITS * AHEAD) {  // (whole warps go round together)
+      Raw8<T> raw[AHEAD][2];
       int m[AHEAD], kb[AHEAD];
 #pragma unroll
       for (int i = 0; i < AHEAD; ++i) {
-        const int u = u0 + i * 16 + group;
+        const int u = u0 + i * UNITS + group;
         p.by_blocks.divmod(u, m[i], kb[i]);
-        raw[i] = {};
-        if (u < units && kb[i] * 128 + lane * 8 < p.K) raw[i].load(static_cast<const T*>(p.x) + (m0 + m[i]) * p.ldx + kb[i] * 128 + lane * 8);
+        raw[i][0] = raw[i][1] = {};
+        const int k = kb[i] * 128 + lane * 16;
+        if (u < units && k < p.K) {
+          const T* x = static_cast<const T*>(p.x) + (m0 + m[i]) * p.ldx + k;
+          raw[i][0].load(x), raw[i][1].load(x + 8);
+        }
       }
 #pragma unroll
       for (int i = 0; i < AHEAD; ++i) {
-        float v[8];
-        raw[i].numbers(v);
-        const float s = half_warp_scale<T>(raw[i], v);
-        if (u0 + i * 16 + group >= units) continue;
+        float big = largest_of(raw[i]);
+#pragma unroll
+        for (int o = 4; o > 0; o >>= 1) big = largest(big, __shfl_xor_sync(0xffffffffu, big, o), 0.f);
+        const float s = fp8_scale(big);
+        if (u0 + i * UNITS + group >= units) continue;
         if (lane == 0) {
           p.scales[(m0 + m[i]) * p.row_pitch + kb[i] * p.block_pitch] = s;
           if (!(s >= 0.f)) report(p.status, JAB_ERR_NONFINITE);
         }
-        const int k = kb[i] * 128 + lane * 8;
+        const int k = kb[i] * 128 + lane * 16;
         const int64_t at = (m0 + m[i]) * p.K + k;
-        if (k < p.K && in_bounds(at + 7, p.M * p.K, p.status)) *reinterpret_cast<uint2*>(p.codes + at) = fp8_codes(v, s);
+        if (k >= p.K || !in_bounds(at + 15, p.M * p.K, p.status)) continue;
+        float v[8], w[8];
+        raw[i][0].numbers(v), raw[i][1].numbers(w);
+        const uint2 c = fp8_codes(v, s), d = fp8_codes(w, s);
+        *reinterpret_cast<uint4*>(p.codes + at) = make_uint4(c.x, c.y, d.x, d.y);
       }
     }
   }
@@ -100,14 +113,7 @@ __global__ void __launch_bounds__(256) fp8_blocks_kernel(const __grid_constant__
     raw[i] = {};
     if (m < p.M && k < p.K) raw[i].load(static_cast<const T*>(p.x) + m * p.ldx + k);
   }
-  float big = 0.f;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    float v[8];
-    raw[i].numbers(v);
-#pragma unroll
-    for (int j = 0; j < 8; j += 2) big = largest(big, v[j], v[j + 1]);
-  }
+  float big = largest_of(raw);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) big = largest(big, __shfl_xor_sync(0xffffffffu, big, o), 0.f);
   if ((threadIdx.x & 31) == 0) top[threadIdx.x >> 5] = big;
@@ -132,9 +138,9 @@ __global__ void __launch_bounds__(256) fp8_blocks_kernel(const __grid_constant__
 template <class T>
 cudaError_t quantize_as(QuantParams p, int block_rows, int sms, cudaStream_t st) {
   if (block_rows == 1) {
-    // units of four half warps' turns where that leaves all SMs two blocks, else of one
+    // two turns of a block's threads where that leaves all SMs two blocks, else one
     const int64_t units = p.M * p.blocks;
-    p.rows = std::max(1, (units >= (int64_t)sms * 128 ? 64 : 16) / p.blocks);
+    p.rows = std::max(1, (units >= (int64_t)sms * 128 ? 64 : 32) / p.blocks);
     p.by_blocks = FastDiv(p.blocks);
     return launch_after(fp8_rows_kernel<T>, (unsigned)std::min<int64_t>((p.M + p.rows - 1) / p.rows, (int64_t)sms * 8), 256, 0, st, p);
   }

@@ -8,8 +8,15 @@ namespace jab {
 
 constexpr float kFp8Top = 448.f;
 
-// Scale of a block whose largest magnitude is `big`; NaN where that is an infinity or a NaN.
+// Scale of a block whose largest magnitude is `big`; NaN where that is an infinity or a NaN. The quotient by a corrected
+// reciprocal is the IEEE one where nothing leaves the normal range (see `quotients`).
 __device__ __forceinline__ float fp8_scale(float big) {
+  if (quot_window(big)) {
+    constexpr float r = 1.f / kFp8Top;
+    float q = __fmul_rn(big, r);
+    q = __fmaf_rn(__fmaf_rn(q, -kFp8Top, big), r, q);
+    return __fmaf_rn(__fmaf_rn(q, -kFp8Top, big), r, q);
+  }
   return big < INFINITY ? __fdiv_rn(big, kFp8Top) : __uint_as_float(0x7fc00000u);
 }
 

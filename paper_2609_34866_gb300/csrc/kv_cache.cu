@@ -292,7 +292,8 @@ cudaError_t write_as(const WriteParams& p, int sms, cudaStream_t st) {
   // third of the heads where that leaves no thread idle: it loads a token's angles once for its rows in turn (2048 tokens of 48
   // heads of 128: 19 us for writing and reading, 22 without; but 64 tokens 4.9 instead of 4.5).
   constexpr int PER_SM = sizeof(T) == 2 ? 768 : 512;
-  const int want = p.n_heads * (DH / 16), share = p.n_tokens >= 4 * (int64_t)sms && want % 96 == 0 ? want / 3 : want;
+  const int want = p.n_heads * (DH / 16), parts = want % 96 == 0 ? 3 : MODE != kWrite && want % 64 == 0 ? 2 : 1;
+  const int share = p.n_tokens >= 4 * (int64_t)sms ? want / parts : want;
   const int threads = (std::min(share, kWriteThreads) + 31) / 32 * 32;
   const int64_t blocks = std::min<int64_t>(p.n_tokens, (int64_t)sms * std::min(32, std::max(1, PER_SM / threads)));
   return launch_after(kv_write_kernel<T, DH, BITS, MODE>, (unsigned)blocks, threads, 0, st, p);

@@ -1,9 +1,9 @@
 // A server step's bookkeeping: pages of ended sequences onto the stack of free ones, pages, slots and positions for new tokens.
 //
-// One cluster does a call: every block sums the counts of all sequences up for itself (8 bytes a sequence, from L2), then takes
-// its share of the rows and pages; what may be overwritten in place (lengths, the stack's size) is written behind the
-// cluster's barrier, when all blocks have read it. Bound: the launch and a chain of three dependent reads (counts, sums,
-// page numbers) for a decoding step; stores of 12 bytes a row for long prompts.
+// One block sums the counts of all sequences up, moves the pages and writes what may be overwritten in place (lengths, the
+// stack's size) when it has read it; with few rows it writes those too, with many a second launch does, from the starts,
+// lengths and page tables that the first has left. Bound: launches and chains of dependent reads (counts, sums, page numbers):
+// 64 single tokens take 3.9 us.
 #include <algorithm>
 
 #include "common.cuh"
@@ -16,11 +16,12 @@ namespace {
 
 constexpr int kThreads = 1024, kWarps = kThreads / 32;
 constexpr int kMostSeqs = 8192;
-constexpr int kMostBlocks = 8;      // of the cluster
-constexpr int kRowsPerBlock = 8192;  // from where one more block pays
+constexpr int kRowsInOne = 4096;   // rows that the first launch writes itself
+constexpr int kRowThreads = 256, kRowsPerBlock = 2048;
 
 struct PlanParams {
   int n_seqs, page, max_pages, free_capacity, shared;
+  FastDiv by_page;
   int64_t n_pages, n_tokens;
   const int32_t *lens, *counts, *n_free;
   int32_t *pages, *free_pages, *new_lens, *new_free, *q_start, *positions;
@@ -71,6 +72,34 @@ __device__ __forceinline__ int walk(const int* start, int n, int i, int b) {
   return b + owner(start + b, n - b, i);
 }
 
+// Slots and positions of the rows [first, end), those from `real` on padding: a warp takes a run of them, a lane four at a time (their
+// page numbers are on the way together). page(b, row, position&) is the page number of sequence b's row.
+template <class Page>
+__device__ __forceinline__ void rows_of(const PlanParams& p, int tid, int threads, int first, int end, int real, const int* start, Page page) {
+  const int warps = threads / 32, run = ((end - first + warps - 1) / warps + 31) / 32 * 32;
+  const int64_t from = first + (int64_t)(tid >> 5) * run, to = min(from + run, (int64_t)end);
+  int b = -1;
+  for (int64_t i0 = from + (tid & 31); i0 < to; i0 += 128) {
+    int pos[4], id[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int64_t i = i0 + 32 * u;
+      pos[u] = 0, id[u] = -1;
+      if (i >= to || i >= real) continue;
+      b = b < 0 ? owner(start, p.n_seqs, (int)i) : walk(start, p.n_seqs, (int)i, b);
+      id[u] = page(b, (int)i, pos[u]);
+      if (id[u] < 0 || id[u] >= p.n_pages) report(p.status, JAB_ERR_INVALID_ARG), id[u] = -1;
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int64_t i = i0 + 32 * u;
+      if (i >= to || !in_bounds(i, p.n_tokens, p.status)) continue;
+      p.positions[i] = pos[u];
+      p.slots[i] = id[u] < 0 ? -1 : (int64_t)id[u] * p.page + pos[u] - p.by_page.quot(pos[u]) * p.page;
+    }
+  }
+}
+
 // RELEASE: counts says which sequences have ended. Else counts of new tokens.
 template <bool RELEASE>
 __global__ void __launch_bounds__(kThreads, 1) kv_plan_kernel(const __grid_constant__ PlanParams p) {
@@ -82,12 +111,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_plan_kernel(const __grid_const
   if (threadIdx.x == 0) bad_s = 0;
   stream_order();
   __syncthreads();
-  const int blocks = gridDim.x, rank = blockIdx.x, tid = threadIdx.x;
+  const int tid = threadIdx.x;
   const int each = (p.n_seqs + kThreads - 1) / kThreads, b0 = min(tid * each, p.n_seqs), b1 = min(b0 + each, p.n_seqs);
   const int64_t room = (int64_t)p.max_pages * p.page;
   const int n_free = *p.n_free;
   const int same = RELEASE ? p.shared / p.page : 0;
-  auto pages_of = [&](int n) { return (n + p.page - 1) / p.page; };  // (n < 2^30, a page at most 2^12)
+  auto pages_of = [&](int n) { return n > 0 ? p.by_page.quot(n - 1) + 1 : 0; };  // (n <= 2^30)
   auto pages_for = [&](int len, int count) {  // that come or go
     return RELEASE ? (count != 0 ? max(pages_of(len) - same, 0) : 0) : pages_of(len + count) - pages_of(len);
   };
@@ -116,31 +145,27 @@ __global__ void __launch_bounds__(kThreads, 1) kv_plan_kernel(const __grid_const
       g += pages_for(len_s[b], count);
     }
   __syncthreads();
-  // in place: all blocks have read lengths, counts and the stack's size once they are past the barrier, and their shares
-  // below go by shared memory, page tables and the stack alone
-  if (blocks > 1) tc::cluster_sync();
-  if (rank == 0) {
-    for (int b = b0; b < b1; ++b) {
-      int to;
-      if (RELEASE) {
-        const int len = p.lens[b];
-        to = !bad && p.counts[b] != 0 ? min(len, p.shared) : len;
-      } else {
-        to = bad ? p.lens[b] : len_s[b] + p.counts[b];
-        p.q_start[b] = bad ? 0 : row_s[b];
-      }
-      p.new_lens[b] = to;
+  // (in place: every thread has read the stack's size, and a sequence's length and count are read by one thread alone)
+  for (int b = b0; b < b1; ++b) {
+    int to;
+    if (RELEASE) {
+      const int len = p.lens[b];
+      to = !bad && p.counts[b] != 0 ? min(len, p.shared) : len;
+    } else {
+      to = bad ? p.lens[b] : len_s[b] + p.counts[b];
+      p.q_start[b] = bad ? 0 : row_s[b];
     }
-    if (tid == 0) {
-      *p.new_free = bad ? n_free : RELEASE ? n_free + (int)all_pages : n_free - (int)all_pages;
-      if (!RELEASE) p.q_start[p.n_seqs] = bad ? 0 : (int)all_rows;
-      if (bad) report(p.status, JAB_ERR_INVALID_ARG);
-    }
+    p.new_lens[b] = to;
   }
-  const int lane = tid & 31, warp = rank * kWarps + (tid >> 5), warps = blocks * kWarps;
+  if (tid == 0) {
+    *p.new_free = bad ? n_free : RELEASE ? n_free + (int)all_pages : n_free - (int)all_pages;
+    if (!RELEASE) p.q_start[p.n_seqs] = bad ? 0 : (int)all_rows;
+    if (bad) report(p.status, JAB_ERR_INVALID_ARG);
+  }
+  const int lane = tid & 31, warp = tid >> 5;
   // pages that come or go: a warp takes a run of them
   if (!bad && all_pages > 0) {
-    const int n = (int)all_pages, run = ((n + warps - 1) / warps + 31) / 32 * 32;
+    const int n = (int)all_pages, run = ((n + kWarps - 1) / kWarps + 31) / 32 * 32;
     const int64_t first = (int64_t)warp * run;
     int b = -1;
     for (int64_t i64 = first + lane; i64 < min(first + run, (int64_t)n); i64 += 32) {
@@ -157,32 +182,26 @@ __global__ void __launch_bounds__(kThreads, 1) kv_plan_kernel(const __grid_const
         *at = id;
     }
   }
-  if (RELEASE) return;
-  // rows: a warp takes a run of them, a lane four at a time (their page numbers are on the way together)
-  const int64_t run = ((p.n_tokens + warps - 1) / warps + 31) / 32 * 32, first = (int64_t)warp * run, end = min(first + run, p.n_tokens);
-  int b = -1;
-  for (int64_t i0 = first + lane; i0 < end; i0 += 128) {
-    int pos[4], id[4];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int64_t i = i0 + 32 * u;
-      pos[u] = 0, id[u] = -1;
-      if (bad || i >= min(end, all_rows)) continue;
-      b = b < 0 ? owner(row_s, p.n_seqs, (int)i) : walk(row_s, p.n_seqs, (int)i, b);
-      pos[u] = len_s[b] + (int)i - row_s[b];
-      const int entry = pos[u] / p.page, mine = pages_of(len_s[b]);
-      // a page of this call comes from the stack: its entry may not be written yet
-      id[u] = entry < mine ? p.pages[(int64_t)b * p.max_pages + entry] : p.free_pages[n_free - 1 - page_s[b] - (entry - mine)];
-      if (id[u] < 0 || id[u] >= p.n_pages) report(p.status, JAB_ERR_INVALID_ARG), id[u] = -1;
-    }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int64_t i = i0 + 32 * u;
-      if (i >= end) continue;
-      p.positions[i] = pos[u];
-      p.slots[i] = id[u] < 0 ? -1 : (int64_t)id[u] * p.page + pos[u] % p.page;
-    }
-  }
+  if (RELEASE || p.n_tokens > kRowsInOne) return;
+  // a page of this call comes from the stack: its entry may not be written yet
+  const int real = bad ? 0 : (int)all_rows;
+  rows_of(p, tid, kThreads, 0, (int)p.n_tokens, real, row_s, [&](int b, int i, int& pos) {
+    pos = len_s[b] + i - row_s[b];
+    const int entry = p.by_page.quot(pos), mine = pages_of(len_s[b]);
+    return entry < mine ? p.pages[(int64_t)b * p.max_pages + entry] : p.free_pages[n_free - 1 - page_s[b] - (entry - mine)];
+  });
+}
+
+__global__ void __launch_bounds__(kRowThreads) kv_rows_kernel(const __grid_constant__ PlanParams p) {
+  extern __shared__ int start[];  // [n_seqs + 1]
+  stream_order();
+  for (int b = threadIdx.x; b <= p.n_seqs; b += kRowThreads) start[b] = p.q_start[b];
+  __syncthreads();
+  const int first = blockIdx.x * kRowsPerBlock, end = min(first + kRowsPerBlock, (int)p.n_tokens);
+  rows_of(p, threadIdx.x, kRowThreads, first, end, min(start[p.n_seqs], end), start, [&](int b, int i, int& pos) {
+    pos = p.new_lens[b] - (start[b + 1] - i);
+    return p.pages[(int64_t)b * p.max_pages + p.by_page.quot(pos)];
+  });
 }
 
 template <bool RELEASE>
@@ -193,6 +212,7 @@ cudaError_t launch(const KvPlanArgs& a, cudaStream_t st) {
   p.lens = a.lens, p.counts = a.counts, p.n_free = a.n_free;
   p.pages = a.pages, p.free_pages = a.free_pages, p.new_lens = a.new_lens, p.new_free = a.new_free;
   p.q_start = a.q_start, p.positions = a.positions, p.slots = a.slots;
+  p.by_page = FastDiv(a.page);
   p.status = a.status;
   auto kern = kv_plan_kernel<RELEASE>;
   static SetUp ready;
@@ -201,29 +221,14 @@ cudaError_t launch(const KvPlanArgs& a, cudaStream_t st) {
   if (e != cudaSuccess) return e;
   e = ready.once(dev, [&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 3 * kMostSeqs * 4); });
   if (e != cudaSuccess) return e;
-  const int64_t share = RELEASE ? (int64_t)a.n_seqs * 8 : a.n_tokens;
-  int blocks = 1;
-  while (blocks < kMostBlocks && share > (int64_t)blocks * kRowsPerBlock) blocks *= 2;
-  cudaLaunchConfig_t cfg = {};
-  cudaLaunchAttribute at[2];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  at[1].id = cudaLaunchAttributeClusterDimension;
-  at[1].val.clusterDim.x = blocks;
-  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
-  cfg.gridDim = dim3(blocks);
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = (size_t)3 * a.n_seqs * 4;
-  cfg.stream = st;
-  cfg.attrs = at;
-  cfg.numAttrs = blocks > 1 ? 2 : 1;
-  e = cudaLaunchKernelEx(&cfg, kern, p);
-  if (e != cudaSuccess) cudaGetLastError();
-  return e;
+  e = launch_after(kern, 1u, kThreads, (size_t)3 * a.n_seqs * 4, st, p);
+  if (e != cudaSuccess || RELEASE || a.n_tokens <= kRowsInOne) return e;
+  return launch_after(kv_rows_kernel, (unsigned)((a.n_tokens + kRowsPerBlock - 1) / kRowsPerBlock), kRowThreads, (size_t)(a.n_seqs + 1) * 4, st, p);
 }
 
 }  // namespace
 
+int kv_plan_kernels(const KvPlanArgs& a) { return a.n_tokens > kRowsInOne ? 2 : 1; }
 cudaError_t launch_kv_plan(const KvPlanArgs& a, cudaStream_t st) { return launch<false>(a, st); }
 cudaError_t launch_kv_release(const KvPlanArgs& a, cudaStream_t st) { return launch<true>(a, st); }
 

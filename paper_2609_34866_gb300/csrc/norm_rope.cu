@@ -42,12 +42,12 @@ __global__ void __launch_bounds__(kBackThreads, 2) norm_rope_back_kernel(const _
   const bool exists = head < p.n_q + p.n_k, is_q = head < p.n_q;
   const bool turns = p.positions != nullptr && 16 * t < p.rotary, pairs = p.neighbours || 16 * t >= p.rotary;
   const int at0 = pairs ? 16 * t : 8 * t, at1 = pairs ? at0 + 8 : at0 + p.rotary / 2;
-  float w[16], dw[16];
+  float2 w[8], dw[8];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
+  for (int i = 0; i < 8; ++i) {
     const float* from = is_q ? p.wq : p.wk;
-    w[i] = from != nullptr && exists ? __ldg(from + (i < 8 ? at0 + i : at1 + i - 8)) : 1.f;
-    dw[i] = 0.f;
+    w[i] = from != nullptr && exists ? __ldg(reinterpret_cast<const float2*>(from + (i < 4 ? at0 + 2 * i : at1 + 2 * i - 8))) : make_float2(1.f, 1.f);
+    dw[i] = make_float2(0.f, 0.f);
   }
   const T* x = static_cast<const T*>(p.x) + (int64_t)head * DH;
   const T* dy = is_q ? static_cast<const T*>(p.dq) + (int64_t)head * DH : static_cast<const T*>(p.dk) + (int64_t)(head - p.n_q) * DH;
@@ -63,7 +63,7 @@ __global__ void __launch_bounds__(kBackThreads, 2) norm_rope_back_kernel(const _
   };
   fetch(blockIdx.x);
   for (int64_t token = blockIdx.x; token < p.n_tokens; token += gridDim.x) {
-    float a[8], b[8], g[8], h[8];
+    alignas(8) float a[8], b[8], g[8], h[8];
     x0.numbers(a), x1.numbers(b), g0.numbers(g), g1.numbers(h);
     const int pos = next;
     const bool fine = p.positions == nullptr || (pos >= 0 && pos < p.rope_len);
@@ -74,36 +74,50 @@ __global__ void __launch_bounds__(kBackThreads, 2) norm_rope_back_kernel(const _
       load8(p.sin_t + (int64_t)pos * (p.rotary / 2) + 8 * t, s);
     }
     fetch(token + gridDim.x);
+    // (packed pairs halve the instructions; no rounding here is part of a definition)
+    float2 *a2 = reinterpret_cast<float2*>(a), *b2 = reinterpret_cast<float2*>(b), *g2 = reinterpret_cast<float2*>(g), *h2 = reinterpret_cast<float2*>(h);
     if (turns && fine) {
-      auto back = [](float& y, float& z, float cs, float sn) {
-        const float da = y * cs + z * sn, db = z * cs - y * sn;
-        y = da, z = db;
-      };
       if (p.neighbours) {
+        auto back = [](float& y, float& z, float cs, float sn) {
+          const float da = y * cs + z * sn, db = z * cs - y * sn;
+          y = da, z = db;
+        };
 #pragma unroll
         for (int i = 0; i < 4; ++i) back(g[2 * i], g[2 * i + 1], c[i], s[i]), back(h[2 * i], h[2 * i + 1], c[4 + i], s[4 + i]);
       } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) back(g[i], h[i], c[i], s[i]);
+        for (int i = 0; i < 4; ++i) {
+          const float2 cs = make_float2(c[2 * i], c[2 * i + 1]), sn = make_float2(s[2 * i], s[2 * i + 1]), ns = make_float2(-sn.x, -sn.y);
+          const float2 y = g2[i], z = h2[i];
+          g2[i] = tc::fma2(z, sn, tc::mul2(y, cs));
+          h2[i] = tc::fma2(y, ns, tc::mul2(z, cs));
+        }
       }
     }
     if (p.eps > 0.f) {
       const float r = norm_factor<LANES>(a, b, p.eps);
-      float dot = 0.f;
+      const float2 r2 = make_float2(r, r);
+      float2 dot2 = make_float2(0.f, 0.f);
+      if (!fine) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        a[i] *= r, b[i] *= r;
-        if (fine) dw[i] += g[i] * a[i], dw[8 + i] += h[i] * b[i];
-        g[i] *= w[i], h[i] *= w[8 + i];
-        dot += g[i] * a[i] + h[i] * b[i];
+        for (int i = 0; i < 4; ++i) g2[i] = h2[i] = make_float2(0.f, 0.f);
       }
 #pragma unroll
-      for (int o = LANES / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
-      dot *= 1.f / DH;
+      for (int i = 0; i < 4; ++i) {
+        a2[i] = tc::mul2(a2[i], r2), b2[i] = tc::mul2(b2[i], r2);
+        dw[i] = tc::fma2(g2[i], a2[i], dw[i]), dw[4 + i] = tc::fma2(h2[i], b2[i], dw[4 + i]);
+        g2[i] = tc::mul2(g2[i], w[i]), h2[i] = tc::mul2(h2[i], w[4 + i]);
+        dot2 = tc::fma2(h2[i], b2[i], tc::fma2(g2[i], a2[i], dot2));
+      }
+      float dot = dot2.x + dot2.y;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        g[i] = r * (g[i] - a[i] * dot);
-        h[i] = r * (h[i] - b[i] * dot);
+      for (int o = LANES / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+      dot *= -1.f / DH;
+      const float2 d2 = make_float2(dot, dot);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        g2[i] = tc::mul2(r2, tc::fma2(a2[i], d2, g2[i]));
+        h2[i] = tc::mul2(r2, tc::fma2(b2[i], d2, h2[i]));
       }
       if (exists && !(r == r)) report(p.status, JAB_ERR_NONFINITE);
     }
@@ -117,7 +131,10 @@ __global__ void __launch_bounds__(kBackThreads, 2) norm_rope_back_kernel(const _
   }
   if (p.part == nullptr) return;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) sums[slot][at0 + i] = exists ? dw[i] : 0.f, sums[slot][at1 + i] = exists ? dw[8 + i] : 0.f;
+  for (int i = 0; i < 4; ++i) {
+    *reinterpret_cast<float2*>(&sums[slot][at0 + 2 * i]) = dw[i];  // (0 without a head)
+    *reinterpret_cast<float2*>(&sums[slot][at1 + 2 * i]) = dw[4 + i];
+  }
   __syncthreads();
   if (threadIdx.x < 2 * DH) {
     const int d = threadIdx.x % DH, first = blockIdx.y * HEADS;
@@ -129,18 +146,18 @@ __global__ void __launch_bounds__(kBackThreads, 2) norm_rope_back_kernel(const _
   }
 }
 
-// The blocks' sums, in their order: 32 columns a block, eight runs of blocks each, added up as pairs.
+// The blocks' sums, in their order: eight columns a block of threads, 32 runs of blocks each, added up as pairs.
 __global__ void __launch_bounds__(256) weight_sum_kernel(const float* part, int n, int dh, float* dwq, float* dwk) {
-  __shared__ float hi_s[8][32], lo_s[8][32];
+  __shared__ float hi_s[32][8], lo_s[32][8];
   stream_order();
-  const int lane = threadIdx.x & 31, run = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
+  const int lane = threadIdx.x & 7, run = threadIdx.x >> 3, col = blockIdx.x * 8 + lane;
   float hi = 0.f, lo = 0.f;
 #pragma unroll 8
-  for (int i = run; i < n; i += 8) pair_add(hi, lo, part[(int64_t)i * 2 * dh + col], 0.f);
+  for (int i = run; i < n; i += 32) pair_add(hi, lo, part[(int64_t)i * 2 * dh + col], 0.f);
   hi_s[run][lane] = hi, lo_s[run][lane] = lo;
   __syncthreads();
   if (run != 0) return;
-  for (int i = 1; i < 8; ++i) pair_add(hi, lo, hi_s[i][lane], lo_s[i][lane]);
+  for (int i = 1; i < 32; ++i) pair_add(hi, lo, hi_s[i][lane], lo_s[i][lane]);
   float* out = col < dh ? dwq : dwk;
   if (out != nullptr) out[col < dh ? col : col - dh] = fabsf(hi) < INFINITY ? hi + lo : hi;
 }
@@ -180,7 +197,9 @@ template <class T, int DH>
 cudaError_t back_as(const BackParams& p, float* dwq, float* dwk, cudaStream_t st) {
   constexpr int HEADS = kBackThreads / (DH / 16);
   const int gy = (p.n_q + p.n_k + HEADS - 1) / HEADS;
-  const int gx = p.n_tokens > 0 ? (int)std::min<int64_t>(p.n_tokens, std::max(1, kMostParts / gy)) : 0;
+  // four tokens a block and more where the weights' gradients are wanted: every block has a part of them to be added up
+  const int64_t at_most = p.part != nullptr ? (p.n_tokens + 3) / 4 : p.n_tokens;
+  const int gx = (int)std::min<int64_t>(at_most, std::max(1, kMostParts / gy));
   if (gx > 0) {
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute at[1];
@@ -198,7 +217,7 @@ cudaError_t back_as(const BackParams& p, float* dwq, float* dwk, cudaStream_t st
     }
   }
   if (p.part == nullptr) return cudaSuccess;
-  return launch_after(weight_sum_kernel, 2 * DH / 32, 256, 0, st, (const float*)p.part, gx * gy, DH, dwq, dwk);
+  return launch_after(weight_sum_kernel, 2 * DH / 8, 256, 0, st, (const float*)p.part, gx * gy, DH, dwq, dwk);
 }
 template <class T>
 cudaError_t back_type(const BackParams& p, int dh, float* dwq, float* dwk, cudaStream_t st) {

@@ -87,6 +87,7 @@ struct KvPlanArgs {
   int64_t* slots;
   int* status;
 };
+int kv_plan_kernels(const KvPlanArgs& a);  // how many launch_kv_plan launches
 cudaError_t launch_kv_plan(const KvPlanArgs& a, cudaStream_t st);
 cudaError_t launch_kv_release(const KvPlanArgs& a, cudaStream_t st);
 

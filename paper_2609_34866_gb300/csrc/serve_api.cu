@@ -437,7 +437,7 @@ jab_status jab_kv_plan(const jab_kv_cache* cache, int32_t n_seqs, int64_t n_toke
   a.lens = lens_dev, a.counts = counts_dev, a.pages = pages_dev, a.free_pages = const_cast<int32_t*>(free_dev), a.n_free = n_free_dev;
   a.new_lens = new_lens_dev, a.new_free = new_free_dev, a.q_start = q_start_dev, a.slots = slots_dev, a.positions = positions_dev;
   a.status = status;
-  JAB_LAUNCH("kv_plan", 1, launch_kv_plan(a, st));
+  JAB_LAUNCH("kv_plan", kv_plan_kernels(a), launch_kv_plan(a, st));
   return JAB_OK;
 }
 
