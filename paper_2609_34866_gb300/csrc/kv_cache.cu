@@ -81,7 +81,7 @@ template <class T, int DH, int BITS, int MODE>
 __global__ void __launch_bounds__(kWriteThreads, sizeof(T) == 2 ? 2 : 1) kv_write_kernel(const __grid_constant__ WriteParams p) {
   constexpr int LANES = DH / 16;
   constexpr bool NORMED = MODE != kWrite;
-  __shared__ float weights[NORMED ? 2 : 1][NORMED ? DH : 1];  // of the norms of Q and K
+  __shared__ alignas(16) float weights[NORMED ? 2 : 1][NORMED ? DH : 1];  // of the norms of Q and K
   stream_order();
   const int t = threadIdx.x % LANES, head0 = threadIdx.x / LANES, heads = blockDim.x / LANES;
   // The thread's groups of 8: partners of a rotation by halves where it turns them, else neighbours.
@@ -137,11 +137,13 @@ __global__ void __launch_bounds__(kWriteThreads, sizeof(T) == 2 ? 2 : 1) kv_writ
       if (p.eps > 0.f) {
         const float r = norm_factor<LANES>(a, b, p.eps);
         if (live && is_k) {
-          const float* w = weights[is_q ? 0 : 1];
+          const float2 *w0 = reinterpret_cast<const float2*>(weights[is_q ? 0 : 1] + at0), *w1 = reinterpret_cast<const float2*>(weights[is_q ? 0 : 1] + at1);
+          const float2 r2 = make_float2(r, r);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            a[i] = __fmul_rn(__fmul_rn(a[i], r), w[at0 + i]);
-            b[i] = __fmul_rn(__fmul_rn(b[i], r), w[at1 + i]);
+          for (int i = 0; i < 4; ++i) {
+            const float2 x = tc::mul2(tc::mul2(make_float2(a[2 * i], a[2 * i + 1]), r2), w0[i]);
+            const float2 y = tc::mul2(tc::mul2(make_float2(b[2 * i], b[2 * i + 1]), r2), w1[i]);
+            a[2 * i] = x.x, a[2 * i + 1] = x.y, b[2 * i] = y.x, b[2 * i + 1] = y.y;
           }
           if (!(r == r)) report(p.status, JAB_ERR_NONFINITE);
         }
@@ -172,8 +174,10 @@ __global__ void __launch_bounds__(kWriteThreads, sizeof(T) == 2 ? 2 : 1) kv_writ
     if (token < p.n_tokens) fetch(token, head);
     float big = 0.f;
     if (live) {
+      if (MODE != kRows || std::is_same<T, half_t>::value) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) big = largest(big, a[i], b[i]);
+        for (int i = 0; i < 8; ++i) big = largest(big, a[i], b[i]);
+      }
       if (is_q || MODE == kRows) {
         const int n = is_q ? p.n_q : p.n_kv;
         const int64_t ld = MODE != kRows ? (int64_t)p.n_q * DH : is_q ? p.ldq : p.ldk;
@@ -187,9 +191,10 @@ __global__ void __launch_bounds__(kWriteThreads, sizeof(T) == 2 ? 2 : 1) kv_writ
         if (std::is_same<T, half_t>::value && !(big < 65520.f)) report(p.status, JAB_ERR_RANGE);
       }
     }
+    if constexpr (MODE == kRows) continue;
 #pragma unroll
     for (int o = LANES / 2; o > 0; o >>= 1) big = largest(big, __shfl_xor_sync(0xffffffffu, big, o), 0.f);
-    if (MODE == kRows || is_q || !live) continue;
+    if (is_q || !live) continue;
     const bool fine = big < INFINITY;
     if (!fine) report(p.status, JAB_ERR_NONFINITE);
     const float scale = fine ? __fdiv_rn(big, (float)((1 << (BITS - 1)) - 1)) : __uint_as_float(0x7fc00000u);

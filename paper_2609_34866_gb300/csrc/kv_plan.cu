@@ -1,9 +1,9 @@
 // A server step's bookkeeping: pages of ended sequences onto the stack of free ones, pages, slots and positions for new tokens.
 //
-// One block sums the counts of all sequences up, moves the pages and writes what may be overwritten in place (lengths, the
-// stack's size) when it has read it; with few rows it writes those too, with many a second launch does, from the starts,
-// lengths and page tables that the first has left. Bound: launches and chains of dependent reads (counts, sums, page numbers):
-// 64 single tokens take 3.9 us.
+// One block sums the counts of all sequences up and writes what may be overwritten in place (lengths, the stack's size) when it
+// has read it; with few rows it also moves the pages and writes the rows, with many a second launch does, whose blocks sum up
+// again what the first has left (250000 rows of 1000 sequences: 28 us for release and plan where one block moves the pages). Bound:
+// launches and chains of dependent reads (counts, sums, page numbers): 64 single tokens take 3.6 us.
 #include <algorithm>
 
 #include "common.cuh"
@@ -30,8 +30,9 @@ struct PlanParams {
 };
 
 // Sums over the block's threads before this one (a, b) and over all of them (all_a, all_b).
+template <int WARPS>
 __device__ __forceinline__ void block_scan(int64_t& a, int64_t& b, int64_t& all_a, int64_t& all_b) {
-  __shared__ int64_t warp_a[kWarps], warp_b[kWarps];
+  __shared__ int64_t warp_a[32], warp_b[32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t a0 = a, b0 = b;
 #pragma unroll
@@ -41,7 +42,7 @@ __device__ __forceinline__ void block_scan(int64_t& a, int64_t& b, int64_t& all_
   }
   if (lane == 31) warp_a[warp] = a, warp_b[warp] = b;
   __syncthreads();
-  int64_t x = warp_a[lane], y = warp_b[lane];
+  int64_t x = lane < WARPS ? warp_a[lane] : 0, y = lane < WARPS ? warp_b[lane] : 0;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const int64_t u = __shfl_up_sync(0xffffffffu, x, o), v = __shfl_up_sync(0xffffffffu, y, o);
@@ -72,28 +73,69 @@ __device__ __forceinline__ int walk(const int* start, int n, int i, int b) {
   return b + owner(start + b, n - b, i);
 }
 
-// Slots and positions of the rows [first, end), those from `real` on padding: a warp takes a run of them, a lane four at a time (their
-// page numbers are on the way together). page(b, row, position&) is the page number of sequence b's row.
-template <class Page>
-__device__ __forceinline__ void rows_of(const PlanParams& p, int tid, int threads, int first, int end, int real, const int* start, Page page) {
-  const int warps = threads / 32, run = ((end - first + warps - 1) / warps + 31) / 32 * 32;
-  const int64_t from = first + (int64_t)(tid >> 5) * run, to = min(from + run, (int64_t)end);
+// Lengths, rows and pages before each sequence, in shared memory.
+struct Sums {
+  int *len, *row, *page;
+  int n_free, pages, rows;  // the stack's size, pages and rows in all
+};
+__device__ __forceinline__ int pages_of(const PlanParams& p, int n) { return n > 0 ? p.by_page.quot(n - 1) + 1 : 0; }  // (n <= 2^30)
+
+// The pages that come or go: each warp of `warps` a run of them, a lane eight at a time (their numbers are on the way together).
+template <bool RELEASE>
+__device__ __forceinline__ void move_pages(const PlanParams& p, const Sums& s, int warp, int warps) {
+  const int n = s.pages, run = ((n + warps - 1) / warps + 31) / 32 * 32, same = RELEASE ? p.shared / p.page : 0;
+  const int64_t first = (int64_t)warp * run, end = min(first + run, (int64_t)n);
   int b = -1;
-  for (int64_t i0 = from + (tid & 31); i0 < to; i0 += 128) {
+  for (int64_t i0 = first + (threadIdx.x & 31); i0 < end; i0 += 256) {
+    const int32_t* from[8];
+    int32_t* to[8];
+    int id[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int64_t i64 = i0 + 32 * u;
+      from[u] = nullptr;
+      if (i64 >= end) continue;
+      const int i = (int)i64;
+      b = b < 0 ? owner(s.page, p.n_seqs, i) : walk(s.page, p.n_seqs, i, b);
+      const int entry = (RELEASE ? same : pages_of(p, s.len[b])) + i - s.page[b], at = RELEASE ? s.n_free + i : s.n_free - 1 - i;
+      if (!in_bounds(entry, p.max_pages, p.status) || !in_bounds(at, p.free_capacity, p.status)) continue;
+      int32_t* table = p.pages + (int64_t)b * p.max_pages + entry;
+      int32_t* stack = p.free_pages + at;
+      from[u] = RELEASE ? table : stack, to[u] = RELEASE ? stack : table;
+      id[u] = *from[u];
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      if (from[u] == nullptr) continue;
+      if (id[u] < 0 || id[u] >= p.n_pages) report(p.status, JAB_ERR_INVALID_ARG);
+      *to[u] = id[u];
+    }
+  }
+}
+
+// Slots and positions of all rows, padding behind the last: as above, four rows of a lane at a time.
+__device__ __forceinline__ void write_rows(const PlanParams& p, const Sums& s, int warp, int warps) {
+  const int n = (int)p.n_tokens, run = ((n + warps - 1) / warps + 31) / 32 * 32;
+  const int64_t first = (int64_t)warp * run, end = min(first + run, (int64_t)n);
+  int b = -1;
+  for (int64_t i0 = first + (threadIdx.x & 31); i0 < end; i0 += 128) {
     int pos[4], id[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const int64_t i = i0 + 32 * u;
       pos[u] = 0, id[u] = -1;
-      if (i >= to || i >= real) continue;
-      b = b < 0 ? owner(start, p.n_seqs, (int)i) : walk(start, p.n_seqs, (int)i, b);
-      id[u] = page(b, (int)i, pos[u]);
+      if (i >= end || i >= s.rows) continue;
+      b = b < 0 ? owner(s.row, p.n_seqs, (int)i) : walk(s.row, p.n_seqs, (int)i, b);
+      pos[u] = s.len[b] + (int)i - s.row[b];
+      // a page of this call comes from the stack: its entry may not be written yet
+      const int entry = p.by_page.quot(pos[u]), mine = pages_of(p, s.len[b]);
+      id[u] = entry < mine ? p.pages[(int64_t)b * p.max_pages + entry] : p.free_pages[s.n_free - 1 - s.page[b] - (entry - mine)];
       if (id[u] < 0 || id[u] >= p.n_pages) report(p.status, JAB_ERR_INVALID_ARG), id[u] = -1;
     }
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const int64_t i = i0 + 32 * u;
-      if (i >= to || !in_bounds(i, p.n_tokens, p.status)) continue;
+      if (i >= end || !in_bounds(i, p.n_tokens, p.status)) continue;
       p.positions[i] = pos[u];
       p.slots[i] = id[u] < 0 ? -1 : (int64_t)id[u] * p.page + pos[u] - p.by_page.quot(pos[u]) * p.page;
     }
@@ -104,9 +146,7 @@ __device__ __forceinline__ void rows_of(const PlanParams& p, int tid, int thread
 template <bool RELEASE>
 __global__ void __launch_bounds__(kThreads, 1) kv_plan_kernel(const __grid_constant__ PlanParams p) {
   extern __shared__ int smem[];
-  int* len_s = smem;                    // [n_seqs]
-  int* row_s = len_s + p.n_seqs;        // rows before a sequence [n_seqs]
-  int* page_s = row_s + p.n_seqs;       // pages given or taken before a sequence [n_seqs]
+  int *len_s = smem, *row_s = len_s + p.n_seqs, *page_s = row_s + p.n_seqs;  // [n_seqs] each
   __shared__ int bad_s;
   if (threadIdx.x == 0) bad_s = 0;
   stream_order();
@@ -116,9 +156,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_plan_kernel(const __grid_const
   const int64_t room = (int64_t)p.max_pages * p.page;
   const int n_free = *p.n_free;
   const int same = RELEASE ? p.shared / p.page : 0;
-  auto pages_of = [&](int n) { return n > 0 ? p.by_page.quot(n - 1) + 1 : 0; };  // (n <= 2^30)
   auto pages_for = [&](int len, int count) {  // that come or go
-    return RELEASE ? (count != 0 ? max(pages_of(len) - same, 0) : 0) : pages_of(len + count) - pages_of(len);
+    return RELEASE ? (count != 0 ? max(pages_of(p, len) - same, 0) : 0) : pages_of(p, len + count) - pages_of(p, len);
   };
   int64_t rows = 0, pages = 0;
   bool bad = n_free < 0 || n_free > p.free_capacity;
@@ -134,7 +173,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_plan_kernel(const __grid_const
   }
   int64_t all_rows, all_pages;
   if (bad) bad_s = 1;  // (any thread's word)
-  block_scan(rows, pages, all_rows, all_pages);
+  block_scan<kWarps>(rows, pages, all_rows, all_pages);
   bad = bad_s != 0 || all_rows > p.n_tokens || (RELEASE ? n_free + all_pages > p.free_capacity : all_pages > n_free);
   int64_t r = rows, g = pages;
   if (!bad)
@@ -162,46 +201,40 @@ __global__ void __launch_bounds__(kThreads, 1) kv_plan_kernel(const __grid_const
     if (!RELEASE) p.q_start[p.n_seqs] = bad ? 0 : (int)all_rows;
     if (bad) report(p.status, JAB_ERR_INVALID_ARG);
   }
-  const int lane = tid & 31, warp = tid >> 5;
-  // pages that come or go: a warp takes a run of them
-  if (!bad && all_pages > 0) {
-    const int n = (int)all_pages, run = ((n + kWarps - 1) / kWarps + 31) / 32 * 32;
-    const int64_t first = (int64_t)warp * run;
-    int b = -1;
-    for (int64_t i64 = first + lane; i64 < min(first + run, (int64_t)n); i64 += 32) {
-      const int i = (int)i64;
-      b = b < 0 ? owner(page_s, p.n_seqs, i) : walk(page_s, p.n_seqs, i, b);
-      const int entry = (RELEASE ? same : pages_of(len_s[b])) + i - page_s[b];
-      int32_t* at = p.pages + (int64_t)b * p.max_pages + entry;
-      int32_t* stack = p.free_pages + (RELEASE ? n_free + i : n_free - 1 - i);
-      const int id = RELEASE ? *at : *stack;
-      if (id < 0 || id >= p.n_pages) report(p.status, JAB_ERR_INVALID_ARG);
-      if (RELEASE)
-        *stack = id;
-      else
-        *at = id;
-    }
-  }
-  if (RELEASE || p.n_tokens > kRowsInOne) return;
-  // a page of this call comes from the stack: its entry may not be written yet
-  const int real = bad ? 0 : (int)all_rows;
-  rows_of(p, tid, kThreads, 0, (int)p.n_tokens, real, row_s, [&](int b, int i, int& pos) {
-    pos = len_s[b] + i - row_s[b];
-    const int entry = p.by_page.quot(pos), mine = pages_of(len_s[b]);
-    return entry < mine ? p.pages[(int64_t)b * p.max_pages + entry] : p.free_pages[n_free - 1 - page_s[b] - (entry - mine)];
-  });
+  if (!RELEASE && p.n_tokens > kRowsInOne) return;
+  Sums sums{len_s, row_s, page_s, n_free, bad ? 0 : (int)all_pages, bad ? 0 : (int)all_rows};
+  move_pages<RELEASE>(p, sums, tid >> 5, kWarps);
+  if (!RELEASE) write_rows(p, sums, tid >> 5, kWarps);
 }
 
+// Pages and rows behind a first launch that did the rest (a call that it refused has no rows).
 __global__ void __launch_bounds__(kRowThreads) kv_rows_kernel(const __grid_constant__ PlanParams p) {
-  extern __shared__ int start[];  // [n_seqs + 1]
+  extern __shared__ int smem[];
+  int *len_s = smem, *row_s = len_s + p.n_seqs, *page_s = row_s + p.n_seqs;
   stream_order();
-  for (int b = threadIdx.x; b <= p.n_seqs; b += kRowThreads) start[b] = p.q_start[b];
+  const int tid = threadIdx.x, each = (p.n_seqs + kRowThreads - 1) / kRowThreads, b0 = min(tid * each, p.n_seqs), b1 = min(b0 + each, p.n_seqs);
+  int64_t none = 0, pages = 0, all_none, all_pages;
+  auto pages_for = [&](int b, int& len) {
+    const int count = p.q_start[b + 1] - p.q_start[b], now = p.new_lens[b];
+    len = now - count;
+    return count > 0 ? pages_of(p, now) - pages_of(p, len) : 0;
+  };
+  for (int b = b0; b < b1; ++b) {
+    int len;
+    pages += pages_for(b, len);
+    len_s[b] = len, row_s[b] = p.q_start[b];
+  }
+  block_scan<kRowThreads / 32>(none, pages, all_none, all_pages);
+  for (int b = b0; b < b1; ++b) {
+    int len;
+    page_s[b] = (int)pages;
+    pages += pages_for(b, len);
+  }
   __syncthreads();
-  const int first = blockIdx.x * kRowsPerBlock, end = min(first + kRowsPerBlock, (int)p.n_tokens);
-  rows_of(p, threadIdx.x, kRowThreads, first, end, min(start[p.n_seqs], end), start, [&](int b, int i, int& pos) {
-    pos = p.new_lens[b] - (start[b + 1] - i);
-    return p.pages[(int64_t)b * p.max_pages + p.by_page.quot(pos)];
-  });
+  const Sums sums{len_s, row_s, page_s, *p.new_free + (int)all_pages, (int)all_pages, p.q_start[p.n_seqs]};
+  const int warp = blockIdx.x * (kRowThreads / 32) + (tid >> 5), warps = gridDim.x * (kRowThreads / 32);
+  move_pages<false>(p, sums, warp, warps);
+  write_rows(p, sums, warp, warps);
 }
 
 template <bool RELEASE>
@@ -219,11 +252,14 @@ cudaError_t launch(const KvPlanArgs& a, cudaStream_t st) {
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
-  e = ready.once(dev, [&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 3 * kMostSeqs * 4); });
+  e = ready.once(dev, [&] {
+    const cudaError_t f = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 3 * kMostSeqs * 4);
+    return f != cudaSuccess ? f : cudaFuncSetAttribute(kv_rows_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 3 * kMostSeqs * 4);
+  });
   if (e != cudaSuccess) return e;
   e = launch_after(kern, 1u, kThreads, (size_t)3 * a.n_seqs * 4, st, p);
   if (e != cudaSuccess || RELEASE || a.n_tokens <= kRowsInOne) return e;
-  return launch_after(kv_rows_kernel, (unsigned)((a.n_tokens + kRowsPerBlock - 1) / kRowsPerBlock), kRowThreads, (size_t)(a.n_seqs + 1) * 4, st, p);
+  return launch_after(kv_rows_kernel, (unsigned)((a.n_tokens + kRowsPerBlock - 1) / kRowsPerBlock), kRowThreads, (size_t)3 * a.n_seqs * 4, st, p);
 }
 
 }  // namespace

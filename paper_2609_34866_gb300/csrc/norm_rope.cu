@@ -32,23 +32,27 @@ constexpr int kBackThreads = 256;
 constexpr int kMostParts = 608;  // blocks along the tokens times blocks along the heads, where the heads allow it
 
 // A thread stays with one head's two groups of 8 (as in the writing kernel) and goes over the tokens, so that its share of the
-// weights' gradient is 16 registers. The next token's rows are under way while one is worked on.
+// weights' gradient is 16 registers. The next token's rows are under way while one is worked on (two ahead: slower, registers).
 template <class T, int DH>
 __global__ void __launch_bounds__(kBackThreads, 2) norm_rope_back_kernel(const __grid_constant__ BackParams p) {
-  constexpr int LANES = DH / 16, HEADS = kBackThreads / LANES;
-  __shared__ float sums[HEADS][DH];
+  constexpr int LANES = DH / 16;
+  __shared__ alignas(16) float sums[kBackThreads / LANES][DH];
+  __shared__ alignas(16) float weights[2][DH];
   stream_order();
-  const int t = threadIdx.x % LANES, slot = threadIdx.x / LANES, head = blockIdx.y * HEADS + slot;
+  for (int i = threadIdx.x; i < 2 * DH; i += blockDim.x) {
+    const float* from = i < DH ? p.wq : p.wk;
+    weights[i / DH][i % DH] = from != nullptr ? __ldg(from + i % DH) : 1.f;
+  }
+  __syncthreads();
+  const int heads = blockDim.x / LANES;
+  const int t = threadIdx.x % LANES, slot = threadIdx.x / LANES, head = blockIdx.y * heads + slot;
   const bool exists = head < p.n_q + p.n_k, is_q = head < p.n_q;
   const bool turns = p.positions != nullptr && 16 * t < p.rotary, pairs = p.neighbours || 16 * t >= p.rotary;
   const int at0 = pairs ? 16 * t : 8 * t, at1 = pairs ? at0 + 8 : at0 + p.rotary / 2;
-  float2 w[8], dw[8];
+  const float2 *w0 = reinterpret_cast<const float2*>(weights[is_q ? 0 : 1] + at0), *w1 = reinterpret_cast<const float2*>(weights[is_q ? 0 : 1] + at1);
+  float2 dw[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float* from = is_q ? p.wq : p.wk;
-    w[i] = from != nullptr && exists ? __ldg(reinterpret_cast<const float2*>(from + (i < 4 ? at0 + 2 * i : at1 + 2 * i - 8))) : make_float2(1.f, 1.f);
-    dw[i] = make_float2(0.f, 0.f);
-  }
+  for (int i = 0; i < 8; ++i) dw[i] = make_float2(0.f, 0.f);
   const T* x = static_cast<const T*>(p.x) + (int64_t)head * DH;
   const T* dy = is_q ? static_cast<const T*>(p.dq) + (int64_t)head * DH : static_cast<const T*>(p.dk) + (int64_t)(head - p.n_q) * DH;
   const int64_t lddy = is_q ? p.lddq : p.lddk;
@@ -95,29 +99,34 @@ __global__ void __launch_bounds__(kBackThreads, 2) norm_rope_back_kernel(const _
       }
     }
     if (p.eps > 0.f) {
-      const float r = norm_factor<LANES>(a, b, p.eps);
-      const float2 r2 = make_float2(r, r);
-      float2 dot2 = make_float2(0.f, 0.f);
+      // r to a few ulp does here: the two sums of a row go through the lanes together
+      float2 sq2 = make_float2(0.f, 0.f), dot2 = make_float2(0.f, 0.f);
       if (!fine) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) g2[i] = h2[i] = make_float2(0.f, 0.f);
       }
+      float2 u2[8];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        a2[i] = tc::mul2(a2[i], r2), b2[i] = tc::mul2(b2[i], r2);
-        dw[i] = tc::fma2(g2[i], a2[i], dw[i]), dw[4 + i] = tc::fma2(h2[i], b2[i], dw[4 + i]);
-        g2[i] = tc::mul2(g2[i], w[i]), h2[i] = tc::mul2(h2[i], w[4 + i]);
-        dot2 = tc::fma2(h2[i], b2[i], tc::fma2(g2[i], a2[i], dot2));
+        u2[i] = tc::mul2(g2[i], w0[i]), u2[4 + i] = tc::mul2(h2[i], w1[i]);
+        sq2 = tc::fma2(b2[i], b2[i], tc::fma2(a2[i], a2[i], sq2));
+        dot2 = tc::fma2(u2[4 + i], b2[i], tc::fma2(u2[i], a2[i], dot2));
       }
-      float dot = dot2.x + dot2.y;
+      float sq = sq2.x + sq2.y, dot = dot2.x + dot2.y;
 #pragma unroll
-      for (int o = LANES / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
-      dot *= -1.f / DH;
-      const float2 d2 = make_float2(dot, dot);
+      for (int o = LANES / 2; o > 0; o >>= 1) {
+        sq += __shfl_xor_sync(0xffffffffu, sq, o);
+        dot += __shfl_xor_sync(0xffffffffu, dot, o);
+      }
+      const float mean = sq * (1.f / DH) + p.eps;
+      const float r = mean < INFINITY ? rsqrtf(mean) : __uint_as_float(0x7fc00000u);
+      const float k = -(r * dot) * r * (1.f / DH);  // of x: -r^2 mean(u x)
+      const float2 r2 = make_float2(r, r), k2 = make_float2(k, k);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        g2[i] = tc::mul2(r2, tc::fma2(a2[i], d2, g2[i]));
-        h2[i] = tc::mul2(r2, tc::fma2(b2[i], d2, h2[i]));
+        dw[i] = tc::fma2(g2[i], tc::mul2(a2[i], r2), dw[i]), dw[4 + i] = tc::fma2(h2[i], tc::mul2(b2[i], r2), dw[4 + i]);
+        g2[i] = tc::mul2(r2, tc::fma2(a2[i], k2, u2[i]));
+        h2[i] = tc::mul2(r2, tc::fma2(b2[i], k2, u2[4 + i]));
       }
       if (exists && !(r == r)) report(p.status, JAB_ERR_NONFINITE);
     }
@@ -136,13 +145,12 @@ __global__ void __launch_bounds__(kBackThreads, 2) norm_rope_back_kernel(const _
     *reinterpret_cast<float2*>(&sums[slot][at1 + 2 * i]) = dw[4 + i];
   }
   __syncthreads();
-  if (threadIdx.x < 2 * DH) {
-    const int d = threadIdx.x % DH, first = blockIdx.y * HEADS;
-    const int q_end = min(max(p.n_q - first, 0), HEADS);
-    const int h0 = threadIdx.x < DH ? 0 : q_end, h1 = threadIdx.x < DH ? q_end : HEADS;
+  const int q_end = min(max(p.n_q - (int)blockIdx.y * heads, 0), heads);
+  for (int i = threadIdx.x; i < 2 * DH; i += blockDim.x) {
+    const int d = i % DH, h0 = i < DH ? 0 : q_end, h1 = i < DH ? q_end : heads;
     float v = 0.f;
-    for (int i = h0; i < h1; ++i) v += sums[i][d];
-    p.part[((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 2 * DH + threadIdx.x] = v;
+    for (int h = h0; h < h1; ++h) v += sums[h][d];
+    p.part[((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 2 * DH + i] = v;
   }
 }
 
@@ -195,8 +203,11 @@ __global__ void __launch_bounds__(64) rope_table_kernel(const __grid_constant__ 
 
 template <class T, int DH>
 cudaError_t back_as(const BackParams& p, float* dwq, float* dwk, cudaStream_t st) {
-  constexpr int HEADS = kBackThreads / (DH / 16);
-  const int gy = (p.n_q + p.n_k + HEADS - 1) / HEADS;
+  // as many heads a block as kBackThreads threads take, and as even a share of them as whole warps allow (40 heads of 128 as 32 and
+  // 8: 161 us, as 20 and 20: 131)
+  constexpr int MOST = kBackThreads / (DH / 16), WARP = 32 / (DH / 16);
+  const int heads = p.n_q + p.n_k, blocks = (heads + MOST - 1) / MOST, share = ((heads + blocks - 1) / blocks + WARP - 1) / WARP * WARP;
+  const int gy = (heads + share - 1) / share;
   // four tokens a block and more where the weights' gradients are wanted: every block has a part of them to be added up
   const int64_t at_most = p.part != nullptr ? (p.n_tokens + 3) / 4 : p.n_tokens;
   const int gx = (int)std::min<int64_t>(at_most, std::max(1, kMostParts / gy));
@@ -206,7 +217,7 @@ cudaError_t back_as(const BackParams& p, float* dwq, float* dwk, cudaStream_t st
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.gridDim = dim3(gx, gy);
-    cfg.blockDim = dim3(kBackThreads);
+    cfg.blockDim = dim3(share * (DH / 16));
     cfg.stream = st;
     cfg.attrs = at;
     cfg.numAttrs = 1;
