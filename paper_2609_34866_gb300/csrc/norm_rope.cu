@@ -29,7 +29,7 @@ struct BackParams {
 };
 
 constexpr int kBackThreads = 256;
-constexpr int kMostParts = 608;  // blocks along the tokens times blocks along the heads, where the heads allow it
+constexpr int kMostParts = 1216;  // blocks along the tokens times blocks along the heads, where the heads allow it
 
 // A thread stays with one head's two groups of 8 (as in the writing kernel) and goes over the tokens, so that its share of the
 // weights' gradient is 16 registers. The next token's rows are under way while one is worked on (two ahead: slower, registers).
@@ -202,15 +202,18 @@ __global__ void __launch_bounds__(64) rope_table_kernel(const __grid_constant__ 
 }
 
 template <class T, int DH>
-cudaError_t back_as(const BackParams& p, float* dwq, float* dwk, cudaStream_t st) {
-  // as many heads a block as kBackThreads threads take, and as even a share of them as whole warps allow (40 heads of 128 as 32 and
-  // 8: 161 us, as 20 and 20: 131)
+cudaError_t back_as(const BackParams& p, float* dwq, float* dwk, int sms, cudaStream_t st) {
+  // as many heads a block as kBackThreads threads take, and as even a share of them as whole warps allow (16384 tokens of 40 heads of
+  // 128 as 32 and 8: 161 us, as 20 and 20: 142)
   constexpr int MOST = kBackThreads / (DH / 16), WARP = 32 / (DH / 16);
   const int heads = p.n_q + p.n_k, blocks = (heads + MOST - 1) / MOST, share = ((heads + blocks - 1) / blocks + WARP - 1) / WARP * WARP;
   const int gy = (heads + share - 1) / share;
   // four tokens a block and more where the weights' gradients are wanted: every block has a part of them to be added up
   const int64_t at_most = p.part != nullptr ? (p.n_tokens + 3) / 4 : p.n_tokens;
-  const int gx = (int)std::min<int64_t>(at_most, std::max(1, kMostParts / gy));
+  // and no more blocks than are resident at once (128 registers a thread): all have the same number of tokens, but for one
+  // (three blocks an SM: 108 us, with four 142)
+  const int resident = sms * std::min(16, 65536 / (128 * share * (DH / 16)));
+  const int gx = (int)std::min<int64_t>(at_most, std::max(1, std::min(kMostParts, resident) / gy));
   if (gx > 0) {
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute at[1];
@@ -231,8 +234,8 @@ cudaError_t back_as(const BackParams& p, float* dwq, float* dwk, cudaStream_t st
   return launch_after(weight_sum_kernel, 2 * DH / 8, 256, 0, st, (const float*)p.part, gx * gy, DH, dwq, dwk);
 }
 template <class T>
-cudaError_t back_type(const BackParams& p, int dh, float* dwq, float* dwk, cudaStream_t st) {
-  return dh == 128 ? back_as<T, 128>(p, dwq, dwk, st) : back_as<T, 64>(p, dwq, dwk, st);
+cudaError_t back_type(const BackParams& p, int dh, float* dwq, float* dwk, int sms, cudaStream_t st) {
+  return dh == 128 ? back_as<T, 128>(p, dwq, dwk, sms, st) : back_as<T, 64>(p, dwq, dwk, sms, st);
 }
 
 bool wants_weights(const NormRopeBackArgs& a) { return a.dwq != nullptr || a.dwk != nullptr; }
@@ -246,7 +249,7 @@ size_t norm_rope_scratch(int n_heads, int dh) {
 
 int norm_rope_back_kernels(const NormRopeBackArgs& a) { return (a.n_tokens > 0 ? 1 : 0) + (wants_weights(a) ? 1 : 0); }
 
-cudaError_t launch_norm_rope_back(const NormRopeBackArgs& a, int, cudaStream_t st) {
+cudaError_t launch_norm_rope_back(const NormRopeBackArgs& a, int sms, cudaStream_t st) {
   BackParams p{};
   p.x = a.x, p.dq = a.dq, p.dk = a.dk;
   p.ldx = a.ldx, p.lddq = a.lddq, p.lddk = a.lddk, p.lddx = a.lddx;
@@ -262,9 +265,9 @@ cudaError_t launch_norm_rope_back(const NormRopeBackArgs& a, int, cudaStream_t s
   p.eps = a.how.norm ? a.how.eps : 0.f;
   p.part = wants_weights(a) ? static_cast<float*>(a.ws) : nullptr;
   p.status = a.status;
-  return a.type == JAB_FP16   ? back_type<half_t>(p, a.head_dim, a.dwq, a.dwk, st)
-         : a.type == JAB_BF16 ? back_type<bf16_t>(p, a.head_dim, a.dwq, a.dwk, st)
-                              : back_type<float>(p, a.head_dim, a.dwq, a.dwk, st);
+  return a.type == JAB_FP16   ? back_type<half_t>(p, a.head_dim, a.dwq, a.dwk, sms, st)
+         : a.type == JAB_BF16 ? back_type<bf16_t>(p, a.head_dim, a.dwq, a.dwk, sms, st)
+                              : back_type<float>(p, a.head_dim, a.dwq, a.dwk, sms, st);
 }
 
 cudaError_t launch_rope_table(const RopeTableArgs& a, cudaStream_t st) {

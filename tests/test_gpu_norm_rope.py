@@ -4,7 +4,7 @@ Without a norm the forward is compared bit for bit (its roundings are the defini
 rounded the other way, one in 2^16 or fewer: at most 2 + rows / 2^14 here. Against float64: the factor, two products and the
 rotation's three roundings are 6 of 2^-24 (a factor rounded the other way 7) of |a c| + |b s|, then half a step of the type.
 Gradients, each of at most 32 roundings in a chain (products with r, w, cos and sin, a sum of 16 products and one over 8
-lanes): 2^-19 of the sums of magnitudes; a weight's gradient adds up `per` rows a thread, 32 to 64 heads and 608 / 8 + 8 parts
+lanes): 2^-19 of the sums of magnitudes; a weight's gradient adds up `per` rows a thread, 32 to 64 heads and the blocks' parts
 as pairs: (per + 64 + 8) 2^-24 more."""
 import pytest
 import torch
@@ -240,7 +240,7 @@ def test_backward(n, hq, hk, dh, dt, part, inter, norm):
     assert bool(((dx.double().view_as(x) - x.grad).abs() <= bound).all())
     if norm:
         heads_a_block = 256 // (dh // 16)
-        per = -(-n // max(1, 608 // -(-(hq + hk) // heads_a_block)))
+        per = -(-n // max(1, 304 // -(-(hq + hk) // heads_a_block)))  # (two blocks an SM at least)
         for got, want, sl in ((dwq, ws[0], slice(0, hq)), (dwk, ws[1], slice(hq, None))):
             want = torch.zeros(dh, device="cuda", dtype=torch.float64) if want.grad is None else want.grad
             top = (gm * xn)[:, sl].sum((0, 1))
