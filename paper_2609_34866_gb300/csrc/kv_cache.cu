@@ -134,7 +134,7 @@ __global__ void __launch_bounds__(kWriteThreads, sizeof(T) == 2 ? 2 : 1) kv_writ
     const bool live = placed && row < p.n_heads && (!turn || turnable) && !(is_q && p.q_out == nullptr);
     if (threadIdx.x == 0 && to >= 0 && (!placed || !turnable)) report(p.status, JAB_ERR_INVALID_ARG);
     if constexpr (NORMED) {
-      if (p.eps > 0.f) {
+      if (p.eps > 0.f && __any_sync(0xffffffffu, live && is_k)) {  // (not for warps that have heads of V alone)
         const float r = norm_factor<LANES>(a, b, p.eps);
         if (live && is_k) {
           const float2 *w0 = reinterpret_cast<const float2*>(weights[is_q ? 0 : 1] + at0), *w1 = reinterpret_cast<const float2*>(weights[is_q ? 0 : 1] + at1);
@@ -296,9 +296,22 @@ cudaError_t write_as(const WriteParams& p, int sms, cudaStream_t st) {
   // A block has a token's heads, or as many of them as kWriteThreads threads take. With four tokens for every SM and more, a
   // third of the heads where that leaves no thread idle: it loads a token's angles once for its rows in turn (2048 tokens of 48
   // heads of 128: 19 us for writing and reading, 22 without; but 64 tokens 4.9 instead of 4.5).
+  // With a norm, or without a cache, the smallest share of whole warps from 64 threads on: 16384 tokens of 40 heads of 128 take 76 us
+  // with 64 threads, 84 with 160; of 48 heads into the cache 116 with 64, 119 with 128.
   constexpr int PER_SM = sizeof(T) == 2 ? 768 : 512;
-  const int want = p.n_heads * (DH / 16), parts = want % 96 == 0 ? 3 : MODE != kWrite && want % 64 == 0 ? 2 : 1;
-  const int share = p.n_tokens >= 4 * (int64_t)sms ? want / parts : want;
+  const int want = p.n_heads * (DH / 16);
+  int share = want;
+  if (p.n_tokens >= 4 * (int64_t)sms) {
+    if (MODE == kWrite) {
+      if (want % 96 == 0) share = want / 3;
+    } else {
+      for (int t = 64; t < want; t += 32)
+        if (want % t == 0) {
+          share = t;
+          break;
+        }
+    }
+  }
   const int threads = (std::min(share, kWriteThreads) + 31) / 32 * 32;
   const int64_t blocks = std::min<int64_t>(p.n_tokens, (int64_t)sms * std::min(32, std::max(1, PER_SM / threads)));
   return launch_after(kv_write_kernel<T, DH, BITS, MODE>, (unsigned)blocks, threads, 0, st, p);
