@@ -494,8 +494,8 @@ jab_status jab_rope_table_scaled(int32_t length, int32_t rotary_dim, float theta
 
 /* What is done to the heads of Q and K of a row before they are used: a norm for each head, then the rotation.
  *   norm (norm != 0)    r = 1 / sqrt(mean x^2 + eps) of the head, rounded to fp32 (nearest but for one in 2^16 or fewer), then
- *                       fl32(fl32(x r) w). eps within 1e-30 .. 1e30. A row whose squares leave fp32's range, or with an infinity or a
- *                       NaN, has r = NaN and raises JAB_ERR_NONFINITE.
+ *                       fl32(fl32(x r) w). eps within 1e-30 .. 1e30. A head with an infinity, a NaN or an element of 2^61.5 and more (32 of
+ *                       its squares leave fp32) has r = NaN and raises JAB_ERR_NONFINITE.
  *   q_weight, k_weight  fp32 [head_dim] on the device, 16-byte aligned, or NULL: all 1
  *   rotation            (positions_dev != NULL) elements [0, rotary_dim) of each head by the table rows of the token's position; the
  *                       others stay. Pair j is (j, j + rotary_dim / 2), or (2j, 2j + 1) with interleaved != 0:
@@ -534,7 +534,8 @@ jab_status jab_qk_norm_rope(int64_t n_tokens, int32_t n_q_heads, int32_t n_k_hea
  *   dX_dev            out type, columns [0, (n_q_heads + n_k_heads) * head_dim) of rows of pitch lddx; the others are left as
  *                     they are
  *   dq_weight_dev, dk_weight_dev  out fp32 [head_dim], or NULL: not wanted (both NULL without a norm)
- * X, dQ, dK and dX do not overlap. A token whose position is out of range is reported; its dX is left as it is and it adds
+ * X, dQ, dK and dX do not overlap. A head whose squares' sum is not finite has r = NaN and raises JAB_ERR_NONFINITE. A token whose
+ * position is out of range is reported; its dX is left as it is and it adds
  * nothing to the weights' gradients. Sums run in a fixed order: repeated calls give the same bits. ws 256-byte aligned. */
 size_t jab_qk_norm_rope_backward_workspace_size(int64_t n_tokens, int32_t n_q_heads, int32_t n_k_heads, int32_t head_dim);
 jab_status jab_qk_norm_rope_backward(int64_t n_tokens, int32_t n_q_heads, int32_t n_k_heads, int32_t head_dim,

@@ -707,7 +707,7 @@ def _wide_rows(t, width: int, name: str, rows: int):
     """(pointer, pitch) of rows of `width` contiguous elements and more."""
     if t.dim() != 2 or t.shape[0] != rows or t.shape[1] < width or (t.shape[1] != 1 and t.stride(1) != 1) or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor of {rows} rows of at least {width} contiguous elements")
-    return t.data_ptr(), t.stride(0) if rows > 1 else t.shape[1]
+    return t.data_ptr(), t.stride(0) if rows > 1 else width
 
 
 def jab_qk_norm_rope(x, n_q_heads: int, n_k_heads: int, head_dim: int, q, k, positions=None, rope=None,

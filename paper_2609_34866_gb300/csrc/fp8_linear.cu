@@ -3,13 +3,20 @@
 //   y[m, n] = sum_b sx[m, b] sw[n / block_rows, b] sum_{k in block b} qx[m, k] qw[n, k]
 //
 // A block's sum is an accumulator of its own: four products of K = 32, then it is read out of tensor memory, multiplied by its
-// scales and added to running sums in registers, while the next block's products fill another accumulator. The output
-// channels are the accumulator's 128 lanes and the tokens its columns, so that one layout serves one token and thousands: a
-// lane's channel has its own scale (block_rows = 1), a column's token another, which every lane reads from shared memory.
+// scales and added to running sums in registers, while the next block's products fill another accumulator.
 //
-// Roles of a block: a warp that issues the copies (TMA, weights and token codes in one ring), a warp that issues the
-// products, eight warps that read out, scale and add up. Many tiles: persistent blocks. Few tiles: one a cluster, whose
-// blocks take ranges of K and add their sums through shared memory in a fixed order.
+// Up to 128 tokens a tile, the output channels on the accumulator's 128 lanes and the tokens on its columns, so that one layout
+// serves one token and many: a lane's channel has its own scale (block_rows = 1), a column's token another, which every lane
+// reads from shared memory. Roles of a block: a warp that issues the copies (TMA, weights and token codes in one ring), two that
+// issue the products of every other block of K (an issue with its waits is 400 clocks: one warp held 16 tokens up), one that
+// brings the scales, eight that read out, scale and add up. Many tiles: persistent blocks. Few tiles: one a cluster, whose blocks
+// take ranges of K and add their sums through shared memory in a fixed order. Many tokens: pairs of blocks, further down.
+//
+// Bound: 8192 tokens x 6144 x 4096 with scales for 128 x 128 weights take 256 us, 21 of them for the tokens' codes: 1.61 PFLOP/s, 0.81
+// of the tensor cores' measured bf16 rate; with a scale for every row's 128 336 us (two operations an element in the read-out, 1660
+// clocks a block of K). One token (25 MB of codes) takes 9.3 us where the bytes take 3.8: two launches, the copies' latency and
+// eleven stages' products and read-outs. (Codes of up to 16 tokens made in the product's own kernel: no faster there, and 5.8 us
+// instead of 5.0 for 1 x 2304 x 768, as the weights' copies cannot begin before the launch before has ended.)
 #include <cudaTypedefs.h>
 
 #include <algorithm>
@@ -381,13 +388,16 @@ __global__ void __launch_bounds__(Cfg<NTOK>::THREADS, 1)
 // would read every token's scale from shared memory, a pass of its own each (8 warps x 128 columns: 1000 clocks for a block of
 // K whose products take 512). With block_rows = 128 a lane has one factor for a block of K; with block_rows = 1 tensor memory is
 // read in the shape that gives a thread two of eight columns, whose scales are 32 passes a warp.
+// Bound: a block of K takes 1130 clocks. Its products take 820 behind one another; with two accumulators of 256 columns (all of
+// tensor memory) one is free again 500 clocks for the barrier of its last product, 450 for the read-out and 400 for the arrival and
+// the next issue after that.
 struct PairCfg {
   static constexpr int ST = 6, STAGE = 2 * TM * BK, THREADS = 384, DST = 2, COLS = 256;
   static constexpr int EPI_REGS = 216, OTHER_REGS = 72;
   static constexpr int SMEM = ST * STAGE + 1024 + 1024 + SST * COLS * 4;
   static_assert(128 * OTHER_REGS + 256 * EPI_REGS <= THREADS * (65536 / THREADS / 8 * 8), "registers");
 };
-constexpr int AHEAD = 4;  // blocks of K that a lane's factors come ahead (two of the weights' blocks in the channel scales)
+constexpr int AHEAD = 4;  // blocks of K that a lane's factors come ahead
 
 // Eight neighbours of a row, or four fp32, in one store.
 __device__ __forceinline__ void store8(void* y, int64_t at, const float2 (&v)[4], int type) {
@@ -598,8 +608,8 @@ __global__ void __launch_bounds__(PairCfg::THREADS, 1)
           }
         }
       } else {
-        // acc[(32 chunk + 4 n + 2 upper + tokens of the second sixteen ...)]: see `at` below
-        float fx[4], nx[4];  // of the thread's four tokens: 16 q + 8 j + lane / 4
+        // acc[4 c + t]: channels n0 + 8 c + 2 (lane % 4) and the next of token m0 + 8 t + lane / 4
+        float fx[4], nx[4];  // of the thread's four tokens
         const int64_t m1 = m0 + (lane >> 2);
         auto fetch = [&](int kb) {
 #pragma unroll

@@ -3,6 +3,8 @@
 //
 //   y = R n, n = (x r) w, r = (mean x^2 + eps)^(-1/2):   g = R^T dy, u = g w,
 //   dx = r (u - x r mean(u x r)),  dw = sum over tokens and heads of g x r
+//
+// Bound: bytes in flight and instructions; 16384 tokens of 40 heads of 128 in bf16 (503 MB) take 108 us, 4.7 TB/s, without a norm 91.
 #include <math.h>
 
 #include <algorithm>

@@ -140,6 +140,19 @@ def test_linear(M, N, K, xt, yt, rows, kind):
     assert J.jab_get_device_status() == 0
 
 
+@pytest.mark.parametrize("M,N,K", [(5, 25000, 272), (20, 21000, 144), (40, 25003, 272), (100, 30000, 400), (2600, 5003, 400), (4000, 4010, 16), (2700, 4872, 528),
+                                   (2, 130, 131072), (130, 200, 65552)])
+@pytest.mark.parametrize("yt,rows", [(BF, 128), (F, 1)])
+def test_linear_many_tiles_for_a_block_and_long_sums(M, N, K, yt, rows):
+    """More tiles than blocks at every tile size, odd numbers of channels, a single block of K, and the longest K."""
+    g = _gen(M + N + K)
+    x = (torch.randn((M, K), generator=g, device="cuda") * 0.05).to(HF)
+    codes, scales = _weights(N, K, rows, g)
+    y = _linear(x, codes, scales, rows, yt)
+    _held(y, x, codes, scales, rows)
+    assert torch.equal(y, _linear(x, codes, scales, rows, yt)) and J.jab_get_device_status() == 0
+
+
 @pytest.mark.parametrize("M", [5, 40, 200, 1000])
 @pytest.mark.parametrize("yt", [BF, F])
 def test_linear_pitches_and_margins(M, yt):

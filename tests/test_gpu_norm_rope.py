@@ -61,7 +61,7 @@ def _same_rows(got, want, norm):
     assert off <= (2 + got.shape[0] // 2 ** 14 if norm else 0), off
 
 
-CASES = [(1, 1, 1, 64), (1, 32, 8, 128), (3, 12, 12, 64), (64, 32, 8, 128), (37, 4, 1, 64), (1001, 12, 4, 128), (700, 5, 0, 64), (5, 0, 3, 128), (130, 96, 8, 128)]
+CASES = [(1, 1, 1, 64), (1, 32, 8, 128), (3, 12, 12, 64), (64, 32, 8, 128), (37, 4, 1, 64), (1001, 12, 4, 128), (700, 5, 0, 64), (5, 0, 3, 128), (130, 96, 8, 128), (20, 300, 56, 64)]
 
 
 @pytest.mark.parametrize("n,hq,hk,dh", CASES)
