@@ -12,8 +12,8 @@
 // brings the scales, eight that read out, scale and add up. Many tiles: persistent blocks. Few tiles: one a cluster, whose blocks
 // take ranges of K and add their sums through shared memory in a fixed order. Many tokens: pairs of blocks, further down.
 //
-// Bound: 8192 tokens x 6144 x 4096 with scales for 128 x 128 weights take 256 us, 21 of them for the tokens' codes: 1.61 PFLOP/s, 0.81
-// of the tensor cores' measured bf16 rate; with a scale for every row's 128 336 us (two operations an element in the read-out, 1660
+// Bound: 8192 tokens x 6144 x 4096 with scales for 128 x 128 weights take 238 us, 21 of them for the tokens' codes: 1.73 PFLOP/s, 0.87
+// of the tensor cores' measured bf16 rate; with a scale for every row's 128 321 us (two operations an element in the read-out, 1660
 // clocks a block of K). One token (25 MB of codes) takes 9.3 us where the bytes take 3.8: two launches, the copies' latency and
 // eleven stages' products and read-outs. (Codes of up to 16 tokens made in the product's own kernel: no faster there, and 5.8 us
 // instead of 5.0 for 1 x 2304 x 768, as the weights' copies cannot begin before the launch before has ended.)
@@ -390,23 +390,27 @@ __global__ void __launch_bounds__(Cfg<NTOK>::THREADS, 1)
 // read in the shape that gives a thread two of eight columns, whose scales are 32 passes a warp.
 // Bound: a block of K takes 1130 clocks. Its products take 820 behind one another; with two accumulators of 256 columns (all of
 // tensor memory) one is free again 500 clocks for the barrier of its last product, 450 for the read-out and 400 for the arrival and
-// the next issue after that.
+// the next issue after that. Three accumulators of 160 columns (263 us where this took 256) and one block a tile (277) were no faster:
+// a pair's products take 1300 clocks from issue to the barrier however short they are, a block's own 48 KB a stage 950.
 struct PairCfg {
-  static constexpr int ST = 6, STAGE = 2 * TM * BK, THREADS = 384, DST = 2, COLS = 256;
+  static constexpr int ST = 5, STAGE = 2 * TM * BK, THREADS = 384, DST = 2, COLS = 256;
+  static constexpr int OUT = 32 * 128;  // a warp's place for 128 bytes of 32 rows on their way out
   static constexpr int EPI_REGS = 216, OTHER_REGS = 72;
-  static constexpr int SMEM = ST * STAGE + 1024 + 1024 + SST * COLS * 4;
+  static constexpr int SMEM = ST * STAGE + 1024 + 1024 + SST * COLS * 4 + 8 * OUT;
   static_assert(128 * OTHER_REGS + 256 * EPI_REGS <= THREADS * (65536 / THREADS / 8 * 8), "registers");
 };
 constexpr int AHEAD = 4;  // blocks of K that a lane's factors come ahead
 
-// Eight neighbours of a row, or four fp32, in one store.
-__device__ __forceinline__ void store8(void* y, int64_t at, const float2 (&v)[4], int type) {
-  if (type == JAB_FP32) {
-    float4* to = reinterpret_cast<float4*>(static_cast<float*>(y) + at);
-    to[0] = make_float4(v[0].x, v[0].y, v[1].x, v[1].y), to[1] = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
-  } else {
-    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(y) + at) =
-        make_uint4(pair_of(v[0].x, v[0].y, type), pair_of(v[1].x, v[1].y, type), pair_of(v[2].x, v[2].y, type), pair_of(v[3].x, v[3].y, type));
+// 32 rows of 128 bytes from a warp's place (16-byte chunk c of row r at c ^ (r & 7)) to rows of `pitch` bytes: four rows a store, where
+// lanes that store from their own rows touch 32 lines at a time (4000 clocks a tile: 256 us where this takes 238). `rows` of them are there.
+template <class Inside>
+__device__ __forceinline__ void rows_out(const uint8_t* place, uint8_t* y, int64_t pitch, int rows, int lane, Inside inside) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int r = 4 * i + (lane >> 3), c = lane & 7;
+    const uint4 v = *reinterpret_cast<const uint4*>(place + r * 128 + ((c ^ (r & 7)) << 4));
+    uint8_t* to = y + r * pitch + 16 * c;
+    if (r < rows && inside(to)) *reinterpret_cast<uint4*>(to) = v;
   }
 }
 
@@ -531,8 +535,10 @@ __global__ void __launch_bounds__(PairCfg::THREADS, 1)
     more_registers<C::EPI_REGS>();
     const int quarter = warp & 3, first = warp < 8 ? 0 : COLS / 2;
     const bool wide = ((p.y_type == JAB_FP32 ? p.ldy % 4 : p.ldy % 8) | (int64_t)(reinterpret_cast<uintptr_t>(p.y) & 15)) == 0;
-    const bool words = p.ldy % 2 == 0 && (reinterpret_cast<uintptr_t>(p.y) & (p.y_type == JAB_FP32 ? 7 : 3)) == 0;
     auto inside = [&](int64_t last) { return in_bounds(last, (p.M - 1) * p.ldy + p.N, p.status); };
+    uint8_t* place = smem + ST * C::STAGE + 1024 + SST * COLS * 4 + (warp - 4) * C::OUT;
+    const int size = p.y_type == JAB_FP32 ? 4 : 2;
+    auto chunk_inside = [&](const uint8_t* to) { return inside((to - static_cast<const uint8_t*>(p.y)) / size + 16 / size - 1); };
     auto read = [&](int d) {  // the accumulator may be written again
       tc::fence_before_sync();
       __syncwarp();
@@ -593,19 +599,41 @@ __global__ void __launch_bounds__(PairCfg::THREADS, 1)
           }
         }
         if (!ok) break;
-        const int64_t m = m0 + lane, at = m * p.ldy + n0;
-        if (m < p.M) {
-          if (wide && n0 + COLS / 2 <= p.N && inside(at + COLS / 2 - 1)) {
+        if (wide && n0 + COLS / 2 <= p.N) {
+          uint8_t* y = static_cast<uint8_t*>(p.y) + (m0 * p.ldy + n0) * size;
+          const int rows = (int)max((int64_t)0, min((int64_t)32, p.M - m0));
+          auto put16 = [&](int c, const uint4& v) { *reinterpret_cast<uint4*>(place + lane * 128 + ((c ^ (lane & 7)) << 4)) = v; };
+          if (size == 4) {
 #pragma unroll
-            for (int c = 0; c < COLS / 4; c += 4) {
-              const float2 v[4] = {acc[c], acc[c + 1], acc[c + 2], acc[c + 3]};
-              store8(p.y, at + 2 * c, v, p.y_type);
+            for (int h = 0; h < 4; ++h) {
+              __syncwarp();
+#pragma unroll
+              for (int c = 0; c < 8; ++c) {
+                const float2 u = acc[16 * h + 2 * c], v = acc[16 * h + 2 * c + 1];
+                put16(c, make_uint4(__float_as_uint(u.x), __float_as_uint(u.y), __float_as_uint(v.x), __float_as_uint(v.y)));
+              }
+              __syncwarp();
+              rows_out(place, y + 128 * h, p.ldy * size, rows, lane, chunk_inside);
             }
           } else {
 #pragma unroll
-            for (int c = 0; c < COLS / 2; ++c)
-              if (n0 + c < p.N && inside(at + c)) put(p.y, at + c, c & 1 ? acc[c / 2].y : acc[c / 2].x, p.y_type);
+            for (int h = 0; h < 2; ++h) {
+              __syncwarp();
+#pragma unroll
+              for (int c = 0; c < 8; ++c) {
+                const float2* v = acc + 32 * h + 4 * c;
+                put16(c, make_uint4(pair_of(v[0].x, v[0].y, p.y_type), pair_of(v[1].x, v[1].y, p.y_type), pair_of(v[2].x, v[2].y, p.y_type),
+                                    pair_of(v[3].x, v[3].y, p.y_type)));
+              }
+              __syncwarp();
+              rows_out(place, y + 128 * h, p.ldy * size, rows, lane, chunk_inside);
+            }
           }
+        } else if (m0 + lane < p.M) {
+          const int64_t at = (m0 + lane) * p.ldy + n0;
+#pragma unroll
+          for (int c = 0; c < COLS / 2; ++c)
+            if (n0 + c < p.N && inside(at + c)) put(p.y, at + c, c & 1 ? acc[c / 2].y : acc[c / 2].x, p.y_type);
         }
       } else {
         // acc[4 c + t]: channels n0 + 8 c + 2 (lane % 4) and the next of token m0 + 8 t + lane / 4
@@ -653,22 +681,49 @@ __global__ void __launch_bounds__(PairCfg::THREADS, 1)
           if (lane == 0) tc::mbar_arrive(&bars->sempty[s]);
         }
         if (!ok) break;
+        if (wide && n0 + COLS / 2 <= p.N) {
+          uint8_t* y = static_cast<uint8_t*>(p.y) + (m0 * p.ldy + n0) * size;
+          const int rows = (int)max((int64_t)0, min((int64_t)32, p.M - m0));
+          if (size == 4) {
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const int64_t m = m1 + 8 * t;
-          if (m >= p.M) continue;
+            for (int h = 0; h < 4; ++h) {
+              __syncwarp();
 #pragma unroll
-          for (int c = 0; c < 16; ++c) {
-            const int n = n0 + 8 * c + 2 * (lane & 3);
-            const int64_t at = m * p.ldy + n;
-            const float2 v = acc[4 * c + t];
-            if (n + 1 < p.N && words) {
-              if (!inside(at + 1)) continue;
-              if (p.y_type == JAB_FP32)
-                *reinterpret_cast<float2*>(static_cast<float*>(p.y) + at) = v;
-              else
-                *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.y) + at) = pair_of(v.x, v.y, p.y_type);
-            } else {
+              for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                  const int r = 8 * t + (lane >> 2), at = r * 128 + (((2 * c + ((lane & 3) >> 1)) ^ (r & 7)) << 4) + 8 * (lane & 1);
+                  *reinterpret_cast<float2*>(place + at) = acc[4 * (4 * h + c) + t];
+                }
+              __syncwarp();
+              rows_out(place, y + 128 * h, p.ldy * size, rows, lane, chunk_inside);
+            }
+          } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              __syncwarp();
+#pragma unroll
+              for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                  const int r = 8 * t + (lane >> 2), at = r * 128 + ((c ^ (r & 7)) << 4) + 4 * (lane & 3);
+                  const float2 v = acc[4 * (8 * h + c) + t];
+                  *reinterpret_cast<uint32_t*>(place + at) = pair_of(v.x, v.y, p.y_type);
+                }
+              __syncwarp();
+              rows_out(place, y + 128 * h, p.ldy * size, rows, lane, chunk_inside);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            const int64_t m = m1 + 8 * t;
+            if (m >= p.M) continue;
+#pragma unroll
+            for (int c = 0; c < 16; ++c) {
+              const int n = n0 + 8 * c + 2 * (lane & 3);
+              const int64_t at = m * p.ldy + n;
+              const float2 v = acc[4 * c + t];
               if (n < p.N && inside(at)) put(p.y, at, v.x, p.y_type);
               if (n + 1 < p.N && inside(at + 1)) put(p.y, at + 1, v.y, p.y_type);
             }
@@ -711,8 +766,8 @@ bool make_map(CUtensorMap* m, const void* base, uint64_t K, uint64_t outer, uint
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Tokens of a tile: the smallest that holds them all; past 128 the pairs' 256 where their rounds, each as long as 1.7 of the others'
-// (1130 and 660 clocks a block of K), take less (512 x 6144 x 4096: 32 us, else 36; 1024: 57 and 52; 2048: 78 and 91).
+// Tokens of a tile: the smallest that holds them all; past 128 the pairs' 256 where their rounds, each as long as 1.6 of the others',
+// take less (768 x 6144 x 4096: 28 us, else 33; 1024: 47.3 and 46.7; 2048: 70 and 89).
 int tile_tokens(int64_t M, int N, int sms) {
   if (M <= 16) return 16;
   if (M <= 32) return 32;
@@ -721,7 +776,7 @@ int tile_tokens(int64_t M, int N, int sms) {
   const int64_t pairs = std::max(sms / 2, 1);
   const int64_t wide = ((M + 255) / 256 * ((N + 255) / 256) + pairs - 1) / pairs;
   const int64_t narrow = ((M + 127) / 128 * ((N + 127) / 128) + sms - 1) / sms;
-  return 17 * wide < 10 * narrow ? 256 : 128;
+  return 16 * wide < 10 * narrow ? 256 : 128;
 }
 
 struct Scratch {
