@@ -657,12 +657,13 @@ def jab_rope_table_scaled(cos, sin, theta: float, kind: str = "plain", factor: f
 def _norm_rope(n: int, dh: int, positions, rope, interleaved, norm_eps, q_weight, k_weight) -> _NormRope:
     qw = kw = pos = cos = sin = None
     length = half = 0
+    f32 = torch.float32
     if norm_eps is not None:
         shape = (dh,)
         if q_weight is not None:
-            qw = _shaped(q_weight, shape, torch.float32, "q_weight")
+            qw = _shaped(q_weight, shape, f32, "q_weight")
         if k_weight is not None:
-            kw = _shaped(k_weight, shape, torch.float32, "k_weight")
+            kw = _shaped(k_weight, shape, f32, "k_weight")
     elif q_weight is not None or k_weight is not None:
         raise ValueError("weights of a norm need norm_eps")
     if rope is not None:
@@ -671,7 +672,7 @@ def _norm_rope(n: int, dh: int, positions, rope, interleaved, norm_eps, q_weight
         cos_t, sin_t = rope
         shape = cos_t.shape
         length, half = shape
-        cos, sin = _shaped(cos_t, shape, torch.float32, "rope"), _shaped(sin_t, shape, torch.float32, "rope")
+        cos, sin = _shaped(cos_t, shape, f32, "rope"), _shaped(sin_t, shape, f32, "rope")
         pos = _shaped(positions, (n,), torch.int32, "positions")
     return _NormRope(norm_eps is not None, norm_eps or 0.0, qw, kw, pos, cos, sin, length, 2 * half, bool(interleaved))
 
@@ -698,16 +699,19 @@ def _heads(t, n: int, heads: int, dh: int, like, name: str):
     """(pointer, pitch) of rows of `heads` heads; no such heads: (None, 0)."""
     if heads == 0:
         return None, 0
-    if t.dtype != like.dtype:
+    if t.dtype is not like.dtype:
         raise ValueError(f"{name} must have x's type")
     return _rows(t, heads * dh, name, n)
 
 
 def _wide_rows(t, width: int, name: str, rows: int):
     """(pointer, pitch) of rows of `width` contiguous elements and more."""
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] < width or (t.shape[1] != 1 and t.stride(1) != 1) or not t.is_cuda:
-        raise ValueError(f"{name} must be a CUDA tensor of {rows} rows of at least {width} contiguous elements")
-    return t.data_ptr(), t.stride(0) if rows > 1 else width
+    shape = t.shape
+    if len(shape) == 2 and shape[0] == rows and shape[1] >= width and t.is_cuda:
+        pitch, step = t.stride()
+        if step == 1:
+            return t.data_ptr(), pitch if rows > 1 else width
+    raise ValueError(f"{name} must be a CUDA tensor of {rows} rows of at least {width} contiguous elements")
 
 
 def jab_qk_norm_rope(x, n_q_heads: int, n_k_heads: int, head_dim: int, q, k, positions=None, rope=None,
@@ -739,14 +743,15 @@ def jab_qk_norm_rope_backward(x, n_q_heads: int, n_k_heads: int, head_dim: int, 
     width = (n_q_heads + n_k_heads) * head_dim
     xp, ldx = _wide_rows(x, width, "x", n)
     dxp, lddx = _wide_rows(dx, width, "dx", n)
-    if dx.dtype != x.dtype:
+    if dx.dtype is not x.dtype:
         raise ValueError("dx must have x's type")
     qp, ldq = _heads(dq, n, n_q_heads, head_dim, x, "dq")
     kp, ldk = _heads(dk, n, n_k_heads, head_dim, x, "dk")
     how = _norm_rope(n, head_dim, positions, rope, interleaved, norm_eps, q_weight, k_weight)
-    dw = [None if w is None else _shaped(w, (head_dim,), torch.float32, "dq_weight and dk_weight") for w in (dq_weight, dk_weight)]
+    wq = None if dq_weight is None else _shaped(dq_weight, (head_dim,), torch.float32, "dq_weight")
+    wk = None if dk_weight is None else _shaped(dk_weight, (head_dim,), torch.float32, "dk_weight")
     st = lib().jab_qk_norm_rope_backward(n, int(n_q_heads), int(n_k_heads), int(head_dim), xp, _dtype(x, "x"), ldx,
-                                         ctypes.byref(how), qp, ldq, kp, ldk, dxp, lddx, *dw, _ptr(ws, torch.uint8, "ws"),
+                                         ctypes.byref(how), qp, ldq, kp, ldk, dxp, lddx, wq, wk, _ptr(ws, torch.uint8, "ws"),
                                          0 if ws is None else ws.numel(), _stream(stream))
     _check(st, "jab_qk_norm_rope_backward")
 
