@@ -522,7 +522,8 @@ jab_status jab_kv_write_norm_rope(const jab_kv_cache* cache, int64_t n_tokens, i
  *                 lies behind them (V) is not read
  *   Q_dev, K_dev  out type [n_tokens, n_q_heads * head_dim] and [n_tokens, n_k_heads * head_dim], pitches ldq, ldk; they may be the
  *                 places of Q and K in X themselves. NULL where there are no such heads
- * A token whose position is out of range is reported (JAB_ERR_INVALID_ARG) and its outputs are left as they are.
+ * A token whose position is out of range is reported (JAB_ERR_INVALID_ARG) and its outputs are left as they are. Outputs in
+ * fp16 that do not fit raise JAB_ERR_RANGE (dX of the gradient too).
  * head_dim 64 or 128; n_q_heads + n_k_heads up to 4096. */
 jab_status jab_qk_norm_rope(int64_t n_tokens, int32_t n_q_heads, int32_t n_k_heads, int32_t head_dim, const void* X_dev,
                             jab_dtype type, int64_t ldx, const jab_norm_rope* how, void* Q_dev, int64_t ldq, void* K_dev,

@@ -80,9 +80,10 @@ __global__ void __launch_bounds__(kBackThreads, 2) norm_rope_back_kernel(const _
       load8(p.sin_t + (int64_t)pos * (p.rotary / 2) + 8 * t, s);
     }
     fetch(token + gridDim.x);
+    if (!fine) continue;  // (the whole block has this token)
     // (packed pairs halve the instructions; no rounding here is part of a definition)
     float2 *a2 = reinterpret_cast<float2*>(a), *b2 = reinterpret_cast<float2*>(b), *g2 = reinterpret_cast<float2*>(g), *h2 = reinterpret_cast<float2*>(h);
-    if (turns && fine) {
+    if (turns) {
       if (p.neighbours) {
         auto back = [](float& y, float& z, float cs, float sn) {
           const float da = y * cs + z * sn, db = z * cs - y * sn;
@@ -103,10 +104,6 @@ __global__ void __launch_bounds__(kBackThreads, 2) norm_rope_back_kernel(const _
     if (p.eps > 0.f) {
       // r to a few ulp does here: the two sums of a row go through the lanes together
       float2 sq2 = make_float2(0.f, 0.f), dot2 = make_float2(0.f, 0.f);
-      if (!fine) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) g2[i] = h2[i] = make_float2(0.f, 0.f);
-      }
       float2 u2[8];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -132,7 +129,13 @@ __global__ void __launch_bounds__(kBackThreads, 2) norm_rope_back_kernel(const _
       }
       if (exists && !(r == r)) report(p.status, JAB_ERR_NONFINITE);
     }
-    if (exists && fine) {
+    if (exists) {
+      if constexpr (std::is_same<T, half_t>::value) {  // finite, but not in fp16: from halfway past its largest on
+        float big = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) big = largest(big, g[i], h[i]);
+        if (!(big < 65520.f)) report(p.status, JAB_ERR_RANGE);
+      }
       const int64_t at = token * p.lddx + (int64_t)head * DH;
       if (in_bounds(at + max(at0, at1) + 7, (p.n_tokens - 1) * p.lddx + (int64_t)(p.n_q + p.n_k) * DH, p.status)) {
         store(static_cast<T*>(p.dx) + at + at0, g);

@@ -148,6 +148,10 @@ def test_norm_nonfinite_and_positions_out_of_range():
     J.jab_qk_norm_rope_backward(s["x"], 1, 1, 64, dy, dy, dx, ws, dq_weight=dw, **_how(s, False))
     assert (dx == 5).all(1).cpu().tolist() == [False, False, True, True, True, False]
     assert J.jab_get_device_status() == 1
+    s["x"][3] = float("nan")  # whatever such a token holds
+    with_nan = torch.zeros_like(dw)
+    J.jab_qk_norm_rope_backward(s["x"], 1, 1, 64, dy, dy, dx, ws, dq_weight=with_nan, **_how(s, False))
+    assert torch.equal(with_nan, dw) and J.jab_get_device_status() == 1
     keep = torch.tensor([0, 1, 5], device="cuda")
     t = dict(s, x=s["x"][keep].contiguous(), pos=s["pos"][keep].contiguous())
     only = torch.zeros_like(dw)
@@ -273,6 +277,17 @@ def test_backward_against_differences():
     u = v[0, 0]
     for got, a, b in ((dwq, (wq + h * u, wk), (wq - h * u, wk)), (dwk, (wq, wk + h * u), (wq, wk - h * u))):
         assert abs((f(x, *a) - f(x, *b)) / (2 * h) - (got.double() * u).sum().item()) <= 2.0 ** -16 * (got.double() * u).abs().sum().item()
+
+
+def test_results_that_do_not_fit_fp16():
+    x = torch.randn((9, 128), generator=_gen(5), device="cuda").to(HF)
+    big, q, k = torch.full((64,), 1e6, device="cuda"), torch.empty((9, 64), dtype=HF, device="cuda"), torch.empty((9, 64), dtype=HF, device="cuda")
+    J.jab_qk_norm_rope(x, 1, 1, 64, q, k, norm_eps=1e-6, k_weight=big)
+    assert J.jab_get_device_status() == 5
+    J.jab_qk_norm_rope_backward(x, 1, 1, 64, torch.ones_like(q), torch.ones_like(k) + k.sign(), torch.empty_like(x), norm_eps=1e-6, q_weight=big)
+    assert J.jab_get_device_status() == 5
+    J.jab_qk_norm_rope_backward(x, 1, 1, 64, torch.ones_like(q), torch.ones_like(k), torch.empty_like(x), norm_eps=1e-6)
+    assert J.jab_get_device_status() == 0
 
 
 def test_backward_of_no_tokens():
