@@ -226,6 +226,25 @@ def test_linear_in_a_graph_and_on_another_stream():
     assert torch.equal(y2, y)
 
 
+@pytest.mark.parametrize("M", [3, 100, 700])
+def test_linear_two_calls_at_once(M):
+    """Two streams, buffers of their own: the values of one call after the other."""
+    N, K = 2048, 1040
+    sets = []
+    for i in range(2):
+        g = _gen(M + i)
+        x = torch.randn((M, K), generator=g, device="cuda").to(BF)
+        sets.append((x, *_weights(N, K, 128 if i else 1, g), torch.empty((M, N), dtype=BF, device="cuda"),
+                     torch.empty(J.jab_fp8_linear_workspace_size(M, N, K), dtype=torch.uint8, device="cuda"), torch.cuda.Stream(), 128 if i else 1))
+    want = [_linear(s[0], s[1], s[2], s[6], BF) for s in sets]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for x, codes, scales, y, ws, st, rows in sets:
+            J.jab_fp8_linear(x, codes, scales, y, ws, block_rows=rows, stream=st)
+    torch.cuda.synchronize()
+    assert all(torch.equal(s[3], w) for s, w in zip(sets, want)) and J.jab_get_device_status() == 0
+
+
 def test_linear_without_rows_and_refusals():
     codes, scales = _weights(128, 256, 128, _gen(1))
     ws = torch.empty(J.jab_fp8_linear_workspace_size(4, 128, 256), dtype=torch.uint8, device="cuda")

@@ -149,6 +149,42 @@ def test_page_numbers_outside_the_cache():
     assert po.tolist() == list(range(20, 32)) + list(range(20, 34)) and qs.tolist() == [0, 12, 26]
 
 
+def test_long_prompts_in_a_graph():
+    """Release and plan in place with more rows than one launch writes, captured once and replayed with other counts, until the pages
+    run out: that call changes nothing, and the one after a release goes on."""
+    B, page, rows = 40, 16, 12000
+    s = State([0] * B, 200, page, 2, spare=1500)
+    dl, dp, df, dn = s.device()
+    ended, counts = _i32([0] * B), _i32([0] * B)
+    qs, sl, po = _i32([0] * (B + 1)), torch.empty(rows, dtype=torch.int64, device="cuda"), _i32([0] * rows)
+
+    def step():
+        J.jab_kv_release(s.cache, dl, ended, dp, df, dn)
+        J.jab_kv_plan(s.cache, dl, counts, dp, df, dn, qs, sl, po)
+
+    step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    lens, pages, free, n = s.lens, s.pages, s.free, s.n_free
+    rng = random.Random(3)
+    refused = 0
+    for t in range(6):
+        e, c = [int(t == 4 and b % 2 == 0) for b in range(B)], [rng.randint(0, 300) for _ in range(B)]
+        ended.copy_(_i32(e)), counts.copy_(_i32(c))
+        graph.replay()
+        lens, free, n = R.release(lens, e, pages, free, n, page, 0)
+        if sum(-(-(l + k) // page) - -(-l // page) for l, k in zip(lens, c)) > n:
+            refused += 1
+            assert J.jab_get_device_status() == 1 and not qs.any() and bool((sl == -1).all())
+        else:
+            lens, pages, n, start, slots, positions = R.plan(lens, c, pages, free, n, page, rows)
+            assert J.jab_get_device_status() == 0
+            assert qs.tolist() == start and sl.tolist() == slots and po.tolist() == positions
+        assert dl.tolist() == lens and dp.tolist() == pages and dn.tolist() == [n] and df.tolist()[:n] == free[:n]
+    assert refused
+
+
 # ------------------------------------------------------------------ together
 @pytest.mark.parametrize("bits", [8, 4])
 def test_steps_of_a_server(bits):
