@@ -443,8 +443,8 @@ jab_status jab_kv_attention(const jab_kv_cache* cache, int32_t n_seqs, int64_t n
 /* Weights, or any rows, in 8-bit floating point (e4m3: 4 significant bits, 448 at most) with an fp32 scale for every block
  * of block_rows rows (1 or 128) x 128 columns; the last blocks of either may be shorter:
  *     s = fl32(max|x| / 448),  code = e4m3(fl32(x / s)), rounded to nearest even, at most 448 in magnitude
- * A block of zeros has s = 0 and codes 0. One with an infinity or a NaN has s = NaN and codes 0, and raises
- * JAB_ERR_NONFINITE on the device.
+ * A zero keeps its sign (-0 has code 0x80), and so does what rounds to zero. A block of zeros has s = 0 and codes 0. One with an
+ * infinity or a NaN has s = NaN and codes 0, and raises JAB_ERR_NONFINITE on the device.
  *   X_dev       type [M, K], pitch ldx
  *   codes_dev   out e4m3 bytes [M, K], 16-byte aligned
  *   scales_dev  out fp32 [ceil(M / block_rows), ceil(K / 128)]

@@ -83,6 +83,29 @@ def test_quantize_scales_of_any_size(dt, top):
         assert torch.equal(scales, s) and torch.equal(codes.float().double(), want)
 
 
+@pytest.mark.parametrize("dt", [BF, HF, F])
+@pytest.mark.parametrize("rows", [1, 128])
+@pytest.mark.parametrize("exponent", [0, -14, 70, -90])
+def test_quantize_signs_of_zeros(dt, rows, exponent):
+    """The bytes themselves: zeros of both signs, and numbers of both signs that round to zero, beside scales that are divided by and scales
+    whose reciprocal is taken."""
+    if dt == HF and exponent not in (0, -14):
+        pytest.skip("not in fp16")
+    x = torch.randn((130, 400), generator=_gen(6), device="cuda").clamp(-1, 1)
+    x[:, 1::4], x[:, 2::8], x[:, 6::8] = -0.0, 0.0, -(2.0 ** -20)
+    x[:, 7::8] = 2.0 ** -20
+    x[:, ::128] = 1.0
+    x[3], x[4] = -0.0, 0.0
+    x = (x * 2.0 ** exponent).to(dt)
+    codes, scales = _quantize(x, rows)
+    want, s = R.fp8(x.float(), rows)
+    minus = torch.signbit(x.float()) & (R.spread(s, rows, *x.shape) > 0)
+    top = torch.arange(127, dtype=torch.uint8, device="cuda")
+    magnitude = torch.searchsorted(top.view(F8).double(), want.abs())  # (the numbers of codes 0 .. 126 in their order)
+    assert torch.equal(codes.view(torch.uint8).long(), magnitude + 128 * minus) and torch.equal(scales, s)
+    assert bool((codes.view(torch.uint8) == 0x80).any()) and J.jab_get_device_status() == 0
+
+
 def test_quantize_nonfinite():
     x = torch.randn((300, 384), generator=_gen(4), device="cuda")
     x[5, 200], x[290, 0] = float("inf"), float("nan")
