@@ -562,9 +562,11 @@ jab_status jab_qk_norm_rope_backward(int64_t n_tokens, int32_t n_q_heads, int32_
  *   n_free_dev, new_free_dev  int32 [1]; new_lens_dev int32 [n_seqs]: they may be the same buffers as n_free_dev and lens_dev
  *   q_start_dev     out int32 [n_seqs + 1]; slots_dev out int64 [n_tokens], positions_dev out int32 [n_tokens]
  * A call that cannot be carried out as a whole changes no pages and no stack: a length or count below 0, a sequence past
- * max_pages pages, more tokens than n_tokens, too few free pages, a stack that would outgrow free_capacity. It raises
- * JAB_ERR_INVALID_ARG on the device, new_lens = lens, new_free = n_free, and all rows are padding (q_start all 0). A page
- * number outside the cache raises it too; the token's slot is then -1. n_seqs up to 8192, max_pages * page_tokens < 2^30. */
+ * max_pages pages, more tokens than n_tokens, too few free pages, a stack that would outgrow free_capacity, a page number
+ * outside the cache among those that would go back. It raises JAB_ERR_INVALID_ARG on the device, new_lens = lens, new_free =
+ * n_free, and all rows are padding (q_start all 0). In jab_kv_plan a page number outside the cache (in a table or on the stack)
+ * raises it too, and the token's slot is then -1. A page must be in one place alone: on the stack, or in the table of one
+ * sequence (of the first shared_len tokens: of all); this is not checked. n_seqs up to 8192, max_pages * page_tokens < 2^30. */
 jab_status jab_kv_release(const jab_kv_cache* cache, int32_t n_seqs, const int32_t* lens_dev, const int32_t* ended_dev,
                           const int32_t* pages_dev, int32_t max_pages, int32_t shared_len, int32_t* free_dev,
                           int32_t free_capacity, const int32_t* n_free_dev, int32_t* new_lens_dev, int32_t* new_free_dev,

@@ -80,10 +80,9 @@ struct Sums {
 };
 __device__ __forceinline__ int pages_of(const PlanParams& p, int n) { return n > 0 ? p.by_page.quot(n - 1) + 1 : 0; }  // (n <= 2^30)
 
-// The pages that come or go: each warp of `warps` a run of them, a lane eight at a time (their numbers are on the way together).
-template <bool RELEASE>
-__device__ __forceinline__ void move_pages(const PlanParams& p, const Sums& s, int warp, int warps) {
-  const int n = s.pages, run = ((n + warps - 1) / warps + 31) / 32 * 32, same = RELEASE ? p.shared / p.page : 0;
+// The pages that come: each warp of `warps` a run of them, a lane eight at a time (their numbers are on the way together).
+__device__ __forceinline__ void take_pages(const PlanParams& p, const Sums& s, int warp, int warps) {
+  const int n = s.pages, run = ((n + warps - 1) / warps + 31) / 32 * 32;
   const int64_t first = (int64_t)warp * run, end = min(first + run, (int64_t)n);
   int b = -1;
   for (int64_t i0 = first + (threadIdx.x & 31); i0 < end; i0 += 256) {
@@ -97,11 +96,10 @@ __device__ __forceinline__ void move_pages(const PlanParams& p, const Sums& s, i
       if (i64 >= end) continue;
       const int i = (int)i64;
       b = b < 0 ? owner(s.page, p.n_seqs, i) : walk(s.page, p.n_seqs, i, b);
-      const int entry = (RELEASE ? same : pages_of(p, s.len[b])) + i - s.page[b], at = RELEASE ? s.n_free + i : s.n_free - 1 - i;
+      const int entry = pages_of(p, s.len[b]) + i - s.page[b], at = s.n_free - 1 - i;
       if (!in_bounds(entry, p.max_pages, p.status) || !in_bounds(at, p.free_capacity, p.status)) continue;
       int32_t* table = p.pages + (int64_t)b * p.max_pages + entry;
-      int32_t* stack = p.free_pages + at;
-      from[u] = RELEASE ? table : stack, to[u] = RELEASE ? stack : table;
+      from[u] = p.free_pages + at, to[u] = table;
       id[u] = *from[u];
     }
 #pragma unroll
@@ -111,6 +109,43 @@ __device__ __forceinline__ void move_pages(const PlanParams& p, const Sums& s, i
       *to[u] = id[u];
     }
   }
+}
+
+// The pages that go, in the same way, once all their numbers are known to be the cache's: else nothing is written and the answer is
+// false. A warp's numbers stay in registers between the two where it has no more than 256 (8192 pages in all). Called by the whole block.
+__device__ __forceinline__ bool give_pages(const PlanParams& p, const Sums& s, int warp, int warps) {
+  const int n = s.pages, run = ((n + warps - 1) / warps + 31) / 32 * 32, same = p.shared / p.page;
+  const int64_t first = (int64_t)warp * run, end = min(first + run, (int64_t)n), begin = first + (threadIdx.x & 31);
+  int b = -1, id[8];
+  auto fetch = [&](int64_t i0) {
+    bool fine = true;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int64_t i64 = i0 + 32 * u;
+      id[u] = 0;
+      if (i64 >= end) continue;
+      const int i = (int)i64;
+      b = b < 0 ? owner(s.page, p.n_seqs, i) : walk(s.page, p.n_seqs, i, b);
+      const int entry = same + i - s.page[b];
+      if (in_bounds(entry, p.max_pages, p.status)) id[u] = p.pages[(int64_t)b * p.max_pages + entry];
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) fine = fine && id[u] >= 0 && id[u] < p.n_pages;
+    return fine;
+  };
+  bool fine = true;
+  for (int64_t i0 = begin; i0 < end; i0 += 256) fine = fetch(i0) && fine;
+  if (!__syncthreads_and(fine)) return false;
+  b = -1;
+  for (int64_t i0 = begin; i0 < end; i0 += 256) {
+    if (run > 256) fetch(i0);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int64_t i = i0 + 32 * u;
+      if (i < end && in_bounds(s.n_free + i, p.free_capacity, p.status)) p.free_pages[s.n_free + i] = id[u];
+    }
+  }
+  return true;
 }
 
 // Slots and positions of all rows, padding behind the last: as above, four rows of a lane at a time.
@@ -184,6 +219,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_plan_kernel(const __grid_const
       g += pages_for(len_s[b], count);
     }
   __syncthreads();
+  Sums sums{len_s, row_s, page_s, n_free, bad ? 0 : (int)all_pages, bad ? 0 : (int)all_rows};
+  if (RELEASE && !bad) bad = !give_pages(p, sums, tid >> 5, kWarps);
   // (in place: every thread has read the stack's size, and a sequence's length and count are read by one thread alone)
   for (int b = b0; b < b1; ++b) {
     int to;
@@ -201,10 +238,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv_plan_kernel(const __grid_const
     if (!RELEASE) p.q_start[p.n_seqs] = bad ? 0 : (int)all_rows;
     if (bad) report(p.status, JAB_ERR_INVALID_ARG);
   }
-  if (!RELEASE && p.n_tokens > kRowsInOne) return;
-  Sums sums{len_s, row_s, page_s, n_free, bad ? 0 : (int)all_pages, bad ? 0 : (int)all_rows};
-  move_pages<RELEASE>(p, sums, tid >> 5, kWarps);
-  if (!RELEASE) write_rows(p, sums, tid >> 5, kWarps);
+  if (RELEASE || p.n_tokens > kRowsInOne) return;
+  take_pages(p, sums, tid >> 5, kWarps);
+  write_rows(p, sums, tid >> 5, kWarps);
 }
 
 // Pages and rows behind a first launch that did the rest (a call that it refused has no rows).
@@ -233,7 +269,7 @@ __global__ void __launch_bounds__(kRowThreads) kv_rows_kernel(const __grid_const
   __syncthreads();
   const Sums sums{len_s, row_s, page_s, *p.new_free + (int)all_pages, (int)all_pages, p.q_start[p.n_seqs]};
   const int warp = blockIdx.x * (kRowThreads / 32) + (tid >> 5), warps = gridDim.x * (kRowThreads / 32);
-  move_pages<false>(p, sums, warp, warps);
+  take_pages(p, sums, warp, warps);
   write_rows(p, sums, warp, warps);
 }
 

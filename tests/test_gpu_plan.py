@@ -149,6 +149,35 @@ def test_page_numbers_outside_the_cache():
     assert po.tolist() == list(range(20, 32)) + list(range(20, 34)) and qs.tolist() == [0, 12, 26]
 
 
+@pytest.mark.parametrize("number", ["-1", "one past the last", "least", "most"])
+@pytest.mark.parametrize("B,each,page,which", [(1, 1, 16, 0), (3, 5, 16, 7), (40, 3, 64, 119), (300, 60, 16, 12345), (300, 60, 16, 17999)])
+def test_a_release_of_page_numbers_outside_the_cache_changes_nothing(B, each, page, which, number):
+    """One bad entry among the pages that would go back, the first and the last among them, with as many pages as stay in registers and
+    with more; a bad entry that does not go back stays unseen."""
+    s = State([each * page] * B, each + 2, page, 1, spare=5)
+    bad = {"-1": -1, "one past the last": s.total, "least": -2 ** 31, "most": 2 ** 31 - 1}[number]
+    good, s.pages[which // each][which % each] = s.pages[which // each][which % each], bad
+    for in_place in (False, True):
+        dl, dp, df, dn = s.device()
+        keep, n0 = df.tolist(), dn.tolist()
+        nl, nn = (None, None) if in_place else (torch.empty_like(dl), torch.empty_like(dn))
+        J.jab_kv_release(s.cache, dl, _i32([1] * B), dp, df, dn, new_lens=nl, new_free=nn)
+        assert J.jab_get_device_status() == 1
+        assert (dl if in_place else nl).tolist() == s.lens and (dn if in_place else nn).tolist() == n0
+        assert df.tolist() == keep and dp.tolist() == s.pages
+    dl, dp, df, dn = s.device()
+    ended = [int(b != which // each) for b in range(B)]
+    J.jab_kv_release(s.cache, dl, _i32(ended), dp, df, dn)  # (that sequence goes on)
+    lens, free, n = R.release(s.lens, ended, s.pages, s.free, s.n_free, page, 0)
+    assert dl.tolist() == lens and df.tolist() == free and dn.tolist() == [n] and J.jab_get_device_status() == 0
+    s.pages[which // each][which % each] = good
+    s.pages[0][each] = bad  # (behind the sequence's pages)
+    dl, dp, df, dn = s.device()
+    J.jab_kv_release(s.cache, dl, _i32([1] * B), dp, df, dn)
+    lens, free, n = R.release(s.lens, [1] * B, s.pages, s.free, s.n_free, page, 0)
+    assert dl.tolist() == lens and df.tolist() == free and dn.tolist() == [n] and J.jab_get_device_status() == 0
+
+
 def test_long_prompts_in_a_graph():
     """Release and plan in place with more rows than one launch writes, captured once and replayed with other counts, until the pages
     run out: that call changes nothing, and the one after a release goes on."""
