@@ -50,7 +50,8 @@ typedef enum {
   JAB_ERR_NONFINITE = 4,     /* device: scale <= 0 or non-finite, or a non-finite result          */
   JAB_ERR_RANGE = 5,         /* device: a value does not fit the fp16 tensor-core operands: X, the
                                 quantised weights, the projected Q|K|V or the output error dO
-                                (|x| > 65504 after rounding)                                    */
+                                (|x| > 65504 after rounding); or the fp16 results of a call
+                                that says so                                                    */
   JAB_ERR_TIMEOUT = 6,       /* device: a bounded wait in a pipelined kernel gave up             */
   JAB_ERR_SCRATCH_LIMIT = 7, /* jab_loss_forward_noalloc: the problem needs more scratch than the
                                 fixed JAB_NOALLOC_SCRATCH_BYTES                                    */
@@ -463,7 +464,7 @@ jab_status jab_fp8_quantize(int64_t M, int32_t K, const void* X_dev, jab_dtype t
  *   w_scales_dev  fp32 [ceil(N / block_rows), ceil(K / 128)]; block_rows 1 or 128
  *   Y_dev         out y_type [M, N], pitch ldy
  * K a multiple of 16 up to 131072; M >= 0 (0: nothing to do), N >= 1. ws 256-byte aligned. Sums run in a fixed order:
- * repeated calls give the same bits. */
+ * repeated calls give the same bits. Results in fp16 that do not fit are infinite and raise JAB_ERR_RANGE on the device. */
 size_t jab_fp8_linear_workspace_size(int64_t M, int32_t N, int32_t K);
 jab_status jab_fp8_linear(int64_t M, int32_t N, int32_t K, const void* X_dev, jab_dtype x_type, int64_t ldx,
                           const void* codes_dev, const float* w_scales_dev, int32_t block_rows, void* Y_dev,

@@ -117,6 +117,21 @@ __device__ __forceinline__ uint32_t pair_of(float a, float b, int type) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
+// Results in fp16 that do not fit: from halfway past its largest (65504) on. (Sums of tokens and channels that are not there are 0, or NaN
+// by what lies in the place of their scales; the maximum passes NaNs over.)
+__device__ __forceinline__ float larger(float big, float2 v) { return fmaxf(big, fmaxf(fabsf(v.x), fabsf(v.y))); }
+__device__ __forceinline__ void check_range(float big, const F8Params& p) {
+  if (big >= 65520.f) report(p.status, JAB_ERR_RANGE);
+}
+template <int N>
+__device__ __forceinline__ void check_range(const float2 (&sums)[N], const F8Params& p) {
+  if (p.y_type != JAB_FP16) return;
+  float big = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) big = larger(big, sums[i]);
+  check_range(big, p);
+}
+
 template <int NTOK, bool ROWS>
 __global__ void __launch_bounds__(Cfg<NTOK>::THREADS, 1)
     fp8_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const __grid_constant__ F8Params p) {
@@ -342,6 +357,12 @@ __global__ void __launch_bounds__(Cfg<NTOK>::THREADS, 1)
             for (int j = 0; j < 8; ++j) sum[j] += c0 + j < all ? load_cluster(at + j * TM * 4) : 0.f;
           }
           if (n >= p.N) continue;
+          if (p.y_type == JAB_FP16) {
+            float big = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) big = larger(big, make_float2(sum[j], sum[j + 1]));
+            check_range(big, p);
+          }
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             const int64_t at = (t0 + c0 + j) * p.ldy + n;
@@ -350,6 +371,7 @@ __global__ void __launch_bounds__(Cfg<NTOK>::THREADS, 1)
         }
         break;
       }
+      check_range(acc, p);
       __syncwarp();
       if (words && cols == HALF && n0 + TM <= p.N) {
         // lanes 2i and 2i + 1 exchange a token: the even one stores the first of two, the odd one the second
@@ -599,6 +621,7 @@ __global__ void __launch_bounds__(PairCfg::THREADS, 1)
           }
         }
         if (!ok) break;
+        check_range(acc, p);
         if (wide && n0 + COLS / 2 <= p.N) {
           uint8_t* y = static_cast<uint8_t*>(p.y) + (m0 * p.ldy + n0) * size;
           const int rows = (int)max((int64_t)0, min((int64_t)32, p.M - m0));
@@ -681,6 +704,7 @@ __global__ void __launch_bounds__(PairCfg::THREADS, 1)
           if (lane == 0) tc::mbar_arrive(&bars->sempty[s]);
         }
         if (!ok) break;
+        check_range(acc, p);
         if (wide && n0 + COLS / 2 <= p.N) {
           uint8_t* y = static_cast<uint8_t*>(p.y) + (m0 * p.ldy + n0) * size;
           const int rows = (int)max((int64_t)0, min((int64_t)32, p.M - m0));

@@ -224,6 +224,29 @@ def test_linear_zeros_and_nonfinite():
     assert y[:, 7].isnan().all() and y[:, :7].isfinite().all() and y[:, 8:].isfinite().all()
 
 
+@pytest.mark.parametrize("M,N,K", [(1, 129, 256), (1, 256, 2048), (40, 130, 2048), (130, 384, 2048), (130, 20000, 272), (3000, 1024, 256), (3000, 1021, 272)])
+@pytest.mark.parametrize("rows", [1, 128])
+@pytest.mark.parametrize("left_over", [0xFF, 0x7F])
+def test_linear_results_that_do_not_fit_fp16(M, N, K, rows, left_over):
+    """One result of 448 * 2 * 73.125 = 65520, halfway between the largest fp16 and what would come next, which rounds to an infinity;
+    the fp32 below it rounds to 65504. Whatever the workspace holds."""
+    ws = torch.empty(J.jab_fp8_linear_workspace_size(M, N, K), dtype=torch.uint8, device="cuda")
+    for m, n, k, sign in ((0, 0, 0, 1), (M - 1, N - 1, K - 1, -1), (M // 2, N // 2, K // 2, 1)):
+        x = torch.zeros((M, K), dtype=BF, device="cuda")
+        codes, scales = torch.zeros((N, K), device="cuda"), torch.ones((-(-N // rows), -(-K // 128)), device="cuda")
+        x[m, k], codes[n, k] = 448.0, 2.0 * sign
+        edge = torch.tensor(73.125)
+        for s, dt, status in ((edge, HF, 5), (torch.nextafter(edge, torch.zeros(())), HF, 0), (edge, BF, 0), (edge, F, 0), (edge * 1e30, HF, 5)):
+            scales[n // rows, k // 128] = s
+            ws.fill_(left_over)
+            y = torch.full((M, N), 7.0, dtype=dt, device="cuda")
+            J.jab_fp8_linear(x, codes.to(F8), scales, y, ws, block_rows=rows)
+            assert J.jab_get_device_status() == status
+            want = torch.zeros((M, N), device="cuda")
+            want[m, n] = 896.0 * sign * s.item()
+            assert torch.equal(y, want.to(dt))
+
+
 def test_linear_in_a_graph_and_on_another_stream():
     g = _gen(11)
     x = torch.randn((37, 768), generator=g, device="cuda").to(HF)
