@@ -699,6 +699,8 @@ def _heads(t, n: int, heads: int, dh: int, like, name: str):
     """(pointer, pitch) of rows of `heads` heads; no such heads: (None, 0)."""
     if heads == 0:
         return None, 0
+    if t is None:
+        raise ValueError(f"{name} is needed: there are {heads} heads of it")
     if t.dtype is not like.dtype:
         raise ValueError(f"{name} must have x's type")
     return _rows(t, heads * dh, name, n)

@@ -135,3 +135,12 @@ def test_binding_refuses_wrong_tensors(J):
         J._norm_rope(2, 64, None, None, False, None, x, None)
     with pytest.raises(ValueError):
         J._norm_rope(2, 64, None, (x, x), False, None, None, None)
+
+
+def test_binding_refuses_missing_heads(J):
+    import torch
+    x = torch.zeros((2, 128))
+    assert J._heads(None, 2, 0, 64, x, "q") == (None, 0)
+    for name in ("q", "k", "dq", "dk"):
+        with pytest.raises(ValueError, match=f"{name} is needed"):
+            J._heads(None, 2, 1, 64, x, name)
