@@ -646,6 +646,8 @@ def jab_rope_table_scaled(cos, sin, theta: float, kind: str = "plain", factor: f
     """cos and sin of the angles position * f_j into fp32 [length, rotary_dim / 2] each, times `attention`. f_j = theta^(-2j /
     rotary_dim) ("plain"), divided by factor ("linear"), or that for pairs of low_turns and fewer in original_length
     tokens, unchanged for those of high_turns and more and in between in between ("by_parts")."""
+    if kind not in _ROPE_KINDS:
+        raise ValueError(f"kind must be one of {', '.join(_ROPE_KINDS)}, got {kind!r}")
     scaling = _RopeScaling(_ROPE_KINDS[kind], float(factor), float(original_length), float(low_turns), float(high_turns),
                            float(attention))
     st = lib().jab_rope_table_scaled(cos.shape[0], 2 * cos.shape[1], float(theta), ctypes.byref(scaling),

@@ -144,3 +144,9 @@ def test_binding_refuses_missing_heads(J):
     for name in ("q", "k", "dq", "dk"):
         with pytest.raises(ValueError, match=f"{name} is needed"):
             J._heads(None, 2, 1, 64, x, name)
+
+
+def test_binding_refuses_unknown_kinds_of_tables(J):
+    import torch
+    with pytest.raises(ValueError, match="kind must be one of"):
+        J.jab_rope_table_scaled(torch.zeros((4, 32)), torch.zeros((4, 32)), 1e4, kind="other")
