@@ -191,6 +191,147 @@ def test_write(n, hq, hk, dh, page, dt, bits, part, inter, norm):
     assert J.jab_get_device_status() == 0
 
 
+def _near(got, exact, mag, dt):
+    """Outputs in type dt: seven roundings of 2^-24 of the magnitudes (the norm's factor rounded the other way is two of them), then half
+    a step."""
+    bound = mag * 7 * 2.0 ** -24 * 1.01 + exact.abs() * HALF_STEP[dt] * 1.01 + (2.0 ** -24 if dt == HF else 2.0 ** -126)
+    assert bool(((got.double() - exact).abs() <= bound).all())
+
+
+def _written(codes, scales, bits, exact, mag):
+    """Codes and scales of rows [..., dh] against the 64-bit rows: a scale is the largest element (off by e) over qmax, rounded; a code
+    lies within half a step of the element over its scale, the element off by e and the quotient by 2^-24 of itself."""
+    qmax = 2 ** (bits - 1) - 1
+    c = (codes if bits == 8 else torch.stack((codes & 15, codes >> 4), -1).flatten(-2)).double() - 2 ** (bits - 1)
+    e, s = mag * 7 * 2.0 ** -24 * 1.01, scales.double()
+    assert bool(((s - exact.abs().amax(-1) / qmax).abs() <= e.amax(-1) / qmax * 1.01 + s * 2.0 ** -24 * 1.01).all())
+    zero = s == 0
+    assert not c[zero].any() and not exact[zero].any()
+    c, e, exact, s = c[~zero], e[~zero], exact[~zero], s[~zero][:, None]
+    assert bool((c.abs() <= qmax).all()) and bool(((c - exact / s).abs() <= 0.5 + e / s + (exact / s).abs() * 2.0 ** -24 * 1.01).all())
+
+
+def _ones(s):
+    """The weights that a missing one stands for."""
+    one = torch.ones_like(s["wq"] if s["wq"] is not None else s["wk"]) if s["wq"] is not None or s["wk"] is not None else None
+    return dict(s, wq=one if s["wq"] is None else s["wq"], wk=one if s["wk"] is None else s["wk"])
+
+
+def _exact(s, hq, hk, dh, inter):
+    """(outputs, magnitudes) of the heads of Q and K in 64 bits."""
+    s = _ones(s)
+    a = dict(s, x=s["x"].abs(), rope=tuple(t.abs() for t in s["rope"]), wq=None if s["wq"] is None else s["wq"].abs(), wk=None if s["wk"] is None else s["wk"].abs())
+    return _want(s, hq, hk, dh, inter, R.norm_rope64, torch.float64), _want(a, hq, hk, dh, inter, _sums, torch.float64)
+
+
+def _check_write(s, n, hq, hk, dh, dt, bits, page, inter, slots):
+    """Every row that has a slot, Q and cache, within bounds of the 64-bit values; nothing else is touched."""
+    pages = -(-(int(slots.max()) + 1) // page) + 1
+    cache = J.KvCache(hk, dh, bits, page, pages)
+    q = torch.full((n, hq * dh), 3.0, dtype=dt, device="cuda")
+    J.jab_kv_write_norm_rope(cache, s["x"], hq, slots, q_out=q, **_how(s, inter))
+    exact, mag = _exact(s, hq, hk, dh, inter)
+    live = slots >= 0
+    assert bool(live.any())
+    _near(q.view(n, hq, dh)[live], exact[live, :hq], mag[live, :hq], dt)
+    assert bool((q[~live] == 3).all())
+    at = slots[live]
+    v = s["x"].double()[:, (hq + hk) * dh : (hq + 2 * hk) * dh].reshape(n, hk, dh)[live]
+    take = lambda t: t[at // page, :, at % page]  # noqa: E731
+    _written(take(cache.k_codes), take(cache.k_scales), bits, exact[live, hq:], mag[live, hq:])
+    _written(take(cache.v_codes), take(cache.v_scales), bits, v, torch.zeros_like(v))
+    touched = torch.zeros((pages, page), dtype=torch.bool, device="cuda")
+    touched[at // page, at % page] = True
+    for t in cache._tensors:
+        assert not t.transpose(1, 2)[~touched].any()
+    assert J.jab_get_device_status() == 0
+
+
+@pytest.mark.parametrize("n,hq,hk,dh,page", [(1, 32, 8, 128, 64), (1, 4, 1, 64, 16), (1, 1, 3, 128, 48), (2, 12, 12, 64, 16), (130, 5, 1, 64, 32), (700, 12, 4, 128, 16)])
+@pytest.mark.parametrize("dt,bits", [(BF, 8), (BF, 4), (HF, 8), (HF, 4), (F, 8), (F, 4)])
+@pytest.mark.parametrize("part,inter,norm", [(1, False, True), (2, True, True), (4, False, False), (1, True, False)])
+def test_write_of_every_row(n, hq, hk, dh, page, dt, bits, part, inter, norm):
+    s = _inputs(n, hq, hk, hk, dh, dt, part, n + 3, norm)
+    slots = torch.randperm((n // page + 2) * page, generator=_gen(n), device="cuda")[:n].contiguous()
+    if n > 2:
+        slots[n // 3] = -1
+    _check_write(s, n, hq, hk, dh, dt, bits, page, inter, slots)
+
+
+WIDTHS = [(128, w) for w in range(16, 129, 16)] + [(64, w) for w in range(16, 65, 16)]
+
+
+@pytest.mark.parametrize("dh,rotary", WIDTHS)
+@pytest.mark.parametrize("dt", [BF, HF, F])
+@pytest.mark.parametrize("inter", [False, True])
+def test_rotations_of_every_width(dh, rotary, dt, inter):
+    """Forward, gradient and cache for every number of elements that may be turned, with and without a norm."""
+    n, hq, hk = 45, 5, 2
+    for norm in (False, True):
+        s = _inputs(n, hq, hk, hk, dh, dt, 1, rotary, norm)
+        s["rope"] = tuple(t.float().cuda() for t in R.table(600, rotary, 1e4))
+        q, k = (torch.full((n, h * dh), 3.0, dtype=dt, device="cuda") for h in (hq, hk))
+        J.jab_qk_norm_rope(s["x"], hq, hk, dh, q, k, **_how(s, inter))
+        got = torch.cat((q, k), 1).view(n, hq + hk, dh)
+        _near(got, *_exact(s, hq, hk, dh, inter), dt)
+        _same_rows(got.reshape(-1, dh), _want(s, hq, hk, dh, inter).to(dt).reshape(-1, dh), norm)
+        for bits in (8, 4):
+            _check_write(s, n, hq, hk, dh, dt, bits, 16, inter, torch.randperm(48, generator=_gen(1), device="cuda")[:n].contiguous())
+        _check_backward(s, n, hq, hk, dh, dt, inter)
+
+
+def _check_backward(s, n, hq, hk, dh, dt, inter):
+    """dx and the weights' gradients (of the weights that there are, or of all) against autograd in 64 bits: bounds as in test_backward,
+    for fewer than 256 tokens (a thread adds up at most two rows)."""
+    norm = s["eps"] is not None
+    g = _gen(n)
+    dq, dk = ((torch.randn((n, h * dh), generator=g, device="cuda")).to(dt) for h in (hq, hk))
+    dx, dwq, dwk = _backward(s, hq, hk, dh, dq, dk, inter, norm)
+    x = s["x"][:, : (hq + hk) * dh].double().reshape(n, hq + hk, dh).requires_grad_()
+    cos, sin = (t[s["pos"].long()].double() for t in s["rope"])
+    one = torch.ones(dh, device="cuda")
+    ws = [(one if s[k] is None else s[k]).double().requires_grad_() for k in ("wq", "wk")] if norm else []
+    w = torch.cat((ws[0].expand(hq, dh), ws[1].expand(hk, dh))) if norm else None
+    R.norm_rope64(x, w, s["eps"], cos, sin, inter).backward(torch.cat((dq, dk), 1).double().view(n, hq + hk, dh))
+    mag = gm = _sums(torch.cat((dq, dk), 1).double().view(n, hq + hk, dh).abs(), None, None, cos.abs(), sin.abs(), inter)
+    if norm:
+        r = 1 / torch.sqrt(x.detach().square().mean(-1, keepdim=True) + 1e-6)
+        xn, um = (x.detach() * r).abs(), gm * w.detach().abs()
+        mag = r * (um + xn * (um * xn).mean(-1, keepdim=True))
+        for got, want, sl in ((dwq, ws[0].grad, slice(0, hq)), (dwk, ws[1].grad, slice(hq, None))):
+            top = (gm * xn)[:, sl].sum((0, 1))
+            assert bool(((got.double() - want).abs() <= top * (2.0 ** -19 + 74 * 2.0 ** -24) + 2.0 ** -126).all())
+    bound = mag * 2.0 ** -19 + x.grad.abs() * HALF_STEP[dt] * 1.01 + (2.0 ** -24 if dt == HF else 2.0 ** -126)
+    assert bool(((dx.double().view_as(x) - x.grad).abs() <= bound).all()) and J.jab_get_device_status() == 0
+
+
+@pytest.mark.parametrize("dt", [BF, HF, F])
+@pytest.mark.parametrize("which", ["wq", "wk", "neither"])
+def test_weights_of_q_or_of_k_alone(dt, which):
+    n, hq, hk, dh = 60, 6, 2, 128
+    s = _inputs(n, hq, hk, hk, dh, dt, 2, 8)
+    for k in ("wq", "wk"):
+        if k != which:
+            s[k] = None
+    q, k = (torch.empty((n, h * dh), dtype=dt, device="cuda") for h in (hq, hk))
+    J.jab_qk_norm_rope(s["x"], hq, hk, dh, q, k, **_how(s, True))
+    _near(torch.cat((q, k), 1).view(n, hq + hk, dh), *_exact(s, hq, hk, dh, True), dt)
+    _check_write(s, n, hq, hk, dh, dt, 8, 32, True, torch.arange(n, device="cuda"))
+    _check_backward(s, n, hq, hk, dh, dt, True)
+
+
+@pytest.mark.parametrize("eps", [1e-30, 1e-5, 10.0, 1e30])
+@pytest.mark.parametrize("size", [1e-12, 1.0, 1e15, 1e18])
+def test_norm_of_any_size_in_64_bits(eps, size):
+    """Every row: the factor at most two of 2^-24 off, the product one."""
+    x = torch.randn((400, 128), generator=_gen(7), device="cuda").clamp(-2, 2) * size
+    q, k = torch.empty_like(x[:, :64]).contiguous(), torch.empty_like(x[:, :64]).contiguous()
+    J.jab_qk_norm_rope(x, 1, 1, 64, q, k, norm_eps=eps)
+    want = R.norm_rope64(x.double().view(-1, 2, 64), None, eps, None, None, False)
+    assert bool(((torch.stack((q, k), 1).double() - want).abs() <= want.abs() * 3 * 2.0 ** -24 * 1.01 + 2.0 ** -126).all())
+    assert J.jab_get_device_status() == 0
+
+
 def test_write_without_norm_is_the_plain_write():
     s = _inputs(200, 12, 4, 4, 128, HF, 1, 3, norm=False)
     a, b = (J.KvCache(4, 128, 8, 32, 8) for _ in range(2))
