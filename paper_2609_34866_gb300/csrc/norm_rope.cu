@@ -292,7 +292,7 @@ cudaError_t launch_rope_table(const RopeTableArgs& a, cudaStream_t st) {
     }
     p.freq_pi[j] = f / pi;
   }
-  return launch_after(rope_table_kernel, (unsigned)((a.length + kRun - 1) / kRun), 64, 0, st, p);
+  return launch_after(rope_table_kernel, (unsigned)((a.length - 1) / kRun + 1), 64, 0, st, p);
 }
 
 }  // namespace jab

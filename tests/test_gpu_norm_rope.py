@@ -6,6 +6,8 @@ rotation's three roundings are 6 of 2^-24 (a factor rounded the other way 7) of 
 Gradients, each of at most 32 roundings in a chain (products with r, w, cos and sin, a sum of 16 products and one over 8
 lanes): 2^-19 of the sums of magnitudes; a weight's gradient adds up `per` rows a thread, 32 to 64 heads and the blocks' parts
 as pairs: (per + 64 + 8) 2^-24 more."""
+import math
+
 import pytest
 import torch
 
@@ -461,3 +463,21 @@ def test_plain_table_is_the_table():
     J.jab_rope_table(*a, 10000.0)
     J.jab_rope_table_scaled(*b, 10000.0)
     assert bool((torch.stack(a) - torch.stack(b)).abs().max() <= 2.0 ** -24)
+
+
+def test_the_longest_table():
+    """Every length that the call takes. Positions of 2^31 over pi are rounded twice to 2^-53 of themselves: 2^-22 of the angle, and half a
+    step of fp32."""
+    if torch.cuda.mem_get_info()[0] < 160 << 30:
+        pytest.skip("139 GB of tables")
+    length = 2 ** 31 - 1
+    cos, sin = (torch.empty((length, 8), device="cuda") for _ in range(2))
+    try:
+        cos[-40:], sin[-40:] = 7.0, 7.0
+        J.jab_rope_table_scaled(cos, sin, 1e4)
+        for p in (0, 1, 2 ** 30 + 3, length - 17, length - 16, length - 15, length - 1):
+            assert abs(cos[p, 0].item() - math.cos(p)) <= 2.0 ** -21 and abs(sin[p, 0].item() - math.sin(p)) <= 2.0 ** -21, p
+        assert bool((cos[-40:].square() + sin[-40:].square() - 1).abs().max() <= 2.0 ** -22)
+    finally:
+        del cos, sin
+        torch.cuda.empty_cache()
