@@ -70,7 +70,7 @@ __device__ __forceinline__ void codes8(const float (&x)[8], float s, uint32_t (&
 
 // What becomes of a row: the rotation of all of Q and K and the cache; a norm for each head, the rotation of a part of it and the
 // cache; the same and an output for K. Bound of the latter two: instructions (issue slots 61 %) and bytes; 16384 tokens of 48 heads of
-// 128 into the cache take 111 us (without the norm 84; 370 MB), 40 heads that go to no cache 77 us (60; 336 MB).
+// 128 into the cache take 107 us (without the norm 80, where kWrite takes 70; 370 MB), 40 heads that go to no cache 77 us (60; 336 MB).
 enum Mode { kWrite, kWriteNormed, kRows };
 
 // Blocks go over the tokens and a token's heads, a row of DH elements by DH / 16 threads, each with elements [8t, 8t + 8)
@@ -89,7 +89,7 @@ __global__ void __launch_bounds__(kWriteThreads, sizeof(T) == 2 ? 2 : 1) kv_writ
   // The thread's groups of 8: partners of a rotation by halves where it turns them, else neighbours.
   const bool turns = !NORMED || 16 * t < p.rotary;
   const int at0 = NORMED && (p.neighbours || !turns) ? 16 * t : 8 * t;
-  const int at1 = !NORMED ? at0 + DH / 2 : p.neighbours || !turns ? at0 + 8 : at0 + p.rotary / 2;
+  const int gap = !NORMED ? DH / 2 : p.neighbours || !turns ? 8 : p.rotary / 2;  // from the first to the second
   if constexpr (NORMED) {
     for (int i = threadIdx.x; i < 2 * DH; i += blockDim.x) {
       const float* w = i < DH ? p.wq : p.wk;
@@ -115,8 +115,8 @@ __global__ void __launch_bounds__(kWriteThreads, sizeof(T) == 2 ? 2 : 1) kv_writ
   };
   auto fetch = [&](int64_t token, int head) {
     if (head < p.n_heads && (head >= p.n_q || p.q_out != nullptr)) {
-      const T* row = static_cast<const T*>(p.x) + token * p.ldx + (int64_t)head * DH;
-      lo.load(row + at0), hi.load(row + at1);
+      const T* row = static_cast<const T*>(p.x) + token * p.ldx + (int64_t)head * DH + at0;
+      lo.load(row), hi.load(row + gap);
     }
   };
   int64_t token = blockIdx.x;
@@ -139,7 +139,7 @@ __global__ void __launch_bounds__(kWriteThreads, sizeof(T) == 2 ? 2 : 1) kv_writ
       if (p.eps > 0.f && __any_sync(0xffffffffu, live && is_k)) {  // (not for warps that have heads of V alone)
         const float r = norm_factor<LANES>(a, b, p.eps);
         if (live && is_k) {
-          const float2 *w0 = reinterpret_cast<const float2*>(weights[is_q ? 0 : 1] + at0), *w1 = reinterpret_cast<const float2*>(weights[is_q ? 0 : 1] + at1);
+          const float2 *w0 = reinterpret_cast<const float2*>(weights[is_q ? 0 : 1] + at0), *w1 = reinterpret_cast<const float2*>(weights[is_q ? 0 : 1] + at0 + gap);
           const float2 r2 = make_float2(r, r);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
@@ -183,11 +183,12 @@ __global__ void __launch_bounds__(kWriteThreads, sizeof(T) == 2 ? 2 : 1) kv_writ
       if (is_q || MODE == kRows) {
         const int n = is_q ? p.n_q : p.n_kv;
         const int64_t ld = MODE != kRows ? (int64_t)p.n_q * DH : is_q ? p.ldq : p.ldk;
-        const int64_t at = now * ld + (is_q ? row : row - p.n_q) * DH;
+        // (rows of Q without a pitch by the sum that has none: by the other one 1024 fp32 tokens of 48 heads of 128 take 9.7 us for 8.8)
+        const int64_t at = MODE != kRows ? (now * p.n_q + row) * DH + at0 : now * ld + (is_q ? row : row - p.n_q) * DH + at0;
         T* out = static_cast<T*>(is_q ? p.q_out : p.k_out) + at;
-        if (in_bounds(at + max(at0, at1) + 7, (p.n_tokens - 1) * ld + (int64_t)n * DH, p.status)) {
-          store(out + at0, a);
-          store(out + at1, b);
+        if (in_bounds(at + gap + 7, (p.n_tokens - 1) * ld + (int64_t)n * DH, p.status)) {
+          store(out, a);
+          store(out + gap, b);
         }
         // finite, but not in Q's type (or neither): from halfway past the largest fp16 (65504) on
         if (std::is_same<T, half_t>::value && !(big < 65520.f)) report(p.status, JAB_ERR_RANGE);
@@ -212,10 +213,10 @@ __global__ void __launch_bounds__(kWriteThreads, sizeof(T) == 2 ? 2 : 1) kv_writ
     const int64_t pg = p.page_shift >= 0 ? to >> p.page_shift : to / p.page;
     const int64_t r = (pg * p.n_kv + h) * p.page + (to - pg * p.page);
     if (!in_bounds(r, p.n_slots * p.n_kv, p.status)) continue;
-    uint8_t* codes = (is_k ? p.k_codes : p.v_codes) + r * (DH * BITS / 8);
+    uint8_t* codes = (is_k ? p.k_codes : p.v_codes) + r * (DH * BITS / 8) + at0 * BITS / 8;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
-      uint8_t* to8 = codes + (half ? at1 : at0) * BITS / 8;
+      uint8_t* to8 = codes + (half ? gap * BITS / 8 : 0);
       if constexpr (BITS == 8)
         *reinterpret_cast<uint2*>(to8) = make_uint2(w[half][0], w[half][1]);
       else
