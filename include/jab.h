@@ -369,7 +369,7 @@ typedef struct {
 
 /* Y[m, n] = s_m w_n sum_k qx[m, k] codes[n, k]: the rows of X are quantised to 8 bits (one scale s_m per
  * token), the sum is exact (whole numbers). Rounded to fp32 it is multiplied by s_m, then by w_n, each
- * product rounded to fp32, before the result is rounded to y_type.
+ * product rounded to fp32, before the result is rounded to y_type (to an infinity where it does not fit).
  *   X_dev         x_type (JAB_FP16 or JAB_BF16) [M, K], pitch ldx
  *   codes_dev     int8 [N, K] (jab_quantize with group_size = d_model, any bit width), 16-byte aligned
  *   w_scales_dev  fp32 [N]
@@ -456,7 +456,8 @@ jab_status jab_fp8_quantize(int64_t M, int32_t K, const void* X_dev, jab_dtype t
 /* Y[m, n] = sum_b sx[m, b] w_scales[n / block_rows, b] sum_{k in block b} qx[m, k] codes[n, k], blocks of 128 of K: the rows
  * of X are quantised as by jab_fp8_quantize with block_rows = 1. A block's sum is fp32, as the tensor cores add it up, its
  * products with the two scales and the sum over the blocks are rounded to fp32, the result to y_type. (With block_rows =
- * 128 the two scales are multiplied first: a product of theirs below 2^-126 loses bits.)
+ * 128 the two scales are multiplied first: a product of theirs below 2^-126 loses bits, and one past fp32 is infinite, which
+ * makes a block's sum of 0 NaN.)
  * The codes of jab_quantize of up to 5 bits at group_size = 128 are e4m3 numbers as they are: a fitted block is served with
  * them and its scales, block_rows = 1.
  *   X_dev         x_type (any of the three) [M, K], pitch ldx

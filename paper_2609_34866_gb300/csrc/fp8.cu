@@ -100,7 +100,8 @@ __global__ void __launch_bounds__(256) fp8_rows_kernel(const __grid_constant__ Q
 }
 
 // 128 rows x 128 columns by a block of threads, in registers. Bound: bytes in flight; 6144 x 4096 of bf16 take 16.2 us with five blocks an
-// SM (48 registers), 20.3 with three (74) and 31 with seven (spilled); 16384 x 8192 67 us, 6.0 TB/s.
+// SM (48 registers and 44 bytes in local memory), 20.3 with three (74) and 31 with seven (more in local memory); 16384 x 8192 67 us, 6.0
+// TB/s. fp32, three blocks an SM (80 registers, 12 bytes in local memory): 6144 x 4096 in 23 us, 5.4 TB/s.
 template <class T>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 5 : 3) fp8_blocks_kernel(const __grid_constant__ QuantParams p) {
   __shared__ float top[8];

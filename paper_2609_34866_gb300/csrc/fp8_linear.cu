@@ -12,11 +12,14 @@
 // brings the scales, eight that read out, scale and add up. Many tiles: persistent blocks. Few tiles: one a cluster, whose blocks
 // take ranges of K and add their sums through shared memory in a fixed order. Many tokens: pairs of blocks, further down.
 //
-// Bound: 8192 tokens x 6144 x 4096 with scales for 128 x 128 weights take 238 us, 21 of them for the tokens' codes: 1.73 PFLOP/s, 0.87
-// of the tensor cores' measured bf16 rate; with a scale for every row's 128 321 us (two operations an element in the read-out, 1660
-// clocks a block of K). One token (25 MB of codes) takes 9.3 us where the bytes take 3.8: two launches, the copies' latency and
-// eleven stages' products and read-outs. (Codes of up to 16 tokens made in the product's own kernel: no faster there, and 5.8 us
-// instead of 5.0 for 1 x 2304 x 768, as the weights' copies cannot begin before the launch before has ended.)
+// Bound: 8192 tokens x 6144 x 4096 with scales for 128 x 128 weights take 238 us, 21 of them for the tokens' codes: 1.73 PFLOP/s, 0.45 of
+// the 3.85 that an e4m3 product with one scale for all reaches here (8192^3). It is the round trip of the accumulators that takes the time
+// (further down), not the products: the tensor pipe is 38 % active. With a scale for every row's 128 321 us (two operations an element in
+// the read-out, 1700 clocks a block of K). One token (25 MB of codes) takes 9.3 us where the weights are in L2 (three sets in turn), 11.2
+// where they are not (twelve), and the bytes take 3.8: two launches, the copies' latency and sixteen stages' products and read-outs on 96
+// SMs (a third K range would need clusters of three, of which fewer than 48 fit). (Codes of up to 16 tokens made in the product's own
+// kernel: no faster there, and 5.8 us instead of 5.0 for 1 x 2304 x 768, as the weights' copies cannot begin before the launch before has
+// ended.)
 #include <cudaTypedefs.h>
 
 #include <algorithm>
@@ -405,15 +408,16 @@ __global__ void __launch_bounds__(Cfg<NTOK>::THREADS, 1)
 }
 
 // ------------------------------------------------------------------ many tokens: pairs of blocks
-// Two blocks of a cluster on two SMs share a tile of 256 tokens x 256 channels: either has 128 of the tokens (its lanes) and the
-// codes of half of the channels, so that a stage is 32 KB a block. Lanes are tokens here: with channels on them every lane
-// would read every token's scale from shared memory, a pass of its own each (8 warps x 128 columns: 1000 clocks for a block of
-// K whose products take 512). With block_rows = 128 a lane has one factor for a block of K; with block_rows = 1 tensor memory is
-// read in the shape that gives a thread two of eight columns, whose scales are 32 passes a warp.
-// Bound: a block of K takes 1130 clocks. Its products take 820 behind one another; with two accumulators of 256 columns (all of
-// tensor memory) one is free again 500 clocks for the barrier of its last product, 450 for the read-out and 400 for the arrival and
-// the next issue after that. Three accumulators of 160 columns (263 us where this took 256) and one block a tile (277) were no faster:
-// a pair's products take 1300 clocks from issue to the barrier however short they are, a block's own 48 KB a stage 950.
+// Two blocks of a cluster on two SMs share a tile of 256 tokens x 256 channels: either has 128 of the tokens (its lanes) and the codes of
+// half of the channels, so that a stage is 32 KB a block. Lanes are tokens here: with channels on them every lane would read every token's
+// scale from shared memory, a pass of its own each (8 warps x 128 columns: 1000 clocks for a block of K whose products would take 512 at
+// the tensor cores' nominal rate). With block_rows = 128 a lane has one factor for a block of K; with block_rows = 1 tensor memory is read
+// in the shape that gives a thread two of eight columns, whose scales are 32 passes a warp. Bound: a block of K takes 1130 clocks. Its
+// products take 820 behind one another, as measured; with two accumulators of 256 columns (all of tensor memory) one is free again 500
+// clocks for the barrier of its last product, 450 for the read-out and 400 for the arrival and the next issue after that. Three
+// accumulators of 160 columns (263 us where this took 256) and one block a tile (277) were no faster: a pair's products take 1300 clocks
+// from issue to the barrier however short they are, a block's own 48 KB a stage 950. (The form with block_rows = 128 has 104 bytes of a
+// thread's state in local memory: registers are allotted for 168 a thread before they are moved.)
 struct PairCfg {
   static constexpr int ST = 5, STAGE = 2 * TM * BK, THREADS = 384, DST = 2, COLS = 256;
   static constexpr int OUT = 32 * 128;  // a warp's place for 128 bytes of 32 rows on their way out

@@ -69,8 +69,10 @@ __device__ __forceinline__ void codes8(const float (&x)[8], float s, uint32_t (&
 }
 
 // What becomes of a row: the rotation of all of Q and K and the cache; a norm for each head, the rotation of a part of it and the
-// cache; the same and an output for K. Bound of the latter two: instructions (issue slots 61 %) and bytes; 16384 tokens of 48 heads of
+// cache; the same and an output for K. Bound of the latter two: instructions (issue slots 61 to 65 %) and bytes; 16384 tokens of 48 heads of
 // 128 into the cache take 107 us (without the norm 80, where kWrite takes 70; 370 MB), 40 heads that go to no cache 77 us (60; 336 MB).
+// The 16-bit instances into the cache are held to 80 registers by two blocks of 384 threads an SM and have 16 to 56 bytes of a
+// thread in local memory; fp16 rows that go to no cache 4.
 enum Mode { kWrite, kWriteNormed, kRows };
 
 // Blocks go over the tokens and a token's heads, a row of DH elements by DH / 16 threads, each with elements [8t, 8t + 8)
@@ -299,8 +301,8 @@ cudaError_t write_as(const WriteParams& p, int sms, cudaStream_t st) {
   // A block has a token's heads, or as many of them as kWriteThreads threads take. With four tokens for every SM and more, a
   // third of the heads where that leaves no thread idle: it loads a token's angles once for its rows in turn (2048 tokens of 48
   // heads of 128: 19 us for writing and reading, 22 without; but 64 tokens 4.9 instead of 4.5).
-  // With a norm, or without a cache, the smallest share of whole warps from 64 threads on: 16384 tokens of 40 heads of 128 take 76 us
-  // with 64 threads, 84 with 160; of 48 heads into the cache 116 with 64, 119 with 128.
+  // With a norm, or without a cache, the smallest share of whole warps from 64 threads on: 16384 tokens of 40 heads of 128 take 77 us
+  // with 64 threads, 84 with 160; of 48 heads into the cache 111 with 64, 117 with 128 (107 with 64 as it is now).
   constexpr int PER_SM = sizeof(T) == 2 ? 768 : 512;
   const int want = p.n_heads * (DH / 16);
   int share = want;

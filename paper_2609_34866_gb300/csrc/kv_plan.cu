@@ -3,7 +3,7 @@
 // One block sums the counts of all sequences up and writes what may be overwritten in place (lengths, the stack's size) when it
 // has read it; with few rows it also moves the pages and writes the rows, with many a second launch does, whose blocks sum up
 // again what the first has left (250000 rows of 1000 sequences: 28 us for release and plan where one block moves the pages). Bound:
-// launches and chains of dependent reads (counts, sums, page numbers): 64 single tokens take 3.6 us.
+// launches and chains of dependent reads (counts, sums, page numbers): 64 single tokens take 4.7 us, the release before them 3.7.
 #include <algorithm>
 
 #include "common.cuh"
